@@ -146,7 +146,16 @@ typedef enum coda_epi_kind {
            nblk = coda_row_partial_blocks(N), every entry overwritten; combine with coda_lse_finalize)
            out3[i] = v[i][y[i]]  (f32[M], the target logit; written by the tile that holds column y[i]).
        in3: int32 y[M] with 0 <= y < N (not checked; an out-of-range y leaves out3[i] unwritten).       */
-    CODA_EPI_LSE_PARTIAL = 10
+    CODA_EPI_LSE_PARTIAL = 10,
+    /* The ops below belong to coda_gemm_scaled, which describes the 8-bit form with block scales. */
+    /* Final op: v in 8 bits.  out: codes [M x W] (ld_out), out2: scales, i0 = pitch of the scales.                        */
+    CODA_EPI_STORE_Q8 = 11,
+    /* SWIGLU_FWD ahead of STORE_Q8, N a multiple of 32.  Optional out: codes [M x N] (ld_out) of the pre-activation v, the
+       checkpoint that SWIGLU_BWD_Q8 reads; out2: its scales, i0 = their pitch.                                            */
+    CODA_EPI_SWIGLU_FWD_Q8 = 12,
+    /* SWIGLU_BWD ahead of STORE_Q8.  in: codes [M x 2N] (ld_in) of Z, in2: their scales, i0 = pitch of the scales.  Optional
+       out2: f32 row statistic as in SWIGLU_BWD, laid out per `flags`, on the values before they are rounded.              */
+    CODA_EPI_SWIGLU_BWD_Q8 = 13
 } coda_epi_kind;
 
 #define CODA_REDUCE_PARTIALS 0u
@@ -297,6 +306,71 @@ CODA_API coda_status coda_fold_gamma(void *stream, const coda_mat *W, const floa
    W_out is bf16 [K x 2N] with row pitch ld_out (elements). */
 CODA_API coda_status coda_interleave_pairs(void *stream, const coda_mat *Wa, const coda_mat *Wb, void *W_out,
                                   int64_t ld_out);
+
+/*
+ * 8 bits with a scale for each block of 128.
+ *
+ * A matrix [R x C] in 8 bits is its codes, OCP E4M3 bytes [R x C] with a row pitch, and its scales, E8M0 bytes: byte s stands for
+ * 2^(s - 127), 255 for NaN.  Blocks run along the rows, 128 columns each, the last may be narrower; scales lie block-major,
+ * scales[b * ld_scales + i] for columns 128 b .. of row i, ceil(C / 128) rows of ld_scales >= R bytes.  Element (i, j) is
+ * code(i, j) * 2^(scales[j / 128][i] - 127).  For contractions along the rows of a weight that is quantised in square blocks the second
+ * form of its scales is scales_t[b * ld_scales_t + j] for rows 128 b .. of column j, ceil(R / 128) rows of ld_scales_t >= C bytes.
+ * Code and scale pointers are 16-byte aligned and all their pitches multiples of 16; a pitch of scales is at most 2^31 - 1.  Scales are
+ * read in whole chunks of 16 bytes: those up to the next multiple of 16 rows have to be readable (the pitch has room for them), their
+ * values do not matter.  What is written ends at the last row and column.
+ *
+ * The scale of a block is the least power of two, and no less than 2^-126, with |x| <= 448 * scale for every finite x of the block;
+ * codes are x / scale to the nearest, ties to even.  A NaN or an infinity becomes the code NaN and has no part in the scale.
+ */
+
+/* X [R x C] bf16 (trans 0, C a multiple of 8) -> codes and scales.  square == 0: blocks of 1 x 128, for activations, gradients and
+   checkpoints; scales_t must be NULL.  square != 0: blocks of 128 x 128, for weights: one set of codes serves A W and A W^T, with `scales`
+   where the contraction runs along the columns of X and scales_t (may be NULL) where it runs along its rows. */
+CODA_API coda_status coda_quantize(void *stream, const coda_mat *X, int32_t square, void *codes, int64_t ld_codes, void *scales,
+                          int64_t ld_scales, void *scales_t, int64_t ld_scales_t);
+
+/* Q (CODA_F8E4M3, [R x C], trans 0, C a multiple of 8) and its scales -> bf16 [R x C]: a checkpoint for the ops that read bf16 (the C of
+   RMSNORM_BWD).  Exact but for values below 2^-133. */
+CODA_API coda_status coda_dequantize(void *stream, const coda_mat *Q, const void *scales, int64_t ld_scales, void *out, int64_t ld_out);
+
+/*
+ * coda_gemm on operands in 8 bits with block scales: D = A op(B) (fp32 accumulate), then the program.
+ *
+ * A: CODA_F8E4M3 [M x K] (trans 0); scales_a [ceil(K / 128)][>= M].  B: CODA_F8E4M3, [N x K] (trans 1) or [K x N] (trans 0); scales_b
+ * [ceil(K / 128)][>= N], one for each block of the contraction and column of D: the first form of a B stored [N x K], the second of one
+ * stored [K x N].  K and N are multiples of 16, M is free.  K == 0 runs the program on D = 0.
+ *
+ * Programs: those of coda_gemm but ACCUM_F32 (for weight gradients see coda_grad_scaled), and
+ *     [ROW_SCALE] STORE_Q8
+ *     [ROW_SCALE] SWIGLU_FWD_Q8 STORE_Q8
+ *     SWIGLU_BWD_Q8 STORE_Q8
+ * whose outputs are 8-bit matrices with scales for blocks of 1 x 128.
+ *
+ * Accuracy: products are exact, scales powers of two; the sums of the 8-bit matrix instructions are off by some 1.3e-5 of the result's
+ * 2-norm, whatever K is (fp32 sums of exact products, as with bf16 operands: 2e-7).
+ *
+ * workspace / workspace_bytes: device memory, 16-byte aligned; may be NULL.  With coda_gemm_scaled_workspace_bytes(M, N, K) bytes (0: no
+ * use for any) shapes with few output tiles divide the contraction among workgroups, which leave fp32 partials there for a second
+ * kernel.  A non-NULL workspace that is smaller is CODA_ERR_WORKSPACE.  It holds nothing between calls; two calls that share one must not
+ * overlap in time.  The order of additions depends on the sizes, the layout of B and whether a workspace is given.
+ */
+CODA_API coda_status coda_gemm_scaled(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const void *scales_a, int64_t ld_scales_a,
+                             const coda_mat *B, const void *scales_b, int64_t ld_scales_b, const coda_epi_op *prog /* host */, int32_t n_ops,
+                             void *workspace, size_t workspace_bytes);
+CODA_API size_t coda_gemm_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/*
+ * The weight gradient from 8-bit checkpoints: G[i][j] += sum_t a[t][i] * b[t][j] over K tokens, in fp32, in place.
+ * A: CODA_F8E4M3 as stored [K x M], trans 1, with its scales [ceil(M / 128)][>= K] (blocks along the features, as the forward pass left
+ * them).  B as stored [K x N], trans 0: CODA_F8E4M3 with scales [ceil(N / 128)][>= K], or CODA_BF16 with scales_b NULL.  M, and N of an
+ * 8-bit B, are multiples of 16, N of a bf16 B of 8; K is free.  G: f32 [M x N], 16-byte aligned, ld_g a multiple of 4.
+ * Elements are widened to bf16 with their scale (exact but below 2^-133) and summed in fp32 by the bf16 matrix instructions.
+ * workspace: as above, coda_grad_scaled_workspace_bytes(M, N, K) bytes.
+ */
+CODA_API coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const void *scales_a, int64_t ld_scales_a,
+                             const coda_mat *B, const void *scales_b, int64_t ld_scales_b, float *G, int64_t ld_g, void *workspace,
+                             size_t workspace_bytes);
+CODA_API size_t coda_grad_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
 CODA_API const char *coda_status_string(coda_status s);
 /* The hipError_t (as int) recorded by the most recent CODA_ERR_LAUNCH on this thread. */

@@ -36,12 +36,14 @@ CODA_OK, CODA_ERR_NULL, CODA_ERR_SHAPE, CODA_ERR_ALIGN, CODA_ERR_DTYPE, CODA_ERR
     CODA_ERR_WORKSPACE, CODA_ERR_LAUNCH = range(8)
 CODA_BF16, CODA_F32, CODA_F8E4M3 = 0, 1, 2
 (CODA_EPI_ROW_SCALE, CODA_EPI_COL_SCALE_SIDE, CODA_EPI_ADD_TILE, CODA_EPI_SWIGLU_FWD, CODA_EPI_SWIGLU_BWD,
- CODA_EPI_ROW_SUMSQ, CODA_EPI_STORE, CODA_EPI_ACCUM_F32, CODA_EPI_ROPE, CODA_EPI_RMSNORM_BWD, CODA_EPI_LSE_PARTIAL) = range(11)
+ CODA_EPI_ROW_SUMSQ, CODA_EPI_STORE, CODA_EPI_ACCUM_F32, CODA_EPI_ROPE, CODA_EPI_RMSNORM_BWD, CODA_EPI_LSE_PARTIAL,
+ CODA_EPI_STORE_Q8, CODA_EPI_SWIGLU_FWD_Q8, CODA_EPI_SWIGLU_BWD_Q8) = range(14)
 CODA_REDUCE_PARTIALS, CODA_REDUCE_ATOMIC, CODA_STORE_F32 = 0, 1, 2
 
 EXPORTS = ["coda_gemm", "coda_gemm_static_ws", "coda_gemm_workspace_bytes", "coda_row_partial_blocks", "coda_row_finalize",
            "coda_col_partial_blocks", "coda_col_finalize", "coda_lse_finalize",
-           "coda_row_sumsq", "coda_fold_gamma", "coda_interleave_pairs", "coda_status_string",
+           "coda_row_sumsq", "coda_fold_gamma", "coda_interleave_pairs", "coda_quantize", "coda_dequantize",
+           "coda_gemm_scaled", "coda_gemm_scaled_workspace_bytes", "coda_grad_scaled", "coda_grad_scaled_workspace_bytes", "coda_status_string",
            "coda_last_hip_error"]
 EXPORTS_UNFUSED = ["coda_unfused_rmsnorm_apply", "coda_unfused_swiglu_fwd", "coda_unfused_swiglu_bwd",
                    "coda_unfused_add_sumsq", "coda_unfused_accumulate"]
@@ -84,6 +86,18 @@ _lib.coda_fold_gamma.restype = ctypes.c_int
 _lib.coda_fold_gamma.argtypes = [_vp, ctypes.POINTER(coda_mat), _vp, _vp, _i64]
 _lib.coda_interleave_pairs.restype = ctypes.c_int
 _lib.coda_interleave_pairs.argtypes = [_vp, ctypes.POINTER(coda_mat), ctypes.POINTER(coda_mat), _vp, _i64]
+_lib.coda_quantize.restype = ctypes.c_int
+_lib.coda_quantize.argtypes = [_vp, _vp, _i32, _vp, _i64, _vp, _i64, _vp, _i64]
+_lib.coda_dequantize.restype = ctypes.c_int
+_lib.coda_dequantize.argtypes = [_vp, _vp, _vp, _i64, _vp, _i64]
+_lib.coda_gemm_scaled.restype = ctypes.c_int
+_lib.coda_gemm_scaled.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i32, _vp, ctypes.c_size_t]
+_lib.coda_gemm_scaled_workspace_bytes.restype = ctypes.c_size_t
+_lib.coda_gemm_scaled_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_lib.coda_grad_scaled.restype = ctypes.c_int
+_lib.coda_grad_scaled.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, ctypes.c_size_t]
+_lib.coda_grad_scaled_workspace_bytes.restype = ctypes.c_size_t
+_lib.coda_grad_scaled_workspace_bytes.argtypes = [_i64, _i64, _i64]
 _lib.coda_status_string.restype = ctypes.c_char_p
 _lib.coda_status_string.argtypes = [ctypes.c_int]
 _lib.coda_last_hip_error.restype = ctypes.c_int
@@ -213,6 +227,36 @@ def store(out, f32=False):
     return _op(coda_epi_op, CODA_EPI_STORE, CODA_STORE_F32 if f32 else 0, None, out, None, None, None, None, None, 0, 0)
 
 
+def _q8(t, scales, what):
+    """Codes and scales are 2-D tensors of bytes; the pitch of the scales."""
+    assert t.dim() == 2 and t.element_size() == 1 and (t.shape[1] <= 1 or t.stride(1) == 1), "%s: a row-major 2-D tensor of codes expected" % what
+    return _scales(scales, (t.shape[1] + 127) // 128, t.shape[0], what)
+
+
+def _scales(scales, blocks, rows, what):
+    """The pitch of scale bytes [blocks x rows].  A tensor of one block may be a row of any pitch."""
+    assert scales.dim() == 2 and scales.element_size() == 1 and (scales.shape[1] <= 1 or scales.stride(1) == 1), "%s: a row-major 2-D tensor of scale bytes expected" % what
+    assert scales.shape[0] >= blocks and scales.shape[1] >= rows, "%s: scales of %d blocks x %d rows expected" % (what, blocks, rows)
+    return scales.stride(0) if scales.shape[0] > 1 else max(scales.stride(0), scales.shape[1])
+
+
+def store_q8(out, scales):
+    """out: codes [M x W]; scales: bytes [ceil(W / 128) x M], pitch a multiple of 16.  coda_gemm_scaled only, like the next two."""
+    return _op(coda_epi_op, CODA_EPI_STORE_Q8, 0, None, out, scales, None, None, None, None, _q8(out, scales, "store_q8"), 0)
+
+
+def swiglu_fwd_q8(preact_out=None, preact_scales=None):
+    """preact_out, preact_scales: codes [M x N] and scale bytes [ceil(N / 128) x M] of the pre-activation, or None."""
+    pitch = 0 if preact_out is None else _q8(preact_out, preact_scales, "swiglu_fwd_q8")
+    return _op(coda_epi_op, CODA_EPI_SWIGLU_FWD_Q8, 0, None, preact_out, preact_scales, None, None, None, None, pitch, 0)
+
+
+def swiglu_bwd_q8(Z, Z_scales, stat_out=None, atomic=False):
+    """Z, Z_scales: what swiglu_fwd_q8 left, codes [M x 2N] and scale bytes [ceil(2N / 128) x M]."""
+    return _op(coda_epi_op, CODA_EPI_SWIGLU_BWD_Q8, CODA_REDUCE_ATOMIC if atomic else CODA_REDUCE_PARTIALS, Z, None, stat_out, Z_scales, None, None, None,
+               _q8(Z, Z_scales, "swiglu_bwd_q8"), 0)
+
+
 def accum_f32(G):
     return _op(coda_epi_op, CODA_EPI_ACCUM_F32, 0, None, G, None, None, None, None, None, 0, 0)
 
@@ -306,6 +350,59 @@ def coda_fold_gamma(W, gamma, W_out, stream=None):
 def coda_interleave_pairs(Wa, Wb, W_out, stream=None):
     a, b = mat(Wa), mat(Wb)
     _check(_lib.coda_interleave_pairs(_stream(stream), ctypes.byref(a), ctypes.byref(b), _ptr(W_out), W_out.stride(0)))
+
+
+# --- 8 bits with a scale for each block of 128: codes and scales are uint8 (or float8_e4m3fn, float8_e8m0fnu) tensors -------
+def _at(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def coda_quantize(X, codes, scales, scales_t=None, square=False, stream=None):
+    """X: bf16 [R x C]; codes: [R x C]; scales: bytes [ceil(C / 128) x R]; with square blocks optionally scales_t: [ceil(R / 128) x C]."""
+    m = mat(X)
+    assert codes.shape == X.shape, "codes of X's shape expected"
+    pitch = _q8(codes, scales, "coda_quantize")
+    pitch_t = 0 if scales_t is None else _scales(scales_t, (X.shape[0] + 127) // 128, X.shape[1], "coda_quantize")
+    _check(_lib.coda_quantize(_stream(stream), ctypes.byref(m), 1 if square else 0, codes.data_ptr(), codes.stride(0), scales.data_ptr(), pitch,
+                              _ptr(scales_t), pitch_t))
+
+
+def coda_dequantize(codes, scales, out, stream=None):
+    """codes, scales -> out: bf16 [R x C]."""
+    m = mat(codes)
+    assert out.dim() == 2 and out.shape == codes.shape and out.dtype == _torch.bfloat16, "a bf16 output of the codes' shape expected"
+    _check(_lib.coda_dequantize(_stream(stream), ctypes.byref(m), scales.data_ptr(), _q8(codes, scales, "coda_dequantize"), out.data_ptr(), out.stride(0)))
+
+
+def coda_gemm_scaled(A, scales_a, B, scales_b, ops, transB=False, stream=None, workspace=None):
+    """D = A op(B), then the epilogue ops.  A: codes [M x K], scales_a: bytes [ceil(K / 128) x M]; B: codes [K x N], or [N x K] with transB,
+    scales_b: bytes [ceil(K / 128) x N].  workspace: optional, coda_gemm_scaled_workspace_bytes(M, N, K) bytes."""
+    a, b = mat(A), mat(B, transB)
+    (M, K), N = A.shape, B.shape[0] if transB else B.shape[1]
+    blocks = (K + 127) // 128
+    ops = list(ops)
+    arr, n = _prog(ops)
+    _check(_lib.coda_gemm_scaled(_stream(stream), M, N, K, ctypes.byref(a), scales_a.data_ptr(), _scales(scales_a, blocks, M, "scales_a"), ctypes.byref(b),
+                                 scales_b.data_ptr(), _scales(scales_b, blocks, N, "scales_b"), arr, n, *_at(workspace)))
+
+
+def coda_gemm_scaled_workspace_bytes(M, N, K):
+    return _lib.coda_gemm_scaled_workspace_bytes(M, N, K)
+
+
+def coda_grad_scaled(A, scales_a, B, scales_b, G, stream=None, workspace=None):
+    """G [M x N] f32 += A^T B over the K rows of both.  A: codes [K x M], scales_a: bytes [ceil(M / 128) x K]; B: codes [K x N] with scales_b, or
+    bf16 [K x N] with scales_b None.  workspace: optional, coda_grad_scaled_workspace_bytes(M, N, K) bytes."""
+    a, b = mat(A, True), mat(B)
+    (K, M), N = A.shape, B.shape[1]
+    assert G.dim() == 2 and G.shape == (M, N) and G.dtype == _torch.float32 and (N <= 1 or G.stride(1) == 1), "a row-major f32 [M x N] gradient expected"
+    pitch_b = 0 if scales_b is None else _scales(scales_b, (N + 127) // 128, K, "scales_b")
+    _check(_lib.coda_grad_scaled(_stream(stream), M, N, K, ctypes.byref(a), scales_a.data_ptr(), _scales(scales_a, (M + 127) // 128, K, "scales_a"),
+                                 ctypes.byref(b), _ptr(scales_b), pitch_b, G.data_ptr(), G.stride(0), *_at(workspace)))
+
+
+def coda_grad_scaled_workspace_bytes(M, N, K):
+    return _lib.coda_grad_scaled_workspace_bytes(M, N, K)
 
 
 def coda_status_string(status):

@@ -6,6 +6,8 @@
 #include "aux_kernels.hpp"
 #include "gemm_launch.hpp"
 #include "narrow_launch.hpp"
+#include "q8.hpp"
+#include "scaled_launch.hpp"
 #include "small_launch.hpp"
 #include "splitk_plan.hpp"
 
@@ -56,13 +58,31 @@ coda_status check_vec(const void *p)
     return aligned4(p) ? CODA_OK : CODA_ERR_ALIGN;
 }
 
+// An 8-bit tile [M x width]: codes at `p`, scales [ceil(width / 128)][>= M] at `s`.
+coda_status check_scales(const void *s, int64_t ld, int64_t rows)
+{
+    if (!s) return CODA_ERR_NULL;
+    if (ld < rows || ld > INT32_MAX) return CODA_ERR_SHAPE;
+    return aligned16(s) && (ld & 15) == 0 ? CODA_OK : CODA_ERR_ALIGN;
+}
+coda_status check_q8_tile(const void *p, int64_t ld, int64_t width, const void *s, int64_t ld_s, int64_t M)
+{
+    if (!p) return CODA_ERR_NULL;
+    if (ld < width || ld > MAX_LD) return CODA_ERR_SHAPE;
+    if (!aligned16(p) || (ld & 15)) return CODA_ERR_ALIGN;
+    return check_scales(s, ld_s, M);
+}
+
 struct Parsed {
     int mode = -1;
     coda::GemmParams p{};
+    bool q8 = false;               // the program ends in STORE_Q8: mode is a Q8Mode
+    coda::Q8Params q{};
 };
 
 // Canonical order: ROW_SCALE < ADD_TILE < ROW_SUMSQ < COL_SCALE_SIDE < final; ROPE only between ROW_SCALE and STORE.
-coda_status parse_program(const coda_epi_op *prog, int32_t n_ops, int64_t N, Parsed &out)
+// `scaled`: the programs of coda_gemm_scaled, which has those that end in STORE_Q8 and no ACCUM_F32.
+coda_status parse_program(const coda_epi_op *prog, int32_t n_ops, int64_t M, int64_t N, bool scaled, Parsed &out)
 {
     if (n_ops < 0 || (n_ops > 0 && !prog)) return CODA_ERR_NULL;
     coda::GemmParams &p = out.p;
@@ -70,10 +90,12 @@ coda_status parse_program(const coda_epi_op *prog, int32_t n_ops, int64_t N, Par
     int pair = 0;            // 0 none, 1 swiglu fwd, 2 swiglu bwd
     bool final_seen = false;
     bool linear_only = false;  // an op that only the linear program supports was used
+    int q8_pair = 0;           // 0 none, 1 SWIGLU_FWD_Q8, 2 SWIGLU_BWD_Q8: only STORE_Q8 may follow
     bool rmsbwd = false;       // RMSNORM_BWD seen: only ADD_TILE and a bf16 STORE may follow
     for (int i = 0; i < n_ops; ++i) {
         const coda_epi_op &op = prog[i];
         if (final_seen) return CODA_ERR_PROGRAM;
+        if (q8_pair && op.kind != CODA_EPI_STORE_Q8) return CODA_ERR_PROGRAM;
         coda_status st;
         switch (op.kind) {
         case CODA_EPI_ROW_SCALE:
@@ -211,8 +233,50 @@ coda_status parse_program(const coda_epi_op *prog, int32_t n_ops, int64_t N, Par
             final_seen = true;
             break;
         }
+        case CODA_EPI_SWIGLU_FWD_Q8:
+            if (!scaled || stage > 1 || pair || rmsbwd) return CODA_ERR_PROGRAM;
+            if (N & 31) return CODA_ERR_SHAPE;             // rows of the halved width are whole chunks of 16 codes
+            if (op.flags != 0) return CODA_ERR_PROGRAM;
+            if (op.out) {
+                if ((st = check_q8_tile(op.out, op.ld_out, N, op.out2, op.i0, M)) != CODA_OK) return st;
+                out.q.z = static_cast<uint8_t *>(op.out);
+                out.q.ldz = op.ld_out;
+                out.q.z_s = static_cast<uint8_t *>(op.out2);
+                out.q.ld_z_s = op.i0;
+            }
+            q8_pair = 1;
+            break;
+        case CODA_EPI_SWIGLU_BWD_Q8:
+            if (!scaled || stage > 0 || pair || rmsbwd) return CODA_ERR_PROGRAM;
+            if ((st = check_q8_tile(op.in, op.ld_in, 2 * N, op.in2, op.i0, M)) != CODA_OK) return st;
+            out.q.z = static_cast<uint8_t *>(const_cast<void *>(op.in));
+            out.q.ldz = op.ld_in;
+            out.q.z_s = static_cast<uint8_t *>(const_cast<void *>(op.in2));
+            out.q.ld_z_s = op.i0;
+            if ((op.flags & ~1u) != 0) return CODA_ERR_PROGRAM;
+            if (op.out2) {
+                if ((st = check_vec(op.out2)) != CODA_OK) return st;
+                p.rowred = static_cast<float *>(op.out2);
+                p.rowred_mode = (op.flags & CODA_REDUCE_ATOMIC) ? coda::ROWRED_ATOMIC : coda::ROWRED_PARTIALS;
+            }
+            q8_pair = 2;
+            break;
+        case CODA_EPI_STORE_Q8: {
+            if (!scaled || pair || rmsbwd || stage > 1) return CODA_ERR_PROGRAM;
+            if (op.flags != 0) return CODA_ERR_PROGRAM;
+            const int64_t width = q8_pair == 1 ? N / 2 : q8_pair == 2 ? 2 * N : N;
+            if ((st = check_q8_tile(op.out, op.ld_out, width, op.out2, op.i0, M)) != CODA_OK) return st;
+            out.q.out = static_cast<uint8_t *>(op.out);
+            out.q.ld_out = op.ld_out;
+            out.q.out_s = static_cast<uint8_t *>(op.out2);
+            out.q.ld_out_s = op.i0;
+            out.q8 = true;
+            out.mode = q8_pair == 1 ? coda::Q8_SWIGLU_FWD : q8_pair == 2 ? coda::Q8_SWIGLU_BWD : coda::Q8_LINEAR;
+            final_seen = true;
+            break;
+        }
         case CODA_EPI_ACCUM_F32:
-            if (stage > 0 || pair) return CODA_ERR_PROGRAM;
+            if (scaled || stage > 0 || pair) return CODA_ERR_PROGRAM;
             if (!op.out) return CODA_ERR_NULL;
             if (op.ld_out < N || op.ld_out > MAX_LD) return CODA_ERR_SHAPE;
             if (!aligned16(op.out) || (op.ld_out & 3)) return CODA_ERR_ALIGN;
@@ -277,12 +341,17 @@ hipError_t dispatch_mode_f8(int mode, int kind, const coda::GemmParams &p, hipSt
     }
 }
 
+// Sizes that the kernels index in 32 bits; K is rounded up to whole pairs of K-steps (64 bf16 or 128 8-bit elements) there
+bool sizes_fit(int64_t M, int64_t N, int64_t K)
+{
+    return M >= 0 && N >= 0 && K >= 0 && M <= INT32_MAX - 256 && N <= INT32_MAX / 2 && K <= INT32_MAX - 128;
+}
+
 // coda_gemm proper (shared by the entry points that differ only in where the split-K workspace comes from).
 coda_status gemm_impl(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const coda_mat *B,
                       const coda_epi_op *prog, int32_t n_ops, void *workspace, size_t workspace_bytes)
 {
-    // the kernels index in 32 bits; K is rounded up to whole pairs of K-steps (64 bf16 or 128 8-bit elements) there
-    if (M < 0 || N < 0 || K < 0 || M > INT32_MAX - 256 || N > INT32_MAX / 2 || K > INT32_MAX - 128) return CODA_ERR_SHAPE;
+    if (!sizes_fit(M, N, K)) return CODA_ERR_SHAPE;
     coda_status st;
     if ((st = check_operand(A, M, K)) != CODA_OK) return st;
     if ((st = check_operand(B, K, N)) != CODA_OK) return st;
@@ -292,7 +361,7 @@ coda_status gemm_impl(void *stream, int64_t M, int64_t N, int64_t K, const coda_
     if (f8 && ((K & 15) || (A->trans && (M & 15)) || (!B->trans && (N & 15)))) return CODA_ERR_SHAPE;
     if ((K & 7) || (N & 7) || (A->trans && (M & 7))) return CODA_ERR_SHAPE;
     Parsed ps;
-    if ((st = parse_program(prog, n_ops, N, ps)) != CODA_OK) return st;
+    if ((st = parse_program(prog, n_ops, M, N, false, ps)) != CODA_OK) return st;
     if (M == 0 || N == 0) return CODA_OK;
 
     coda::GemmParams &p = ps.p;
@@ -499,6 +568,142 @@ coda_status coda_interleave_pairs(void *stream, const coda_mat *Wa, const coda_m
     return launch_status(coda::launch_interleave_pairs(
         static_cast<hipStream_t>(stream), static_cast<const uint16_t *>(Wa->ptr), Wa->ld,
         static_cast<const uint16_t *>(Wb->ptr), Wb->ld, Wa->rows, Wa->cols, static_cast<uint16_t *>(W_out), ld_out));
+}
+
+coda_status coda_quantize(void *stream, const coda_mat *X, int32_t square, void *codes, int64_t ld_codes, void *scales, int64_t ld_scales,
+                          void *scales_t, int64_t ld_scales_t)
+{
+    if (!X) return CODA_ERR_NULL;
+    if (X->dtype != CODA_BF16) return CODA_ERR_DTYPE;
+    if (X->trans || X->rows < 0 || X->cols < 0 || X->rows > INT32_MAX || X->ld < X->cols || X->ld > MAX_LD || (X->cols & 7)) return CODA_ERR_SHAPE;
+    if (!square && scales_t) return CODA_ERR_SHAPE;        // scales along the columns are those of square blocks
+    if (X->rows == 0 || X->cols == 0) return CODA_OK;
+    if (!X->ptr) return CODA_ERR_NULL;
+    if (!aligned16(X->ptr) || (X->ld & 7)) return CODA_ERR_ALIGN;
+    coda_status st;
+    if ((st = check_q8_tile(codes, ld_codes, X->cols, scales, ld_scales, X->rows)) != CODA_OK) return st;
+    if (scales_t && (st = check_scales(scales_t, ld_scales_t, X->cols)) != CODA_OK) return st;
+    if ((X->cols + 127) / 128 * ((X->rows + 15) / 16) > INT32_MAX) return CODA_ERR_SHAPE;
+    return launch_status(coda::launch_quantize(static_cast<hipStream_t>(stream), static_cast<const uint16_t *>(X->ptr), X->rows, X->cols, X->ld, square != 0,
+                                               static_cast<uint8_t *>(codes), ld_codes, static_cast<uint8_t *>(scales), ld_scales,
+                                               static_cast<uint8_t *>(scales_t), ld_scales_t));
+}
+
+coda_status coda_dequantize(void *stream, const coda_mat *Q, const void *scales, int64_t ld_scales, void *out, int64_t ld_out)
+{
+    if (!Q) return CODA_ERR_NULL;
+    if (Q->dtype != CODA_F8E4M3) return CODA_ERR_DTYPE;
+    if (Q->trans || Q->rows < 0 || Q->cols < 0 || Q->rows > INT32_MAX || (Q->cols & 7)) return CODA_ERR_SHAPE;
+    if (Q->rows == 0 || Q->cols == 0) return CODA_OK;
+    coda_status st;
+    if ((st = check_q8_tile(Q->ptr, Q->ld, Q->cols, scales, ld_scales, Q->rows)) != CODA_OK) return st;
+    if ((st = check_tile(out, ld_out, Q->cols)) != CODA_OK) return st;
+    if ((Q->cols + 127) / 128 * ((Q->rows + 31) / 32) > INT32_MAX) return CODA_ERR_SHAPE;
+    return launch_status(coda::launch_dequantize(static_cast<hipStream_t>(stream), static_cast<const uint8_t *>(Q->ptr), Q->rows, Q->cols, Q->ld,
+                                                 static_cast<const uint8_t *>(scales), ld_scales, static_cast<uint16_t *>(out), ld_out));
+}
+
+size_t coda_gemm_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (!sizes_fit(M, N, K) || M == 0 || N == 0) return 0;
+    return coda::scaled_bytes(coda::plan_scaled(M, N, K, true), M, N);
+}
+
+coda_status coda_gemm_scaled(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const void *scales_a, int64_t ld_scales_a,
+                             const coda_mat *B, const void *scales_b, int64_t ld_scales_b, const coda_epi_op *prog, int32_t n_ops, void *workspace,
+                             size_t workspace_bytes)
+{
+    if (!sizes_fit(M, N, K)) return CODA_ERR_SHAPE;
+    coda_status st;
+    if ((st = check_operand(A, M, K)) != CODA_OK) return st;
+    if ((st = check_operand(B, K, N)) != CODA_OK) return st;
+    if (A->dtype != CODA_F8E4M3 || B->dtype != CODA_F8E4M3) return CODA_ERR_DTYPE;
+    if (A->trans || (K & 15) || (N & 15)) return CODA_ERR_SHAPE;
+    if (K > 0) {
+        if (M > 0 && (st = check_scales(scales_a, ld_scales_a, M)) != CODA_OK) return st;
+        if (N > 0 && (st = check_scales(scales_b, ld_scales_b, N)) != CODA_OK) return st;
+    }
+    Parsed ps;
+    if ((st = parse_program(prog, n_ops, M, N, true, ps)) != CODA_OK) return st;
+    if (M == 0 || N == 0) return CODA_OK;
+    coda::ScaledPlan plan = coda::plan_scaled(M, N, K, workspace != nullptr);
+    if (workspace) {
+        if (!aligned16(workspace)) return CODA_ERR_ALIGN;
+        if (workspace_bytes < coda::scaled_bytes(plan, M, N)) return CODA_ERR_WORKSPACE;
+    }
+    if (plan.nsplit == 0 && !ps.q8 && ps.mode == coda::EPI_RMSNORM_BWD) plan.bm = coda::TILE_M;      // its column partials are per 256 rows
+    if (((M + plan.bm - 1) / plan.bm) * ((N + plan.bn - 1) / plan.bn) > INT32_MAX / 16) return CODA_ERR_SHAPE;
+    ps.p.M = (int)M;
+    ps.p.N = (int)N;
+    ps.p.K = (int)K;
+    coda::ScaledParams p{};
+    p.A = static_cast<const unsigned char *>(A->ptr);
+    p.B = static_cast<const unsigned char *>(B->ptr);
+    p.sa = static_cast<const unsigned char *>(scales_a);
+    p.sb = static_cast<const unsigned char *>(scales_b);
+    p.lda = A->ld;
+    p.ldb = B->ld;
+    p.ld_sa = ld_scales_a;
+    p.ld_sb = ld_scales_b;
+    p.M = (int)M;
+    p.N = (int)N;
+    p.K = (int)K;
+    p.part = static_cast<float *>(workspace);
+    return launch_status(coda::launch_gemm_scaled(plan, ps.mode, ps.q8, B->trans != 0, ps.p, ps.q, p, static_cast<hipStream_t>(stream)));
+}
+
+size_t coda_grad_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    if (!sizes_fit(M, N, K) || M == 0 || N == 0) return 0;
+    return coda::grad_bytes(coda::plan_grad(M, N, K, true), M, N);
+}
+
+coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const void *scales_a, int64_t ld_scales_a,
+                             const coda_mat *B, const void *scales_b, int64_t ld_scales_b, float *G, int64_t ld_g, void *workspace, size_t workspace_bytes)
+{
+    if (!sizes_fit(M, N, K)) return CODA_ERR_SHAPE;
+    coda_status st;
+    if ((st = check_operand(A, M, K)) != CODA_OK) return st;
+    if ((st = check_operand(B, K, N)) != CODA_OK) return st;
+    if (A->dtype != CODA_F8E4M3) return CODA_ERR_DTYPE;
+    const bool b8 = B->dtype == CODA_F8E4M3;
+    if (!A->trans || B->trans || (M & 15) || (N & (b8 ? 15 : 7))) return CODA_ERR_SHAPE;
+    if (!b8 && scales_b) return CODA_ERR_DTYPE;            // a bf16 operand has no scales
+    if (K > 0) {
+        if (M > 0 && (st = check_scales(scales_a, ld_scales_a, K)) != CODA_OK) return st;
+        if (b8 && N > 0 && (st = check_scales(scales_b, ld_scales_b, K)) != CODA_OK) return st;
+    }
+    if (M == 0 || N == 0) return CODA_OK;
+    if (!G) return CODA_ERR_NULL;
+    if (ld_g < N || ld_g > MAX_LD) return CODA_ERR_SHAPE;
+    if (!aligned16(G) || (ld_g & 3)) return CODA_ERR_ALIGN;
+    const int nsplit = coda::plan_grad(M, N, K, workspace != nullptr);
+    if (workspace) {
+        if (!aligned16(workspace)) return CODA_ERR_ALIGN;
+        if (workspace_bytes < coda::grad_bytes(nsplit, M, N)) return CODA_ERR_WORKSPACE;
+    }
+    if (((M + 255) / 256) * ((N + 255) / 256) > INT32_MAX / 16) return CODA_ERR_SHAPE;
+    coda::GemmParams g{};
+    g.M = (int)M;
+    g.N = (int)N;
+    g.K = (int)K;
+    g.out = G;
+    g.ld_out = ld_g;
+    g.out_once = coda::gradient_once(M, N, ld_g * 4, reinterpret_cast<uintptr_t>(G));
+    coda::GradParams p{};
+    p.A = static_cast<const unsigned char *>(A->ptr);
+    p.B = static_cast<const unsigned char *>(B->ptr);
+    p.sa = static_cast<const unsigned char *>(scales_a);
+    p.sb = static_cast<const unsigned char *>(scales_b);
+    p.lda = A->ld;
+    p.ldb = B->ld * (b8 ? 1 : 2);
+    p.ld_sa = ld_scales_a;
+    p.ld_sb = ld_scales_b;
+    p.M = (int)M;
+    p.N = (int)N;
+    p.K = (int)K;
+    p.part = static_cast<float *>(workspace);
+    return launch_status(coda::launch_grad_scaled(nsplit, b8, g, p, static_cast<hipStream_t>(stream)));
 }
 
 const char *coda_status_string(coda_status s)

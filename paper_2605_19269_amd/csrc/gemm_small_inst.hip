@@ -66,6 +66,17 @@ static hipError_t launch_rows(const GemmParams &p, const float *part, int nsplit
     return hipGetLastError();
 }
 
+hipError_t launch_program_rows(int mode, const GemmParams &p, const float *part, int nsplit, hipStream_t s)
+{
+    switch (mode) {
+    case EPI_LINEAR: return launch_rows<EPI_LINEAR>(p, part, nsplit, s);
+    case EPI_SWIGLU_FWD: return launch_rows<EPI_SWIGLU_FWD>(p, part, nsplit, s);
+    case EPI_SWIGLU_BWD: return launch_rows<EPI_SWIGLU_BWD>(p, part, nsplit, s);
+    case EPI_RMSNORM_BWD: return launch_rows<EPI_RMSNORM_BWD>(p, part, nsplit, s);
+    default: return launch_rows<EPI_ACCUM>(p, part, nsplit, s);
+    }
+}
+
 static SmallParams small_params(const GemmParams &p, bool f8, int chain, int rot_cols)
 {
     const int64_t esz = f8 ? 1 : 2;
@@ -91,14 +102,7 @@ hipError_t launch_gemm_small(const SmallPlan &pl, int mode, bool f8, bool ak, bo
                             : (bkc ? launch_fused<true, false>(pl.bm, mode, p, q, s) : launch_fused<false, false>(pl.bm, mode, p, q, s));
     const hipError_t e = f8 ? (bkc ? launch_tile<true, true>(pl, ak, q, s) : launch_tile<false, true>(pl, ak, q, s))
                             : (bkc ? launch_tile<true, false>(pl, ak, q, s) : launch_tile<false, false>(pl, ak, q, s));
-    if (e != hipSuccess) return e;
-    switch (mode) {
-    case EPI_LINEAR: return launch_rows<EPI_LINEAR>(p, part, pl.nsplit, s);
-    case EPI_SWIGLU_FWD: return launch_rows<EPI_SWIGLU_FWD>(p, part, pl.nsplit, s);
-    case EPI_SWIGLU_BWD: return launch_rows<EPI_SWIGLU_BWD>(p, part, pl.nsplit, s);
-    case EPI_RMSNORM_BWD: return launch_rows<EPI_RMSNORM_BWD>(p, part, pl.nsplit, s);
-    default: return launch_rows<EPI_ACCUM>(p, part, pl.nsplit, s);
-    }
+    return e != hipSuccess ? e : launch_program_rows(mode, p, part, pl.nsplit, s);
 }
 
 hipError_t launch_gemm_direct(int tile, int mode, bool f8, bool ak, bool bkc, const GemmParams &p, int chain, int rot_cols, hipStream_t s)
