@@ -35,8 +35,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # The small-tile kernels: MFMA accumulators in ordinary registers.  Workgroups of few waves and much LDS leave a wave 512
 # registers, and the compiler then keeps the accumulators in the upper half and copies them around every MFMA.
 FLAGS_SMALL = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
+SMALL = ("gemm_small", "gemm_direct", "gemm_scaled_inst", "gemm_scaled_tile_128", "grad_scaled")
 
-SOURCES = ["coda_api.hip", "aux_kernels.hip", "q8_kernels.hip", "gemm_scaled_inst.hip", "grad_scaled_inst.hip", "gemm_small_inst.hip", "gemm_narrow_inst.hip",
+SOURCES = ["coda_api.hip", "aux_kernels.hip", "q8_kernels.hip", "gemm_scaled_inst.hip", "grad_scaled_inst.hip",
+           "gemm_scaled_tile_256_nt.hip", "gemm_scaled_tile_256_nn.hip", "gemm_scaled_tile_128_nt.hip", "gemm_scaled_tile_128_nn.hip",
+           "gemm_small_inst.hip", "gemm_narrow_inst.hip",
            "gemm_direct_inst_nn.hip", "gemm_direct_inst_nt.hip", "gemm_direct_inst_tn.hip", "gemm_direct_inst_tt.hip",
            "gemm_direct_inst_f8_nn.hip", "gemm_direct_inst_f8_nt.hip", "gemm_direct_inst_f8_tn.hip", "gemm_direct_inst_f8_tt.hip",
            "gemm_inst_nn.hip", "gemm_inst_nt.hip", "gemm_inst_tn.hip", "gemm_inst_tt.hip",
@@ -55,7 +58,7 @@ def _compile(src, force):
     newest = max(os.path.getmtime(p) for p in [path] + _headers())
     if not force and os.path.exists(obj) and os.path.getmtime(obj) >= newest:
         return obj, ""
-    flags = FLAGS + (FLAGS_SMALL if src.startswith(("gemm_small", "gemm_direct", "gemm_scaled", "grad_scaled")) else [])
+    flags = FLAGS + (FLAGS_SMALL if src.startswith(SMALL) else [])
     r = subprocess.run([HIPCC] + flags + ["-Rpass-analysis=kernel-resource-usage", "-c", path, "-o", obj],
                        capture_output=True, text=True)
     text = r.stdout + r.stderr

@@ -7,9 +7,8 @@
 // byte for the lane's row of A and one for its column of B.  So the sums stay in one set of fp32 accumulators and a block costs
 // a few byte reads.  Scales lie [block][row]: the rows of a tile are BM consecutive bytes.
 //
-// The ring, its loads and waits are those of the small tiles (gemm_small.hpp).  The fragments of A are read in place: the row of
-// blocks i of the next half stage follows the MFMAs of row i of this one, which leaves 256 x 256 tiles the registers that they need
-// (two waves a SIMD, 256 registers: 128 accumulators, 32 + 32 fragments).
+// Tiles of up to 128 rows: the ring, its loads and waits are those of the small tiles (gemm_small.hpp).  256 x 256: see
+// scaled_contract_large.
 #pragma once
 #include "gemm_small.hpp"
 #include "epi_rows.hpp"
@@ -200,6 +199,282 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
     int t = 0;
     for (; t + S + (ragged ? 1 : 0) < KT; ++t) stage(t, true);
     for (; t < KT; ++t) stage(t, false);
+    __syncthreads();
+}
+
+// ---------------------------------------------------------------------------------
+// 256 x 256 tiles: eight waves of 128 x 64, two on a SIMD and one phase apart, as in the large kernel of unscaled 8-bit operands
+// (gemm_item_dl_f8).  That one's ring fills LDS: three pair slots of A (a pair of K-steps is 128 bytes of the contraction, one block)
+// and two of B, 160 KB.  The scales need room, and A's third slot is only ever half in use: the upper rows of a pair are fetched when the
+// lower rows of the pair two before have been read for good.  So A has five half slots of 16 KB -- half h of pair T at (2 T + h) mod 5 --
+// and there are 16 KB for the scales of eight pairs and for the programs' exchange.
+//   M1  even step: fetch A's lower rows of pair T+2 (over the upper rows of T-1), odd step: its upper rows (over the lower rows of T).
+//       Read the upper row fragments, odd step: the scales of pair T+1 as well, and wait for all loads but those of pair T+2
+//   C1  MFMAs of the lower rows
+//   M2  odd step: fetch B of pair T+2.  Read the lower row and the column fragments of the next step
+//   C2  MFMAs of the upper rows
+// The wave that runs a phase behind is done with what a load overwrites: its reads of the upper rows of T-1 and of B were waited for two
+// phases before; those of the lower rows of T, one phase before, are waited for in the phase that issues them (even M2).
+// Scales come for four pairs at once, a load of 256 bytes from every wave: two waves that fetched them for every pair, under a mask and out
+// of step with the others, cost 5 %.
+// 16384 x 4096 x 28672, B [K x N]: 1394 us, 2.76 PFLOP/s (unscaled 8-bit operands 1304).  Four waves of 256 x 64 with two whole slots: 1750 (their loads are in flight for half to one
+// stage, which is less than what memory takes, and one wave on a SIMD has no other to compute while it issues them).
+// ---------------------------------------------------------------------------------
+// 4 bytes a lane, straight to LDS; by all lanes or, where `mask` is 0 (else -1), none.  Without a branch: the compiler sinks MFMAs from in front of one into the
+// block behind it, and with them a compute phase into the memory phase.
+__device__ __forceinline__ void dl_load4_if(int mask, uint32_t voff, const void *sbase, uint32_t lds_addr)
+{
+    uint64_t keep;
+    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b32 exec_lo, %1\n\ts_mov_b32 exec_hi, %1\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b64 exec, %0"
+                 : "=&s"(keep)
+                 : "s"(mask), "v"(voff), "s"(sbase), "s"(lds_addr)
+                 : "memory", "m0");
+}
+
+struct ScaledLargeCfg : DlCfg<256, 256, 2, 4, 4> {
+    static constexpr int HALF = 128 * 128, A_REGION = 5 * HALF, PAIR_B = 256 * 128, B_REGION = 2 * PAIR_B, TILES = A_REGION + B_REGION;
+    static constexpr int SCALES = 512, LDS = TILES + 8 * SCALES, RED = 2 * WGN * BM * 4, EPI_RING = 128 * 1024;
+    static_assert(LDS + RED <= 160 * 1024 && EPI_RING <= TILES, "LDS");
+};
+
+// RAGGED: tiles on the edges of M and N, and K that is no whole number of blocks.
+template <class C, bool BKC, bool RAGGED>
+__device__ __forceinline__ void scaled_contract_large(Acc32<C> &acc, const ScaledParams &p, int m0, int n0, unsigned char *smem)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave & 1, wn = wave >> 1;
+    const int P = RAGGED ? (p.K + 127) / 128 : p.K / 128;            // pairs of K-steps
+    const int valid_m = RAGGED ? (p.M - m0 < 256 ? p.M - m0 : 256) : 256, valid_n = RAGGED ? (p.N - n0 < 256 ? p.N - n0 : 256) : 256;
+    acc_zero(acc);
+    // A: two wave-loads of a half slot per wave.  Local row q of half h is row (q / 64) * 128 + 64 h + q % 64 of the tile.
+    uint32_t offa[2][2], offb[4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int q = (wave * 2 + i) * 8 + (lane >> 3), r = (q >> 6) * 128 + h * 64 + (q & 63);
+            offa[h][i] = (uint32_t)((int64_t)(r < valid_m ? r : valid_m - 1) * p.lda + (((lane & 7) ^ ((q >> 1) & 7)) << 4));
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        offb[i] = BKC ? dl_goffset_pair_f8(wave * 4 + i, lane, p.ldb, valid_n) : dl_goffset_mn_f8(wave * 4 + i, lane, p.ldb, valid_n);
+    const int64_t stepb = BKC ? (int64_t)128 : 128 * p.ldb;
+    const unsigned char *ga = p.A + (int64_t)m0 * p.lda, *gb = p.B + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)smem;
+    // scales: wave w < 4 fetches A's of pair w of four, wave 4 + w B's, four rows a lane (past the last row: its chunk again; past the last
+    // pair: that one's again)
+    const bool scales_b = wave >= 4;
+    const int last = ((scales_b ? valid_n : valid_m) - 1) & ~3;
+    const uint32_t offs = (uint32_t)(lane * 4 < last ? lane * 4 : last);
+    const int64_t steps = scales_b ? p.ld_sb : p.ld_sa;
+    const unsigned char *gs = scales_b ? p.sb + n0 : p.sa + m0;
+
+    auto a_half = [&](int T, int h) { return (2 * T + h) % 5 * C::HALF; };
+    auto b_slot = [&](int T) { return C::A_REGION + (T & 1) * C::PAIR_B; };
+    auto scale_slot = [&](int T) { return C::TILES + (T & 7) * C::SCALES; };
+    auto load_or_zero = [&](bool there, uint32_t off, const unsigned char *from, int to) {
+        if (there) dl_load16(off, from, lds0 + (uint32_t)to);
+        else *reinterpret_cast<u32x4 *>(smem + to + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+    };
+    // `inside`: the caller knows that the pair lies within K
+    auto issue_a = [&](int T, int h, bool inside) {
+        const int to = a_half(T, h) + wave * 2048;
+        const unsigned char *from = ga + (int64_t)T * 128;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int q = (wave * 2 + i) * 8 + (lane >> 3);
+            if (RAGGED && !inside) load_or_zero(T * 128 + (((lane & 7) ^ ((q >> 1) & 7)) << 4) < p.K, offa[h][i], from, to + i * 1024);
+            else dl_load16(offa[h][i], from, lds0 + (uint32_t)(to + i * 1024));
+        }
+    };
+    auto issue_b = [&](int T, bool inside) {
+        const int to = b_slot(T) + wave * 4096;
+        const unsigned char *from = gb + (int64_t)T * stepb;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = BKC ? dl_chunk_k_pair_f8(wave * 4 + i, lane) : dl_chunk_k_mn_f8(wave * 4 + i, lane);
+            if (RAGGED && !inside) load_or_zero(T * 128 + at < p.K, offb[i], from, to + i * 1024);
+            else dl_load16(offb[i], from, lds0 + (uint32_t)(to + i * 1024));
+        }
+    };
+    auto issue_scales = [&](int T, bool now) {       // of pairs T .. T + 3, T a multiple of four
+        const int w = T + (wave & 3);
+        dl_load4_if(__builtin_amdgcn_readfirstlane(now ? -1 : 0), offs, gs + (w < P ? w : P - 1) * steps, lds0 + (uint32_t)(scale_slot(w) + (scales_b ? 256 : 0)));
+    };
+
+    // Fragment addresses: loop-invariant lane parts, the slot's scalar offset added in a compute phase (as in gemm_item_dl_f8).
+    constexpr int NXB = 2;
+    auto pin = [](uint32_t &x) { asm volatile("" : "+v"(x)); };
+    uint32_t la[2], lb[NXB];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int r = wm * 64 + (lane & 31), sw = (r >> 1) & 7;
+        la[c] = (uint32_t)(r * 128 + (((2 * (lane >> 5) + c) ^ sw) << 4));
+        pin(la[c]);
+        if (BKC) {
+            const int rb = wn * 64 + (lane & 31), sb = (rb >> 1) & 7;
+            lb[c] = (uint32_t)(rb * 128 + (((2 * (lane >> 5) + c) ^ sb) << 4));
+        } else {
+            const int i = lane & 15, g = lane >> 4, chunk = ((wn * 64 + c * 32) >> 4) + (g & 1), k0 = 32 * (g >> 1) + (i >> 1);
+            lb[c] = (uint32_t)(k0 * 256 + ((chunk ^ (2 * (k0 & 7))) << 4) + ((i & 1) << 3));
+        }
+        pin(lb[c]);
+    }
+    auto prep_a = [&](uint32_t(&x)[2], int T, int step, int h) {
+        uint32_t so = (uint32_t)a_half(T, h);
+        asm volatile("" : "+s"(so));
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            x[c] = (la[c] ^ (uint32_t)(step * 64)) + so;
+            pin(x[c]);
+        }
+    };
+    auto prep_b = [&](uint32_t(&x)[NXB], int T, int step) {
+        uint32_t so = (uint32_t)(b_slot(T) + (BKC ? 0 : step * 64 * 256));
+        asm volatile("" : "+s"(so));
+#pragma unroll
+        for (int c = 0; c < NXB; ++c) {
+            x[c] = (BKC ? lb[c] ^ (uint32_t)(step * 64) : lb[c]) + so;
+            pin(x[c]);
+        }
+    };
+    auto two_chunks = [&](uint32_t lo, uint32_t hi) -> i32x8 {
+        const u32x4 a = *reinterpret_cast<const u32x4 *>(smem + lo), b = *reinterpret_cast<const u32x4 *>(smem + hi);
+        return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+    };
+    auto load_a = [&](i32x8(&f)[2], const uint32_t(&x)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) f[i] = two_chunks(x[0] + (uint32_t)(i * 32 * 128), x[1] + (uint32_t)(i * 32 * 128));
+    };
+    auto load_b = [&](i32x8(&f)[2], const uint32_t(&x)[NXB]) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (BKC) {
+                f[j] = two_chunks(x[0] + (uint32_t)(j * 32 * 128), x[1] + (uint32_t)(j * 32 * 128));
+            } else {
+                typedef int v2i __attribute__((ext_vector_type(2)));
+                typedef __attribute__((address_space(3))) v2i lds_v2i;
+                const unsigned char *a = smem + x[j];
+                const v2i r0 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i *)(a));
+                const v2i r1 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i *)(a + 8 * 256));
+                const v2i r2 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i *)(a + 16 * 256));
+                const v2i r3 = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i *)(a + 24 * 256));
+                f[j] = i32x8{r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
+            }
+        }
+    };
+    // The scales of a wave's four row blocks in one register and of its two column blocks in another: the instruction selects the byte.
+    struct Scales {
+        uint32_t a[4], b[2];
+    };
+    auto load_scales = [&](Scales &s, int T) {
+        const unsigned char *at = smem + scale_slot(T) + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s.a[i] = at[wm * 128 + i * 32];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) s.b[j] = at[256 + wn * 64 + j * 32];
+    };
+    int sa = 0, sb = 0, na = 0, nb = 0;
+    auto pack_scales = [&](const Scales &s) {
+        na = (int)(s.a[0] | s.a[1] << 8 | s.a[2] << 16 | s.a[3] << 24);
+        nb = (int)(s.b[0] | s.b[1] << 8);
+    };
+    auto mma = [&](const i32x8(&fa)[2], const i32x8(&fb)[2], auto half) {
+        constexpr int H = decltype(half)::value;
+        acc.a[2 * H][0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[0], fa[0], acc.a[2 * H][0], 0, 0, 0, sb, 2 * H, sa);
+        acc.a[2 * H][1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[1], fa[0], acc.a[2 * H][1], 0, 0, 1, sb, 2 * H, sa);
+        acc.a[2 * H + 1][0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[0], fa[1], acc.a[2 * H + 1][0], 0, 0, 0, sb, 2 * H + 1, sa);
+        acc.a[2 * H + 1][1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[1], fa[1], acc.a[2 * H + 1][1], 0, 0, 1, sb, 2 * H + 1, sa);
+    };
+    auto phase_barrier = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const std::integral_constant<int, 0> LOWER{};
+    const std::integral_constant<int, 1> UPPER{};
+    i32x8 fal[2], fah[2], fb0[2], fb1[2];
+    uint32_t xal[2], xah[2], xb[NXB];
+    Scales ns;
+    // One K-step, `odd` of pair T: steady: pair T + 2 exists, and lies within K.
+    auto step = [&](int T, auto odd, const i32x8(&fbc)[2], i32x8(&fbn)[2], bool last, bool steady) {
+        constexpr int O = decltype(odd)::value;
+        if (steady || T + 2 < P) issue_a(T + 2, O, steady);                       // memory phase 1
+        load_a(fah, xah);
+        if (O == 1 && !last) {
+            load_scales(ns, T + 1);
+            if (steady) wait_loads<4>();
+            else wait_loads<0>();
+        }
+        phase_barrier();
+        __builtin_amdgcn_s_setprio(1);                                           // compute phase 1
+        mma(fal, fbc, LOWER);
+        if (!last) {
+            prep_b(xb, T + O, 1 - O);
+            prep_a(xal, T + O, 1 - O, 0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (O == 1 && !last) pack_scales(ns);
+        phase_barrier();
+        if (!last) {                                                             // memory phase 2
+            if (O == 1 && (steady || T + 2 < P)) issue_b(T + 2, steady);
+            if (O == 1) issue_scales(T + 4, (T & 3) == 0 && T + 4 < P);
+            load_b(fbn, xb);
+            load_a(fal, xal);
+            if (O == 0) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the lower rows of T have been read
+        }
+        phase_barrier();
+        __builtin_amdgcn_s_setprio(1);                                           // compute phase 2
+        mma(fah, fbc, UPPER);
+        if (!last) prep_a(xah, T + O, 1 - O, 1);
+        __builtin_amdgcn_s_setprio(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (O == 1 && !last) {
+            sa = na;
+            sb = nb;
+        }
+        phase_barrier();
+    };
+    const std::integral_constant<int, 0> EVEN{};
+    const std::integral_constant<int, 1> ODD{};
+
+    issue_scales(0, true);
+    issue_a(0, 0, false);
+    issue_a(0, 1, false);
+    issue_b(0, false);
+    if (P > 1) {
+        issue_a(1, 0, false);
+        issue_a(1, 1, false);
+        issue_b(1, false);
+    }
+    if (P > 1 && (!RAGGED || 256 <= p.K)) wait_loads<8>();
+    else wait_loads<0>();
+    __syncthreads();
+    prep_a(xal, 0, 0, 0);
+    prep_b(xb, 0, 0);
+    prep_a(xah, 0, 0, 1);
+    load_a(fal, xal);
+    load_b(fb0, xb);
+    load_scales(ns, 0);
+    pack_scales(ns);
+    sa = na;
+    sb = nb;
+    if (wave >= 4) phase_barrier();                     // the second wave of every SIMD runs one phase behind
+    int T = 0;
+    for (; T + 2 < P && (!RAGGED || (T + 3) * 128 <= p.K); ++T) {
+        step(T, EVEN, fb0, fb1, false, true);
+        step(T, ODD, fb1, fb0, false, true);
+    }
+    for (; T + 1 < P; ++T) {                            // the ring runs dry, or the last pair reaches past K
+        step(T, EVEN, fb0, fb1, false, false);
+        step(T, ODD, fb1, fb0, false, false);
+    }
+    step(T, EVEN, fb0, fb1, false, false);
+    step(T, ODD, fb1, fb0, true, false);
+    if (wave < 4) phase_barrier();                      // every wave passes the same number of barriers
     __syncthreads();
 }
 
@@ -484,6 +759,22 @@ __global__ __launch_bounds__(C::NT) __attribute__((amdgpu_waves_per_eu(2, 2), am
         if (edge) run_epilogue<C, Acc32<C>, EPI, true, C::S * C::TILES>(acc, g, m0, n0, tn, smem, red, (int)threadIdx.x);
         else run_epilogue<C, Acc32<C>, EPI, false, C::S * C::TILES>(acc, g, m0, n0, tn, smem, red, (int)threadIdx.x);
     }
+}
+
+template <bool BKC, int EPI, bool Q8, bool RAGGED>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void gemm_scaled_large(const GemmParams g, const Q8Params q, const ScaledParams p)
+{
+    using C = ScaledLargeCfg;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS + C::RED];
+    int tm, tn;
+    tile_coords((int)blockIdx.x, p.tiles_m * p.tiles_n, p.tiles_m, p.tiles_n, tm, tn);
+    const int m0 = tm * 256, n0 = tn * 256;
+    Acc32<C> acc;
+    if (RAGGED && p.K == 0) acc_zero(acc);
+    else scaled_contract_large<C, BKC, RAGGED>(acc, p, m0, n0, smem);
+    float *red = reinterpret_cast<float *>(smem + C::LDS);
+    if constexpr (Q8) run_epilogue_q8<C, EPI, RAGGED>(acc, g, q, m0, n0, tn, smem, red, (int)threadIdx.x);
+    else run_epilogue<C, Acc32<C>, EPI, RAGGED, C::EPI_RING>(acc, g, m0, n0, tn, smem, red, (int)threadIdx.x);
 }
 
 template <class C, bool BKC>

@@ -1,31 +1,9 @@
-// gemm_scaled_inst.hip -- instantiations and host launchers of gemm_scaled.hpp.
+// gemm_scaled_inst.hip -- host launcher of gemm_scaled.hpp and its divided contractions; tiles with their programs: gemm_scaled_tile_*.hip.
 #include "gemm_scaled.hpp"
 #include "scaled_launch.hpp"
 #include "small_launch.hpp"
 
 namespace coda {
-
-template <class C, bool BKC, int EPI, bool Q8>
-static hipError_t launch_tile(const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s)
-{
-    hipLaunchKernelGGL((gemm_scaled_tile<C, BKC, EPI, Q8>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(C::NT), 0, s, g, q, p);
-    return hipGetLastError();
-}
-template <class C, bool BKC>
-static hipError_t launch_program(int mode, bool q8, const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s)
-{
-    if (q8) {
-        if (mode == Q8_LINEAR) return launch_tile<C, BKC, Q8_LINEAR, true>(g, q, p, s);
-        if (mode == Q8_SWIGLU_FWD) return launch_tile<C, BKC, Q8_SWIGLU_FWD, true>(g, q, p, s);
-        return launch_tile<C, BKC, Q8_SWIGLU_BWD, true>(g, q, p, s);
-    }
-    if (mode == EPI_LINEAR) return launch_tile<C, BKC, EPI_LINEAR, false>(g, q, p, s);
-    if (mode == EPI_SWIGLU_FWD) return launch_tile<C, BKC, EPI_SWIGLU_FWD, false>(g, q, p, s);
-    if (mode == EPI_SWIGLU_BWD) return launch_tile<C, BKC, EPI_SWIGLU_BWD, false>(g, q, p, s);
-    if constexpr (C::BM == 256)                      // column partials are per 256 rows
-        if (mode == EPI_RMSNORM_BWD) return launch_tile<C, BKC, EPI_RMSNORM_BWD, false>(g, q, p, s);
-    return hipErrorInvalidConfiguration;
-}
 
 template <class C>
 static hipError_t launch_partial(bool bkc, const ScaledParams &p, hipStream_t s)
@@ -52,10 +30,8 @@ hipError_t launch_gemm_scaled(const ScaledPlan &pl, int mode, bool q8, bool bkc,
     p.tiles_n = (p.N + pl.bn - 1) / pl.bn;
     p.nsplit = pl.nsplit;
     if (pl.nsplit == 0) {
-        using C256 = ScaledCfg<256, 256, 2, 4, 2>;
-        using C128 = ScaledCfg<128, 256, 2, 4, 3>;
-        if (pl.bm == 256) return bkc ? launch_program<C256, true>(mode, q8, g, q, p, s) : launch_program<C256, false>(mode, q8, g, q, p, s);
-        return bkc ? launch_program<C128, true>(mode, q8, g, q, p, s) : launch_program<C128, false>(mode, q8, g, q, p, s);
+        if (pl.bm == 256) return bkc ? launch_scaled_256<true>(mode, q8, g, q, p, s) : launch_scaled_256<false>(mode, q8, g, q, p, s);
+        return bkc ? launch_scaled_128<true>(mode, q8, g, q, p, s) : launch_scaled_128<false>(mode, q8, g, q, p, s);
     }
     const hipError_t e = pl.bm == 32   ? launch_partial<ScaledCfg<32, 128, 1, 4, 3>>(bkc, p, s)
                          : pl.bm == 64 ? launch_partial<ScaledCfg<64, 128, 1, 4, 3>>(bkc, p, s)

@@ -54,6 +54,16 @@ inline size_t scaled_bytes(const ScaledPlan &pl, int64_t M, int64_t N) { return 
 hipError_t launch_gemm_scaled(const ScaledPlan &pl, int mode, bool q8, bool bkc, const GemmParams &g, const Q8Params &q, const ScaledParams &p,
                               hipStream_t s);
 
+// a tile and its program in one kernel, per layout of B (true: [N x K])
+template <bool BKC>
+hipError_t launch_scaled_256(int mode, bool q8, const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s);
+template <bool BKC>
+hipError_t launch_scaled_128(int mode, bool q8, const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s);
+template <> hipError_t launch_scaled_256<true>(int, bool, const GemmParams &, const Q8Params &, const ScaledParams &, hipStream_t);
+template <> hipError_t launch_scaled_256<false>(int, bool, const GemmParams &, const Q8Params &, const ScaledParams &, hipStream_t);
+template <> hipError_t launch_scaled_128<true>(int, bool, const GemmParams &, const Q8Params &, const ScaledParams &, hipStream_t);
+template <> hipError_t launch_scaled_128<false>(int, bool, const GemmParams &, const Q8Params &, const ScaledParams &, hipStream_t);
+
 // Ranges of the tokens of a gradient, so that its 256 x 256 tiles fill the chip; 1: G is added to by the tiles' own kernel
 inline int plan_grad(int64_t M, int64_t N, int64_t K, bool workspace)
 {
