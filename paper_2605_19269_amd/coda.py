@@ -120,7 +120,8 @@ _blib.coda_calib_mfma_loop16.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp]
 # The calls of every layer: the C functions take their place, and hand unusual arguments on to them.
 from . import _binding  # noqa: E402  (links libcoda.so)
 
-_NATIVE = ("coda_gemm", "coda_row_finalize", "coda_row_sumsq", "coda_col_finalize", "coda_lse_finalize")
+_NATIVE = ("coda_gemm", "coda_row_finalize", "coda_row_sumsq", "coda_col_finalize", "coda_lse_finalize", "coda_quantize", "coda_dequantize",
+           "coda_gemm_scaled", "coda_grad_scaled")
 _binding.ctypes_calls(*(getattr(_lib, _n) for _n in _NATIVE))
 for _n in _NATIVE:
     setattr(_lib, _n, getattr(_binding, _n))
@@ -228,16 +229,13 @@ def store(out, f32=False):
 
 
 def _q8(t, scales, what):
-    """Codes and scales are 2-D tensors of bytes; the pitch of the scales."""
-    assert t.dim() == 2 and t.element_size() == 1 and (t.shape[1] <= 1 or t.stride(1) == 1), "%s: a row-major 2-D tensor of codes expected" % what
-    return _scales(scales, (t.shape[1] + 127) // 128, t.shape[0], what)
+    """The pitch of the scales of a 2-D tensor of codes; both are tensors of bytes."""
+    return _binding.q8_pitch(t, scales, 0, 0, what)
 
 
 def _scales(scales, blocks, rows, what):
-    """The pitch of scale bytes [blocks x rows].  A tensor of one block may be a row of any pitch."""
-    assert scales.dim() == 2 and scales.element_size() == 1 and (scales.shape[1] <= 1 or scales.stride(1) == 1), "%s: a row-major 2-D tensor of scale bytes expected" % what
-    assert scales.shape[0] >= blocks and scales.shape[1] >= rows, "%s: scales of %d blocks x %d rows expected" % (what, blocks, rows)
-    return scales.stride(0) if scales.shape[0] > 1 else max(scales.stride(0), scales.shape[1])
+    """The pitch of scale bytes [blocks x rows]."""
+    return _binding.q8_pitch(None, scales, blocks, rows, what)
 
 
 def store_q8(out, scales):
@@ -359,31 +357,34 @@ def _at(workspace):
 
 def coda_quantize(X, codes, scales, scales_t=None, square=False, stream=None):
     """X: bf16 [R x C]; codes: [R x C]; scales: bytes [ceil(C / 128) x R]; with square blocks optionally scales_t: [ceil(R / 128) x C]."""
-    m = mat(X)
+    _torch or _import_torch()
+    m = _binding.mat(X, False, _DTYPES)
     assert codes.shape == X.shape, "codes of X's shape expected"
     pitch = _q8(codes, scales, "coda_quantize")
     pitch_t = 0 if scales_t is None else _scales(scales_t, (X.shape[0] + 127) // 128, X.shape[1], "coda_quantize")
-    _check(_lib.coda_quantize(_stream(stream), ctypes.byref(m), 1 if square else 0, codes.data_ptr(), codes.stride(0), scales.data_ptr(), pitch,
-                              _ptr(scales_t), pitch_t))
+    _check(_lib.coda_quantize(_stream(stream), m, 1 if square else 0, codes.data_ptr(), codes.stride(0), scales.data_ptr(), pitch, _ptr(scales_t), pitch_t))
 
 
 def coda_dequantize(codes, scales, out, stream=None):
     """codes, scales -> out: bf16 [R x C]."""
-    m = mat(codes)
-    assert out.dim() == 2 and out.shape == codes.shape and out.dtype == _torch.bfloat16, "a bf16 output of the codes' shape expected"
-    _check(_lib.coda_dequantize(_stream(stream), ctypes.byref(m), scales.data_ptr(), _q8(codes, scales, "coda_dequantize"), out.data_ptr(), out.stride(0)))
+    torch = _torch or _import_torch()
+    m = _binding.mat(codes, False, _DTYPES)
+    assert out.shape == codes.shape and out.dtype == torch.bfloat16 and (out.shape[1] <= 1 or out.stride(1) == 1), "a bf16 output of the codes' shape expected"
+    _check(_lib.coda_dequantize(_stream(stream), m, scales.data_ptr(), _q8(codes, scales, "coda_dequantize"), out.data_ptr(), out.stride(0)))
 
 
 def coda_gemm_scaled(A, scales_a, B, scales_b, ops, transB=False, stream=None, workspace=None):
     """D = A op(B), then the epilogue ops.  A: codes [M x K], scales_a: bytes [ceil(K / 128) x M]; B: codes [K x N], or [N x K] with transB,
     scales_b: bytes [ceil(K / 128) x N].  workspace: optional, coda_gemm_scaled_workspace_bytes(M, N, K) bytes."""
-    a, b = mat(A), mat(B, transB)
-    (M, K), N = A.shape, B.shape[0] if transB else B.shape[1]
+    _torch or _import_torch()
+    M, N, K, a, b = _binding.gemm_mats(A, B, False, transB, _DTYPES)
     blocks = (K + 127) // 128
-    ops = list(ops)
-    arr, n = _prog(ops)
-    _check(_lib.coda_gemm_scaled(_stream(stream), M, N, K, ctypes.byref(a), scales_a.data_ptr(), _scales(scales_a, blocks, M, "scales_a"), ctypes.byref(b),
-                                 scales_b.data_ptr(), _scales(scales_b, blocks, N, "scales_b"), arr, n, *_at(workspace)))
+    ops = list(ops)      # as in coda_gemm
+    arr = _binding.prog(ops, coda_epi_op)
+    if arr is None:
+        arr = _prog(ops)[0]
+    _check(_lib.coda_gemm_scaled(_stream(stream), M, N, K, a, scales_a.data_ptr(), _scales(scales_a, blocks, M, "scales_a"), b, scales_b.data_ptr(),
+                                 _scales(scales_b, blocks, N, "scales_b"), arr, len(ops), *_at(workspace)))
 
 
 def coda_gemm_scaled_workspace_bytes(M, N, K):
@@ -393,12 +394,12 @@ def coda_gemm_scaled_workspace_bytes(M, N, K):
 def coda_grad_scaled(A, scales_a, B, scales_b, G, stream=None, workspace=None):
     """G [M x N] f32 += A^T B over the K rows of both.  A: codes [K x M], scales_a: bytes [ceil(M / 128) x K]; B: codes [K x N] with scales_b, or
     bf16 [K x N] with scales_b None.  workspace: optional, coda_grad_scaled_workspace_bytes(M, N, K) bytes."""
-    a, b = mat(A, True), mat(B)
-    (K, M), N = A.shape, B.shape[1]
-    assert G.dim() == 2 and G.shape == (M, N) and G.dtype == _torch.float32 and (N <= 1 or G.stride(1) == 1), "a row-major f32 [M x N] gradient expected"
+    torch = _torch or _import_torch()
+    M, N, K, a, b = _binding.gemm_mats(A, B, True, False, _DTYPES)
+    assert G.shape == (M, N) and G.dtype == torch.float32 and (N <= 1 or G.stride(1) == 1), "a row-major f32 [M x N] gradient expected"
     pitch_b = 0 if scales_b is None else _scales(scales_b, (N + 127) // 128, K, "scales_b")
-    _check(_lib.coda_grad_scaled(_stream(stream), M, N, K, ctypes.byref(a), scales_a.data_ptr(), _scales(scales_a, (M + 127) // 128, K, "scales_a"),
-                                 ctypes.byref(b), _ptr(scales_b), pitch_b, G.data_ptr(), G.stride(0), *_at(workspace)))
+    _check(_lib.coda_grad_scaled(_stream(stream), M, N, K, a, scales_a.data_ptr(), _scales(scales_a, (M + 127) // 128, K, "scales_a"), b, _ptr(scales_b),
+                                 pitch_b, G.data_ptr(), G.stride(0), *_at(workspace)))
 
 
 def coda_grad_scaled_workspace_bytes(M, N, K):

@@ -12,7 +12,7 @@
 
 namespace {
 
-PyObject *s_data_ptr, *s_stride, *s_shape, *s_dtype, *s_keep;
+PyObject *s_data_ptr, *s_stride, *s_shape, *s_dtype, *s_keep, *s_element_size;
 static_assert(sizeof(coda_mat) == 40 && sizeof(coda_epi_op) == 96, "the layouts that coda.py mirrors");
 
 // t.data_ptr() as a pointer
@@ -179,6 +179,54 @@ PyObject *prog(PyObject *, PyObject *const *a, Py_ssize_t n)
     return out;
 }
 
+// Sizes and row pitch of a row-major 2-D tensor of bytes; false (without an exception) if it is none
+bool bytes_2d(PyObject *t, int64_t *rows, int64_t *cols, int64_t *pitch)
+{
+    PyObject *size = PyObject_CallMethodNoArgs(t, s_element_size), *shape = size ? PyObject_GetAttr(t, s_shape) : nullptr;
+    PyObject *stride = shape ? PyObject_CallMethodNoArgs(t, s_stride) : nullptr;
+    bool ok = stride != nullptr;
+    int64_t step = 1;
+    if (ok) {
+        const long one = PyLong_AsLong(size);
+        ok = !(one == -1 && PyErr_Occurred());
+        if (ok && (one != 1 || PySequence_Size(shape) != 2)) {
+            PyErr_Clear();
+            ok = false;
+        }
+        ok = ok && item(shape, 0, rows) && item(shape, 1, cols) && item(stride, 0, pitch) && item(stride, 1, &step) && (*cols <= 1 || step == 1);
+    }
+    Py_XDECREF(size);
+    Py_XDECREF(shape);
+    Py_XDECREF(stride);
+    return ok;
+}
+// q8_pitch(codes, scales, blocks, rows, what) -> the pitch of scale bytes [blocks x rows]; with codes, a 2-D tensor of bytes, blocks and rows are
+// those of its columns and rows
+PyObject *q8_pitch(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "q8_pitch takes 5 arguments");
+    int64_t blocks = 0, rows = 0, cols = 0, pitch = 0, have_blocks = 0, have_rows = 0;
+    if (a[0] != Py_None) {
+        if (!bytes_2d(a[0], &rows, &cols, &pitch)) {
+            if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "%U: a row-major 2-D tensor of codes expected", a[4]);
+            return nullptr;
+        }
+        blocks = (cols + 127) / 128;
+    } else {
+        blocks = PyLong_AsLongLong(a[2]);
+        rows = PyLong_AsLongLong(a[3]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    if (!bytes_2d(a[1], &have_blocks, &have_rows, &pitch)) {
+        if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "%U: a row-major 2-D tensor of scale bytes expected", a[4]);
+        return nullptr;
+    }
+    if (have_blocks < blocks || have_rows < rows)
+        return PyErr_Format(PyExc_AssertionError, "%U: scales of %lld blocks x %lld rows expected", a[4], (long long)blocks, (long long)rows);
+    if (have_blocks <= 1 && pitch < have_rows) pitch = have_rows;                    // one row of any pitch
+    return PyLong_FromLongLong(pitch);
+}
+
 // ---- the calls.  Arguments are pointers (an address, None, the bytes of a structure) and numbers; anything else takes the ctypes function.
 struct Args {
     PyObject *const *a;
@@ -212,8 +260,8 @@ struct Args {
     }
 };
 
-enum Call { GEMM, ROW_FINALIZE, ROW_SUMSQ, COL_FINALIZE, LSE_FINALIZE, CALLS };
-constexpr int ARITY[CALLS] = {10, 8, 3, 5, 8};
+enum Call { GEMM, ROW_FINALIZE, ROW_SUMSQ, COL_FINALIZE, LSE_FINALIZE, QUANTIZE, DEQUANTIZE, GEMM_SCALED, GRAD_SCALED, CALLS };
+constexpr int ARITY[CALLS] = {10, 8, 3, 5, 8, 9, 6, 14, 14};
 PyObject *g_ctypes[CALLS];           // set once, when coda.py is imported
 
 template <int CALL>
@@ -252,6 +300,30 @@ PyObject *call(PyObject *, PyObject *const *a, Py_ssize_t n)
             const int64_t N = x.num(2), nblk = x.num(3);
             float *out = x.ptr<float>(4);
             CODA_RUN(coda_col_finalize(stream, parts, N, nblk, out))
+        } else if constexpr (CALL == QUANTIZE) {
+            const coda_mat *X = x.ptr<const coda_mat>(1);
+            const int64_t square = x.num(2), ldc = x.num(4), lds = x.num(6), ldt = x.num(8);
+            void *codes = x.ptr<void>(3), *s = x.ptr<void>(5), *st2 = x.ptr<void>(7);
+            CODA_RUN(coda_quantize(stream, X, square != 0, codes, ldc, s, lds, st2, ldt))
+        } else if constexpr (CALL == DEQUANTIZE) {
+            const coda_mat *Q = x.ptr<const coda_mat>(1);
+            const void *s = x.ptr<const void>(2);
+            const int64_t lds = x.num(3), ldo = x.num(5);
+            void *out = x.ptr<void>(4);
+            CODA_RUN(coda_dequantize(stream, Q, s, lds, out, ldo))
+        } else if constexpr (CALL == GEMM_SCALED || CALL == GRAD_SCALED) {
+            const int64_t M = x.num(1), N = x.num(2), K = x.num(3), lda = x.num(6), ldb = x.num(9), n8 = x.num(11), bytes = x.num(13);
+            const coda_mat *A = x.ptr<const coda_mat>(4), *B = x.ptr<const coda_mat>(7);
+            const void *sa = x.ptr<const void>(5), *sb = x.ptr<const void>(8);
+            void *ws = x.ptr<void>(12);
+            if (bytes < 0 || (CALL == GEMM_SCALED && (n8 < 0 || n8 > INT32_MAX))) x.usual = false;
+            if constexpr (CALL == GEMM_SCALED) {
+                const coda_epi_op *p = x.ptr<const coda_epi_op>(10);
+                CODA_RUN(coda_gemm_scaled(stream, M, N, K, A, sa, lda, B, sb, ldb, p, (int32_t)n8, ws, (size_t)bytes))
+            } else {
+                float *G = x.ptr<float>(10);
+                CODA_RUN(coda_grad_scaled(stream, M, N, K, A, sa, lda, B, sb, ldb, G, n8, ws, (size_t)bytes))
+            }
         } else {
             const float *pmax = x.ptr<const float>(1), *psum = x.ptr<const float>(2), *ztgt = x.ptr<const float>(5);
             const int64_t M = x.num(3), nblk = x.num(4);
@@ -265,7 +337,7 @@ PyObject *call(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyObject_Vectorcall(g_ctypes[CALL], a, (size_t)n, nullptr);
 }
 
-// ctypes_calls(gemm, row_finalize, row_sumsq, col_finalize, lse_finalize)
+// ctypes_calls(gemm, row_finalize, row_sumsq, col_finalize, lse_finalize, quantize, dequantize, gemm_scaled, grad_scaled)
 PyObject *ctypes_calls(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (n != CALLS) return PyErr_Format(PyExc_TypeError, "one function for every call");
@@ -287,6 +359,11 @@ PyMethodDef methods[] = {CODA_FAST("op", op),
                          CODA_FAST("coda_row_sumsq", call<ROW_SUMSQ>),
                          CODA_FAST("coda_col_finalize", call<COL_FINALIZE>),
                          CODA_FAST("coda_lse_finalize", call<LSE_FINALIZE>),
+                         CODA_FAST("q8_pitch", q8_pitch),
+                         CODA_FAST("coda_quantize", call<QUANTIZE>),
+                         CODA_FAST("coda_dequantize", call<DEQUANTIZE>),
+                         CODA_FAST("coda_gemm_scaled", call<GEMM_SCALED>),
+                         CODA_FAST("coda_grad_scaled", call<GRAD_SCALED>),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -299,6 +376,7 @@ PyMODINIT_FUNC PyInit__binding(void)
     s_shape = PyUnicode_InternFromString("shape");
     s_dtype = PyUnicode_InternFromString("dtype");
     s_keep = PyUnicode_InternFromString("_keep");
-    if (!s_data_ptr || !s_stride || !s_shape || !s_dtype || !s_keep) return nullptr;
+    s_element_size = PyUnicode_InternFromString("element_size");
+    if (!s_data_ptr || !s_stride || !s_shape || !s_dtype || !s_keep || !s_element_size) return nullptr;
     return PyModule_Create(&module);
 }

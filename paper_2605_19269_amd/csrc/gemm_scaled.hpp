@@ -17,6 +17,22 @@
 
 namespace coda {
 
+// 4 bytes a lane, straight to LDS
+__device__ __forceinline__ void dl_load4(uint32_t voff, const void *sbase, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(voff), "s"(sbase), "s"(lds_addr) : "memory", "m0");
+}
+// The same by all lanes or, where `mask` is 0 (else -1), none.  Without a branch: the compiler sinks MFMAs from in front of one into the
+// block behind it, and with them a compute phase into the memory phase.
+__device__ __forceinline__ void dl_load4_if(int mask, uint32_t voff, const void *sbase, uint32_t lds_addr)
+{
+    uint64_t keep;
+    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b32 exec_lo, %1\n\ts_mov_b32 exec_hi, %1\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b64 exec, %0"
+                 : "=&s"(keep)
+                 : "s"(mask), "v"(voff), "s"(sbase), "s"(lds_addr)
+                 : "memory", "m0");
+}
+
 template <int BM_, int BN_, int WGM_, int WGN_, int S_>
 struct ScaledCfg : SmallCfg<BM_, BN_, WGM_, WGN_, S_, true> {
     using Base = SmallCfg<BM_, BN_, WGM_, WGN_, S_, true>;
@@ -220,17 +236,6 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
 // 16384 x 4096 x 28672, B [K x N]: 1394 us, 2.76 PFLOP/s (unscaled 8-bit operands 1304).  Four waves of 256 x 64 with two whole slots: 1750 (their loads are in flight for half to one
 // stage, which is less than what memory takes, and one wave on a SIMD has no other to compute while it issues them).
 // ---------------------------------------------------------------------------------
-// 4 bytes a lane, straight to LDS; by all lanes or, where `mask` is 0 (else -1), none.  Without a branch: the compiler sinks MFMAs from in front of one into the
-// block behind it, and with them a compute phase into the memory phase.
-__device__ __forceinline__ void dl_load4_if(int mask, uint32_t voff, const void *sbase, uint32_t lds_addr)
-{
-    uint64_t keep;
-    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b32 exec_lo, %1\n\ts_mov_b32 exec_hi, %1\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dword %2, %3\n\ts_mov_b64 exec, %0"
-                 : "=&s"(keep)
-                 : "s"(mask), "v"(voff), "s"(sbase), "s"(lds_addr)
-                 : "memory", "m0");
-}
-
 struct ScaledLargeCfg : DlCfg<256, 256, 2, 4, 4> {
     static constexpr int HALF = 128 * 128, A_REGION = 5 * HALF, PAIR_B = 256 * 128, B_REGION = 2 * PAIR_B, TILES = A_REGION + B_REGION;
     static constexpr int SCALES = 512, LDS = TILES + 8 * SCALES, RED = 2 * WGN * BM * 4, EPI_RING = 128 * 1024;
@@ -386,6 +391,11 @@ __device__ __forceinline__ void scaled_contract_large(Acc32<C> &acc, const Scale
         acc.a[2 * H + 1][0] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[0], fa[1], acc.a[2 * H + 1][0], 0, 0, 0, sb, 2 * H + 1, sa);
         acc.a[2 * H + 1][1] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[1], fa[1], acc.a[2 * H + 1][1], 0, 0, 1, sb, 2 * H + 1, sa);
     };
+    // MFMAs stay in their phase: sunk over a branch, to where their result is used, they keep the fragments alive
+    auto pin_sums = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) asm volatile("" : "+v"(acc.a[2 * h + i][0]), "+v"(acc.a[2 * h + i][1]));
+    };
     auto phase_barrier = [&]() {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
@@ -411,6 +421,7 @@ __device__ __forceinline__ void scaled_contract_large(Acc32<C> &acc, const Scale
         phase_barrier();
         __builtin_amdgcn_s_setprio(1);                                           // compute phase 1
         mma(fal, fbc, LOWER);
+        if (!steady) pin_sums(0);
         if (!last) {
             prep_b(xb, T + O, 1 - O);
             prep_a(xal, T + O, 1 - O, 0);
@@ -429,6 +440,7 @@ __device__ __forceinline__ void scaled_contract_large(Acc32<C> &acc, const Scale
         phase_barrier();
         __builtin_amdgcn_s_setprio(1);                                           // compute phase 2
         mma(fah, fbc, UPPER);
+        if (!steady) pin_sums(1);
         if (!last) prep_a(xah, T + O, 1 - O, 1);
         __builtin_amdgcn_s_setprio(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -509,78 +521,99 @@ __device__ __forceinline__ void run_epilogue_q8(Acc32<C> &acc, const GemmParams 
                                                 float *red, int tid)
 {
     constexpr int BM = C::BM, NB = C::WTM / 32, NU = C::WTN / 8;
-    static_assert(C::BN == 256 && C::WTN == 64 && C::WGN == 4 && BM * 512 <= C::LDS, "tile");
-    const int lane = tid & 63, wave = tid >> 6, lrow = lane & 31, half = lane >> 5;
+    static_assert(C::BN == 256 && C::WTN == 64 && C::WGN == 4 && BM * 512 + 1024 <= C::LDS, "tile");
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lrow = lane & 31, half = lane >> 5;
     const int wm = wave % C::WGM, wn = wave / C::WGM, rw = wm * C::WTM, nw = n0 + wn * 64;
     const int rows_ok = EDGE ? clampi(p.M - m0, 0, BM) : BM, cols_ok = EDGE ? clampi(p.N - n0, 0, 256) : 256;
     auto there = [&](int u) { return !EDGE || nw + u * 8 + half * 4 < p.N; };
     auto either_half = [&](float m) { return fmaxf(m, __shfl_xor(m, 32, 64)); };
 
     if constexpr (MODE == Q8_SWIGLU_BWD) {
-        constexpr int NCH = 32, STEPS = BM * NCH / C::NT, BATCH = 8;
-        static_assert(STEPS % BATCH == 0, "whole batches");
-        const uint8_t *z = q.z + (int64_t)m0 * q.ldz + 2 * n0;
+        // A wave's 64 columns are one block of the doubled width, so it works by itself.  Its rows of Z, 128 bytes each, go straight to
+        // a region of its own, in the layout of Stage (a chunk's place is its lane's, so the swizzle is in what the lane fetches), 32
+        // rows are computed while the next are on their way, and the codes of dZ take the place of Z's.  No register holds Z ahead of
+        // time: 128 accumulators and the 64 values of a lane's row leave none (fetched to registers: 120 spilled; 8192 x 8192 x 2048 290 us, so 167).
+        constexpr int RB = 128, P = 32;
+        using St = Stage<RB>;
+        unsigned char *reg = ring + wave * (C::WTM * RB), *zs = ring + BM * 512 + wave * 128;
+        const bool want_stat = p.rowred_mode != ROWRED_NONE;
+        const int wave_rows = EDGE ? clampi(rows_ok - rw, 0, C::WTM) : C::WTM, wave_bytes = EDGE ? clampi(2 * (p.N - nw), 0, RB) : RB;
+        const int64_t kb = n0 / 64 + wn;
+        if (!EDGE || (wave_rows > 0 && wave_bytes > 0)) {
+            const int last = (wave_rows - 1) & ~3;
+            if (lane < 32) dl_load4(lane * 4 < last ? lane * 4 : last, q.z_s + kb * q.ld_z_s + m0 + rw, (uint32_t)(uintptr_t)zs);
+            const uint8_t *z = q.z + (int64_t)(m0 + rw) * q.ldz + 2 * nw;
 #pragma unroll
-        for (int b = 0; b < STEPS; b += BATCH) {
-            u32x4 t[BATCH];
-#pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                const int idx = (b + k) * C::NT + tid, r = idx / NCH, c = idx % NCH;
-                t[k] = u32x4{0u, 0u, 0u, 0u};
-                if (!EDGE || (r < rows_ok && c * 8 < cols_ok)) t[k] = *reinterpret_cast<const u32x4 *>(z + r * q.ldz + c * 16);
+            for (int it = 0; it < C::WTM / St::RPI; ++it) {
+                const int r = it * St::RPI + (lane >> 3), c = ((lane & 7) ^ ((r >> 1) & 7)) << 4;
+                const int rr = EDGE && r >= wave_rows ? wave_rows - 1 : r, cc = EDGE && c >= wave_bytes ? wave_bytes - 16 : c;
+                dl_load16((uint32_t)((int64_t)rr * q.ldz + cc), z, (uint32_t)(uintptr_t)reg + (uint32_t)(it * 1024));
             }
+            auto block = [&](auto ic) {
+                constexpr int i = decltype(ic)::value;
+                wait_loads<(NB - 1 - i) * (P / St::RPI)>();
+                const int r = rw + i * 32 + lrow;
+                const float s = q8_scale(zs[i * 32 + lrow]);
+                uint32_t ulane = St::template unit_lane<8, 32>(lane);
+                asm volatile("" : "+v"(ulane));
+                float dz[NU][8], stat = 0.0f;
 #pragma unroll
-            for (int k = 0; k < BATCH; ++k) {
-                const int idx = (b + k) * C::NT + tid, r = idx / NCH, c = idx % NCH;
-                *reinterpret_cast<u32x4 *>(ring + q8_spot<512>(r, c * 16)) = t[k];
-            }
-        }
-        const int64_t kb = n0 / 64 + wn;             // the wave's block of 128 of the doubled width
-        uint32_t zb[NB];
+                for (int u = 0; u < NU; ++u) {
+                    const u32x2 w = *reinterpret_cast<const u32x2 *>(reg + St::template unit_addr<32>(ulane, i, u * 16));
+                    const f32x4 d = acc.get(i, u);
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const int r = rw + i * 32 + lrow;
-            zb[i] = !EDGE || (r < rows_ok && nw < p.N) ? q.z_s[kb * q.ld_z_s + m0 + r] : 127u;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const int r = rw + i * 32 + lrow;
-            const float s = q8_scale(zb[i]);
-            float dz[NU][8], largest = 0.0f, stat = 0.0f;
-#pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                const u32x2 w = *reinterpret_cast<const u32x2 *>(ring + q8_spot<512>(r, wn * 128 + u * 16 + half * 8));
-                const f32x4 d = acc.get(i, u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x2 gu = e & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e >> 1], false);
-                    const float g = gu[0] * s, up = gu[1] * s, sg = fast_sigmoid(g), sl = g * sg;
-                    const float dU = d[e] * sl, dG = d[e] * up * (sg + sl * (1.0f - sg));
-                    dz[u][2 * e] = dG;
-                    dz[u][2 * e + 1] = dU;
-                    if (there(u)) {
-                        largest = fmaxf(largest, fmaxf(q8_magnitude(dG), q8_magnitude(dU)));
-                        stat += g * dG + up * dU;
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x2 gu = e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[e >> 1], s, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[e >> 1], s, false);
+                        const float g = gu[0], up = gu[1], sg = fast_sigmoid(g), sl = g * sg;
+                        dz[u][2 * e] = d[e] * up * (sg + sl * (1.0f - sg));
+                        dz[u][2 * e + 1] = d[e] * sl;
+                        if (want_stat && there(u)) stat += g * dz[u][2 * e] + up * dz[u][2 * e + 1];
                     }
+                    if (u & 1) __builtin_amdgcn_sched_barrier(0);
                 }
-            }
-            const uint32_t byte = q8_scale_byte(either_half(largest));
-            const float inv = q8_inverse(byte);
+                const float largest = q8_largest([&](auto take) {
 #pragma unroll
-            for (int u = 0; u < NU; ++u)
-                *reinterpret_cast<u32x2 *>(ring + q8_spot<512>(r, wn * 128 + u * 16 + half * 8)) =
-                    u32x2{q8_codes(dz[u][0], dz[u][1], dz[u][2], dz[u][3], inv), q8_codes(dz[u][4], dz[u][5], dz[u][6], dz[u][7], inv)};
-            if (half == 0 && (!EDGE || (r < rows_ok && nw < p.N))) q.out_s[kb * q.ld_out_s + m0 + r] = (uint8_t)byte;
-            if (p.rowred_mode != ROWRED_NONE) {
-                stat += __shfl_xor(stat, 32, 64);
-                if (half == 0) red[wn * BM + r] = stat;
+                    for (int u = 0; u < NU; ++u)
+                        if (there(u)) {
+                            take(dz[u][0], dz[u][1]);
+                            take(dz[u][2], dz[u][3]);
+                            take(dz[u][4], dz[u][5]);
+                            take(dz[u][6], dz[u][7]);
+                        }
+                });
+                const uint32_t byte = q8_scale_byte(either_half(largest));
+                const float scale = q8_scale(byte);
+                uint32_t ulane2 = St::template unit_lane<8, 32>(lane);
+                asm volatile("" : "+v"(ulane2));
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+                    *reinterpret_cast<u32x2 *>(reg + St::template unit_addr<32>(ulane2, i, u * 16)) =
+                        u32x2{q8_codes(dz[u][0], dz[u][1], dz[u][2], dz[u][3], scale), q8_codes(dz[u][4], dz[u][5], dz[u][6], dz[u][7], scale)};
+                zs[i * 32 + lrow] = (unsigned char)byte;
+                if (want_stat) {
+                    stat += __shfl_xor(stat, 32, 64);
+                    if (half == 0) red[wn * BM + r] = stat;
+                }
+                stage_fence();
+            };
+            block(std::integral_constant<int, 0>{});
+            block(std::integral_constant<int, 1>{});
+            if constexpr (NB > 2) {
+                block(std::integral_constant<int, 2>{});
+                block(std::integral_constant<int, 3>{});
             }
-            __builtin_amdgcn_sched_barrier(0);
+            static_assert(NB == 2 || NB == 4, "blocks");
+            // stores after the last wait for loads
+            stage_store<RB, C::WTM, EDGE, false>(reg, q.out + (int64_t)(m0 + rw) * q.ld_out + 2 * nw, q.ld_out, wave_rows, wave_bytes, lane);
+            uint8_t *to = q.out_s + kb * q.ld_out_s + m0 + rw;
+#pragma unroll
+            for (int r = lane; r < C::WTM; r += 64)
+                if (!EDGE || r < wave_rows) to[r] = zs[r];
+        } else if (want_stat) {
+            for (int r = lane; r < C::WTM; r += 64) red[wn * BM + rw + r] = 0.0f;
         }
-        __syncthreads();
-        q8_store_rows<C, 512, EDGE>(ring, q.out + (int64_t)m0 * q.ld_out + 2 * n0, q.ld_out, rows_ok, 2 * cols_ok, tid);
-        if (p.rowred_mode != ROWRED_NONE)
+        if (want_stat) {
+            __syncthreads();
             for (int r = tid; r < BM; r += C::NT) {
                 const int m = m0 + r;
                 if (EDGE && m >= p.M) continue;
@@ -588,6 +621,7 @@ __device__ __forceinline__ void run_epilogue_q8(Acc32<C> &acc, const GemmParams 
                 if (p.rowred_mode == ROWRED_PARTIALS) p.rowred[(int64_t)tn * p.M + m] = s;
                 else atomicAdd(p.rowred + m, s);
             }
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -600,13 +634,15 @@ __device__ __forceinline__ void run_epilogue_q8(Acc32<C> &acc, const GemmParams 
         auto put_values = [&](uint8_t *out, int64_t ld, uint8_t *scales, int64_t ld_s) {
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
-                float largest = 0.0f;
+                const float largest = either_half(q8_largest([&](auto take) {
 #pragma unroll
-                for (int u = 0; u < NU; ++u) {
-                    const f32x4 v = acc.get(i, u);
-                    if (there(u)) largest = fmaxf(fmaxf(fmaxf(largest, q8_magnitude(v[0])), fmaxf(q8_magnitude(v[1]), q8_magnitude(v[2]))), q8_magnitude(v[3]));
-                }
-                largest = either_half(largest);
+                    for (int u = 0; u < NU; ++u)
+                        if (there(u)) {
+                            const f32x4 v = acc.get(i, u);
+                            take(v[0], v[1]);
+                            take(v[2], v[3]);
+                        }
+                }));
                 if (half == 0) red[wn * BM + rw + i * 32 + lrow] = largest;
             }
             __syncthreads();
@@ -615,11 +651,11 @@ __device__ __forceinline__ void run_epilogue_q8(Acc32<C> &acc, const GemmParams 
             for (int i = 0; i < NB; ++i) {
                 const int r = rw + i * 32 + lrow;
                 const uint32_t byte = q8_scale_byte(fmaxf(red[(wn & 2) * BM + r], red[((wn & 2) + 1) * BM + r]));
-                const float inv = q8_inverse(byte);
+                const float scale = q8_scale(byte);
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
                     const f32x4 v = acc.get(i, u);
-                    *reinterpret_cast<uint32_t *>(ring + q8_spot<256>(r, wn * 64 + u * 8 + half * 4)) = q8_codes(v[0], v[1], v[2], v[3], inv);
+                    *reinterpret_cast<uint32_t *>(ring + q8_spot<256>(r, wn * 64 + u * 8 + half * 4)) = q8_codes(v[0], v[1], v[2], v[3], scale);
                 }
                 if ((wn & 1) == 0 && half == 0 && (!EDGE || (r < rows_ok && nw < p.N))) scales[kb * ld_s + m0 + r] = (uint8_t)byte;
             }
@@ -633,15 +669,16 @@ __device__ __forceinline__ void run_epilogue_q8(Acc32<C> &acc, const GemmParams 
             // silu(g) u takes the place of its pair; the row's 128 of them are the tile's
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
-                float largest = 0.0f;
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
                     const f32x4 v = acc.get(i, u);
-                    const float h0 = v[0] * fast_sigmoid(v[0]) * v[1], h1 = v[2] * fast_sigmoid(v[2]) * v[3];
-                    acc.set(i, u, f32x4{h0, h1, 0.0f, 0.0f});
-                    if (there(u)) largest = fmaxf(largest, fmaxf(q8_magnitude(h0), q8_magnitude(h1)));
+                    acc.set(i, u, f32x4{v[0] * fast_sigmoid(v[0]) * v[1], v[2] * fast_sigmoid(v[2]) * v[3], 0.0f, 0.0f});
                 }
-                largest = either_half(largest);
+                const float largest = either_half(q8_largest([&](auto take) {
+#pragma unroll
+                    for (int u = 0; u < NU; ++u)
+                        if (there(u)) take(acc.get(i, u)[0], acc.get(i, u)[1]);
+                }));
                 if (half == 0) red[wn * BM + rw + i * 32 + lrow] = largest;
             }
             __syncthreads();
@@ -649,12 +686,11 @@ __device__ __forceinline__ void run_epilogue_q8(Acc32<C> &acc, const GemmParams 
             for (int i = 0; i < NB; ++i) {
                 const int r = rw + i * 32 + lrow;
                 const uint32_t byte = q8_scale_byte(fmaxf(fmaxf(red[r], red[BM + r]), fmaxf(red[2 * BM + r], red[3 * BM + r])));
-                const float inv = q8_inverse(byte);
+                const float scale = q8_scale(byte);
 #pragma unroll
                 for (int u = 0; u < NU; ++u) {
                     const f32x4 v = acc.get(i, u);
-                    *reinterpret_cast<uint16_t *>(ring + q8_spot<128>(r, wn * 32 + u * 4 + half * 2)) =
-                        (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+                    *reinterpret_cast<uint16_t *>(ring + q8_spot<128>(r, wn * 32 + u * 4 + half * 2)) = q8_codes2(v[0], v[1], scale);
                 }
                 if (wn == 0 && half == 0 && (!EDGE || r < rows_ok)) q.out_s[(int64_t)tn * q.ld_out_s + m0 + r] = (uint8_t)byte;
             }
@@ -695,18 +731,17 @@ __global__ __launch_bounds__(256) void epi_rows_q8_kernel(const GemmParams p, co
         float dz[8], largest = 0.0f, stat = 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const f32x2 gu = e & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)zc[e >> 1], true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)zc[e >> 1], false);
-            const float g = gu[0] * s, up = gu[1] * s, sg = fast_sigmoid(g), sl = g * sg;
-            const float dU = v[e] * sl, dG = v[e] * up * (sg + sl * (1.0f - sg));
-            dz[2 * e] = dG;
-            dz[2 * e + 1] = dU;
-            largest = fmaxf(largest, fmaxf(q8_magnitude(dG), q8_magnitude(dU)));
-            stat += g * dG + up * dU;
+            const f32x2 gu = e & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(zc[e >> 1], s, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(zc[e >> 1], s, false);
+            const float g = gu[0], up = gu[1], sg = fast_sigmoid(g), sl = g * sg;
+            dz[2 * e] = v[e] * up * (sg + sl * (1.0f - sg));
+            dz[2 * e + 1] = v[e] * sl;
+            largest = fmaxf(largest, fmaxf(q8_magnitude(dz[2 * e]), q8_magnitude(dz[2 * e + 1])));
+            stat += g * dz[2 * e] + up * dz[2 * e + 1];
         }
         const uint32_t byte = q8_scale_byte(lanes_max<16>(ok ? largest : 0.0f));
         if (ok) {
-            const float inv = q8_inverse(byte);
-            *reinterpret_cast<u32x2 *>(q.out + (int64_t)m * q.ld_out + 2 * n) = u32x2{q8_codes(dz[0], dz[1], dz[2], dz[3], inv), q8_codes(dz[4], dz[5], dz[6], dz[7], inv)};
+            const float scale = q8_scale(byte);
+            *reinterpret_cast<u32x2 *>(q.out + (int64_t)m * q.ld_out + 2 * n) = u32x2{q8_codes(dz[0], dz[1], dz[2], dz[3], scale), q8_codes(dz[4], dz[5], dz[6], dz[7], scale)};
             if ((lane & 15) == 0) q.out_s[(int64_t)(n >> 6) * q.ld_out_s + m] = (uint8_t)byte;
         }
         if (p.rowred_mode != ROWRED_NONE) {
@@ -722,7 +757,7 @@ __global__ __launch_bounds__(256) void epi_rows_q8_kernel(const GemmParams p, co
             const float largest = fmaxf(fmaxf(q8_magnitude(v[0]), q8_magnitude(v[1])), fmaxf(q8_magnitude(v[2]), q8_magnitude(v[3])));
             const uint32_t byte = q8_scale_byte(lanes_max<32>(ok ? largest : 0.0f));
             if (!ok) return;
-            *reinterpret_cast<uint32_t *>(out + (int64_t)m * ld + n) = q8_codes(v[0], v[1], v[2], v[3], q8_inverse(byte));
+            *reinterpret_cast<uint32_t *>(out + (int64_t)m * ld + n) = q8_codes(v[0], v[1], v[2], v[3], q8_scale(byte));
             if ((lane & 31) == 0) scales[(int64_t)(n >> 7) * ld_s + m] = (uint8_t)byte;
         };
         if constexpr (MODE == Q8_LINEAR) {
@@ -731,8 +766,7 @@ __global__ __launch_bounds__(256) void epi_rows_q8_kernel(const GemmParams p, co
             if (q.z) put_values(q.z, q.ldz, q.z_s, q.ld_z_s);
             const float h0 = v[0] * fast_sigmoid(v[0]) * v[1], h1 = v[2] * fast_sigmoid(v[2]) * v[3];
             const uint32_t byte = q8_scale_byte(lanes_max<64>(ok ? fmaxf(q8_magnitude(h0), q8_magnitude(h1)) : 0.0f));
-            const float inv = q8_inverse(byte);
-            if (ok) *reinterpret_cast<uint16_t *>(q.out + (int64_t)m * q.ld_out + (n >> 1)) = (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(h0 * inv, h1 * inv, 0, false);
+            if (ok) *reinterpret_cast<uint16_t *>(q.out + (int64_t)m * q.ld_out + (n >> 1)) = q8_codes2(h0, h1, q8_scale(byte));
             if (lane == 0) q.out_s[(int64_t)tn * q.ld_out_s + m] = (uint8_t)byte;
         }
     }

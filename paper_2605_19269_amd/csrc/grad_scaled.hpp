@@ -19,9 +19,8 @@ __device__ __forceinline__ void widen16(u32x4 (&o)[2], u32x4 w, float s)
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[e], true);
-        o[e >> 1][(e & 1) * 2] = pack_bf16x2(a[0] * s, a[1] * s);
-        o[e >> 1][(e & 1) * 2 + 1] = pack_bf16x2(b[0] * s, b[1] * s);
+        o[e >> 1][(e & 1) * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], s, false));
+        o[e >> 1][(e & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[e], s, true));
     }
 }
 

@@ -21,12 +21,20 @@ __device__ __forceinline__ uint32_t q8_scale_byte(float amax)
     const int e = (int)(b >> 23) - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
     return (uint32_t)(e < 1 ? 1 : e);                      // at most 247
 }
-// 2^(127 - byte) of a byte that q8_scale_byte made
-__device__ __forceinline__ float q8_inverse(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
-// 2^(byte - 127) of any byte
-__device__ __forceinline__ float q8_scale(uint32_t byte)
+// 2^(byte - 127), as the conversions of gfx950 take it: they use the exponent (all ones: NaN), so 255 needs no case of its own.  Checked over
+// all codes and bytes against the product in fp32.
+__device__ __forceinline__ float q8_scale(uint32_t byte) { return __builtin_bit_cast(float, byte == 0 ? 0x00400000u : byte << 23); }
+typedef __attribute__((ext_vector_type(2))) short q8_pair;
+// Four codes of v / scale, to the nearest, ties to even, in two instructions.  Finite elements are within range; infinities and NaN become NaN.
+__device__ __forceinline__ uint32_t q8_codes(float a, float b, float c, float d, float scale)
 {
-    return __builtin_bit_cast(float, byte == 0 ? 0x00400000u : (byte == 255 ? 0x7fc00000u : byte << 23));
+    q8_pair w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true));
+}
+__device__ __forceinline__ uint16_t q8_codes2(float a, float b, float scale)
+{
+    return (uint16_t)__builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q8_pair{0, 0}, a, b, scale, false)[0];
 }
 // |v| where it is finite, else 0: a block's scale comes from its finite elements
 __device__ __forceinline__ float q8_magnitude(float v)
@@ -34,11 +42,18 @@ __device__ __forceinline__ float q8_magnitude(float v)
     const float a = __builtin_fabsf(v);
     return a < __builtin_inff() ? a : 0.0f;
 }
-// Four codes of v * inv, to the nearest, ties to even.  Finite elements are within range; infinities and NaN become NaN.
-__device__ __forceinline__ uint32_t q8_codes(float a, float b, float c, float d, float inv)
+// The largest finite magnitude of the values that `each(f)` hands to f two at a time.  The maximum passes over NaN by itself (one instruction
+// for two values), so a wave looks at its values again only where an infinity is among them.
+template <class F>
+__device__ __forceinline__ float q8_largest(F each)
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+    float m = 0.0f;
+    each([&](float a, float b) { m = fmaxf(fmaxf(m, __builtin_fabsf(a)), __builtin_fabsf(b)); });
+    if (__ballot(m == __builtin_inff())) {
+        m = 0.0f;
+        each([&](float a, float b) { m = fmaxf(fmaxf(m, q8_magnitude(a)), q8_magnitude(b)); });
+    }
+    return m;
 }
 
 hipError_t launch_quantize(hipStream_t s, const uint16_t *X, int64_t R, int64_t C, int64_t ld, bool square, uint8_t *q, int64_t ldq, uint8_t *sc,

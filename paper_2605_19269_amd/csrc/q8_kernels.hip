@@ -5,19 +5,31 @@ namespace coda {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
-static __device__ __forceinline__ float lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
-static __device__ __forceinline__ float hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 
-// Largest finite magnitude among eight bf16 values
-static __device__ __forceinline__ float largest8(u32x4 v)
+// Largest finite magnitude among bf16 values, two at a time as whole numbers: the bits of magnitudes are in their order, those of infinities
+// and NaN from 0x7f80 on.  Where there are any, they are taken out and the maximum found again.
+template <int N>
+static __device__ __forceinline__ float largest_bf16(const u32x4 (&v)[N])
 {
-    float m = 0.0f;
+    u16x2 m = {0, 0};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) m = fmaxf(m, fmaxf(q8_magnitude(lo(v[e])), q8_magnitude(hi(v[e]))));
-    return m;
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, v[i][e] & 0x7fff7fffu));
+    uint32_t top = m[0] > m[1] ? m[0] : m[1];
+    if (__ballot(top >= 0x7f80u)) {                      // a wave's branch: seldom taken
+        top = 0;
+        for (int i = 0; i < N; ++i)
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t a = v[i][e] & 0x7fffu, b = (v[i][e] >> 16) & 0x7fffu;
+                top = a < 0x7f80u && a > top ? a : top;
+                top = b < 0x7f80u && b > top ? b : top;
+            }
+    }
+    return __builtin_bit_cast(float, top << 16);
 }
 template <int CTRL>
 static __device__ __forceinline__ float dpp_max(float m)
@@ -32,9 +44,17 @@ static __device__ __forceinline__ float max16(float m)
     m = dpp_max<0x141>(m);       // row_half_mirror
     return dpp_max<0x140>(m);    // row_mirror
 }
-static __device__ __forceinline__ u32x2 codes8(u32x4 v, float inv)
+static __device__ __forceinline__ u32x2 codes8(u32x4 v, float scale)
 {
-    return u32x2{q8_codes(lo(v[0]), hi(v[0]), lo(v[1]), hi(v[1]), inv), q8_codes(lo(v[2]), hi(v[2]), lo(v[3]), hi(v[3]), inv)};
+    u32x2 o;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t a = v[2 * e], b = v[2 * e + 1];
+        q8_pair w = {0, 0};
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, a), scale, false);
+        o[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, b), scale, true));
+    }
+    return o;
 }
 
 // Blocks of 1 x 128: sixteen lanes a row, eight elements a lane, four rows a wave and pass.  The scales of consecutive rows lie
@@ -58,8 +78,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const uint16_t *__re
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int64_t r = r0 + p * 4 + g;
-        const uint32_t byte = q8_scale_byte(max16(largest8(v[p])));
-        if (r < R && col < C) *reinterpret_cast<u32x2 *>(q + r * ldq + col) = codes8(v[p], q8_inverse(byte));
+        const u32x4 one[1] = {v[p]};
+        const uint32_t byte = q8_scale_byte(max16(largest_bf16(one)));
+        if (r < R && col < C) *reinterpret_cast<u32x2 *>(q + r * ldq + col) = codes8(v[p], q8_scale(byte));
         word[p] = (uint32_t)__builtin_amdgcn_readlane((int)byte, 0) | (uint32_t)__builtin_amdgcn_readlane((int)byte, 16) << 8 |
                   (uint32_t)__builtin_amdgcn_readlane((int)byte, 32) << 16 | (uint32_t)__builtin_amdgcn_readlane((int)byte, 48) << 24;
     }
@@ -94,20 +115,17 @@ __global__ __launch_bounds__(256) void quantize_square_kernel(const uint16_t *__
         v[p] = u32x4{0u, 0u, 0u, 0u};
         if (r < R && col < C) v[p] = *reinterpret_cast<const u32x4 *>(X + r * ld + col);
     }
-    float m = 0.0f;
-#pragma unroll
-    for (int p = 0; p < 8; ++p) m = fmaxf(m, largest8(v[p]));
-    m = max16(m);
+    float m = max16(largest_bf16(v));
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     m = fmaxf(m, __shfl_xor(m, 32, 64));
     if (lane == 0) largest[tid >> 6] = m;
     __syncthreads();
     const uint32_t byte = q8_scale_byte(fmaxf(fmaxf(largest[0], largest[1]), fmaxf(largest[2], largest[3])));
-    const float inv = q8_inverse(byte);
+    const float scale = q8_scale(byte);
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
         const int64_t r = r0 + p * 16 + rl;
-        if (r < R && col < C) *reinterpret_cast<u32x2 *>(q + r * ldq + col) = codes8(v[p], inv);
+        if (r < R && col < C) *reinterpret_cast<u32x2 *>(q + r * ldq + col) = codes8(v[p], scale);
     }
     if (tid < Q8_BLOCK) {
         if (r0 + tid < R) sc[kb * lds + r0 + tid] = (uint8_t)byte;
@@ -150,10 +168,8 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *__restri
         u32x4 o[2];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[p][e], false), d = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[p][e], true);
-            const f32x2 as = {a[0] * s, a[1] * s}, ds = {d[0] * s, d[1] * s};
-            o[e >> 1][(e & 1) * 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(as, bf16x2));
-            o[e >> 1][(e & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(ds, bf16x2));
+            o[e >> 1][(e & 1) * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[p][e], s, false));
+            o[e >> 1][(e & 1) * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[p][e], s, true));
         }
         u32x4 *to = reinterpret_cast<u32x4 *>(out + r * ld_out + col);
         to[0] = o[0];
