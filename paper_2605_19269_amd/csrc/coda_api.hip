@@ -677,12 +677,12 @@ coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_t K, cons
     if (!G) return CODA_ERR_NULL;
     if (ld_g < N || ld_g > MAX_LD) return CODA_ERR_SHAPE;
     if (!aligned16(G) || (ld_g & 3)) return CODA_ERR_ALIGN;
-    const int nsplit = coda::plan_grad(M, N, K, workspace != nullptr);
+    const coda::GradPlan plan = coda::plan_grad(M, N, K, workspace != nullptr);
     if (workspace) {
         if (!aligned16(workspace)) return CODA_ERR_ALIGN;
-        if (workspace_bytes < coda::grad_bytes(nsplit, M, N)) return CODA_ERR_WORKSPACE;
+        if (workspace_bytes < coda::grad_bytes(plan, M, N)) return CODA_ERR_WORKSPACE;
     }
-    if (((M + 255) / 256) * ((N + 255) / 256) > INT32_MAX / 16) return CODA_ERR_SHAPE;
+    if (((M + plan.tile - 1) / plan.tile) * ((N + plan.tile - 1) / plan.tile) > INT32_MAX / 16) return CODA_ERR_SHAPE;
     coda::GemmParams g{};
     g.M = (int)M;
     g.N = (int)N;
@@ -703,7 +703,7 @@ coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_t K, cons
     p.N = (int)N;
     p.K = (int)K;
     p.part = static_cast<float *>(workspace);
-    return launch_status(coda::launch_grad_scaled(nsplit, b8, g, p, static_cast<hipStream_t>(stream)));
+    return launch_status(coda::launch_grad_scaled(plan, b8, g, p, static_cast<hipStream_t>(stream)));
 }
 
 const char *coda_status_string(coda_status s)

@@ -24,82 +24,93 @@ __device__ __forceinline__ void widen16(u32x4 (&o)[2], u32x4 w, float s)
     }
 }
 
-// C: 256 x 256 tiles, eight waves of 128 x 64.  A stage is 64 tokens: four [32][256] bf16 tiles (A and B, two halves) of 16 KB in the layout
-// of lds_mn, two slots of them.  A thread widens two granules of sixteen columns of each operand per stage.
-template <class C, bool B8>
+// C: 256 x 256 tiles in eight waves of 128 x 64, or 128 x 128 in four of 64 x 64, two workgroups a CU.  A stage is 32 H tokens: H bf16 tiles of 32 tokens of either operand in the layout of lds_mn, two slots of them.  A
+// thread widens granules of sixteen columns, a few of each operand, for the next stage while this one is multiplied.
+template <class C, int H, bool B8>
 __global__ __launch_bounds__(C::NT) __attribute__((amdgpu_waves_per_eu(2, 2), amdgpu_num_vgpr(256))) void grad_scaled_kernel(const GemmParams g, const GradParams p)
 {
-    constexpr int TILE = 32 * 256 * 2, SLOT = 4 * TILE, NB = C::WTM / 16, NU = C::WTN / 16;
-    static_assert(C::BM == 256 && C::BN == 256 && C::NT == 512, "thread -> granule");
+    constexpr int GRA = C::BM / 16, GRB = C::BN / 16, QA = 32 * H * GRA / C::NT, QB = 32 * H * GRB / C::NT;       // granules a token, a thread
+    constexpr int TA = 32 * C::BM * 2, TB = 32 * C::BN * 2, SLOT = H * (TA + TB), NB = C::WTM / 16, NU = C::WTN / 16;
+    static_assert(32 * H * GRA % C::NT == 0 && 32 * H * GRB % C::NT == 0 && C::NT % GRA == 0 && C::NT % GRB == 0, "thread -> granule");
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * SLOT];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % C::WGM, wn = wave / C::WGM;
     const int tiles = p.tiles_m * p.tiles_n, split = (int)blockIdx.x / tiles;
     int tm, tn;
     tile_coords((int)blockIdx.x - split * tiles, tiles, p.tiles_m, p.tiles_n, tm, tn);
-    const int m0 = tm * 256, n0 = tn * 256;
-    const int stages = (p.K + 63) / 64;
+    const int m0 = tm * C::BM, n0 = tn * C::BN;
+    const int stages = (p.K + 32 * H - 1) / (32 * H);
     const int s0 = (int)((int64_t)split * stages / p.nsplit), s1 = (int)((int64_t)(split + 1) * stages / p.nsplit);
 
-    const int k = tid >> 4, gr = tid & 15;           // the thread's token (and k + 32) and granule
-    const bool in_a = m0 + gr * 16 < p.M, in_b = n0 + gr * 16 < p.N;             // M, N: multiples of 16 (bf16 B: of 8)
-    const bool half_b = !B8 && n0 + gr * 16 + 8 >= p.N;
-    const unsigned char *pa = p.A + m0 + gr * 16, *pb = p.B + (int64_t)(n0 + gr * 16) * (B8 ? 1 : 2);
-    const unsigned char *psa = p.sa + (int64_t)((m0 + gr * 16) >> 7) * p.ld_sa;
-    const unsigned char *psb = B8 ? p.sb + (int64_t)((n0 + gr * 16) >> 7) * p.ld_sb : nullptr;
-    u32x4 ra[2], rb[2][B8 ? 1 : 2];
-    uint32_t ba[2], bb[2];
+    // the thread's granule columns, and its token in a stage; further granules are NT / GR tokens on
+    const int ka = tid / GRA, ca = tid % GRA * 16, kb = tid / GRB, cb = tid % GRB * 16;
+    const bool in_a = m0 + ca < p.M, in_b = n0 + cb < p.N;                       // M, N: multiples of 16 (bf16 B: of 8)
+    const bool half_b = !B8 && n0 + cb + 8 >= p.N;
+    const unsigned char *pa = p.A + m0 + ca, *pb = p.B + (int64_t)(n0 + cb) * (B8 ? 1 : 2);
+    const unsigned char *psa = p.sa + (int64_t)((m0 + ca) >> 7) * p.ld_sa;
+    const unsigned char *psb = B8 ? p.sb + (int64_t)((n0 + cb) >> 7) * p.ld_sb : nullptr;
+    u32x4 ra[QA], rb[QB][B8 ? 1 : 2];
+    uint32_t ba[QA], bb[QB];
     auto fetch = [&](int s) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t t = (int64_t)s * 64 + h * 32 + k;
-            const bool in = t < p.K;
-            ra[h] = rb[h][0] = u32x4{0u, 0u, 0u, 0u};
-            ba[h] = bb[h] = 127u;
-            if constexpr (!B8) rb[h][1] = u32x4{0u, 0u, 0u, 0u};
-            if (in && in_a) {
-                ra[h] = *reinterpret_cast<const u32x4 *>(pa + t * p.lda);
-                ba[h] = psa[t];
+        for (int q = 0; q < QA; ++q) {
+            const int64_t t = (int64_t)s * (32 * H) + ka + q * (C::NT / GRA);
+            ra[q] = u32x4{0u, 0u, 0u, 0u};
+            ba[q] = 127u;
+            if (t < p.K && in_a) {
+                ra[q] = *reinterpret_cast<const u32x4 *>(pa + t * p.lda);
+                ba[q] = psa[t];
             }
-            if (in && in_b) {
-                rb[h][0] = *reinterpret_cast<const u32x4 *>(pb + t * p.ldb);
-                if constexpr (B8) bb[h] = psb[t];
-                else if (!half_b) rb[h][1] = *reinterpret_cast<const u32x4 *>(pb + t * p.ldb + 16);
+        }
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            const int64_t t = (int64_t)s * (32 * H) + kb + q * (C::NT / GRB);
+            rb[q][0] = u32x4{0u, 0u, 0u, 0u};
+            bb[q] = 127u;
+            if constexpr (!B8) rb[q][1] = u32x4{0u, 0u, 0u, 0u};
+            if (t < p.K && in_b) {
+                rb[q][0] = *reinterpret_cast<const u32x4 *>(pb + t * p.ldb);
+                if constexpr (B8) bb[q] = psb[t];
+                else if (!half_b) rb[q][1] = *reinterpret_cast<const u32x4 *>(pb + t * p.ldb + 16);
             }
         }
     };
-    const uint32_t spot = lds_mn<256>(k, gr);
     auto put = [&](int slot) {
+        u32x4 w[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            u32x4 w[2];
-            widen16(w, ra[h], q8_scale(ba[h]));
-            u32x4 *at = reinterpret_cast<u32x4 *>(smem + slot * SLOT + h * TILE + spot);
+        for (int q = 0; q < QA; ++q) {
+            const int k = ka + q * (C::NT / GRA);
+            widen16(w, ra[q], q8_scale(ba[q]));
+            u32x4 *at = reinterpret_cast<u32x4 *>(smem + slot * SLOT + (k >> 5) * TA + lds_mn<C::BM>(k & 31, ca >> 4));
             at[0] = w[0];
             at[1] = w[1];
+        }
+#pragma unroll
+        for (int q = 0; q < QB; ++q) {
+            const int k = kb + q * (C::NT / GRB);
             if constexpr (B8) {
-                widen16(w, rb[h][0], q8_scale(bb[h]));
+                widen16(w, rb[q][0], q8_scale(bb[q]));
             } else {
-                w[0] = rb[h][0];
-                w[1] = rb[h][1];
+                w[0] = rb[q][0];
+                w[1] = rb[q][1];
             }
-            u32x4 *bt = reinterpret_cast<u32x4 *>(smem + slot * SLOT + (2 + h) * TILE + spot);
-            bt[0] = w[0];
-            bt[1] = w[1];
+            u32x4 *at = reinterpret_cast<u32x4 *>(smem + slot * SLOT + H * TA + (k >> 5) * TB + lds_mn<C::BN>(k & 31, cb >> 4));
+            at[0] = w[0];
+            at[1] = w[1];
         }
     };
     Acc16<C> acc;
     acc_zero(acc);
     auto contract = [&](int slot) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const unsigned char *ta = smem + slot * SLOT + h * TILE, *tb = ta + 2 * TILE;
+        for (int h = 0; h < H; ++h) {
+            const unsigned char *ta = smem + slot * SLOT + h * TA, *tb = smem + slot * SLOT + H * TA + h * TB;
             bf16x8 fb[NU];
 #pragma unroll
-            for (int u = 0; u < NU; ++u) fb[u] = dl_frag16<256, false>(tb, wn * C::WTN + u * 16, lane);
+            for (int u = 0; u < NU; ++u) fb[u] = dl_frag16<C::BN, false>(tb, wn * C::WTN + u * 16, lane);
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
-                const bf16x8 fa = dl_frag16<256, false>(ta, wm * C::WTM + i * 16, lane);
+                const bf16x8 fa = dl_frag16<C::BM, false>(ta, wm * C::WTM + i * 16, lane);
 #pragma unroll
                 for (int u = 0; u < NU; ++u) acc.a[i][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[u], fa, acc.a[i][u], 0, 0, 0);
             }
@@ -110,11 +121,26 @@ __global__ __launch_bounds__(C::NT) __attribute__((amdgpu_waves_per_eu(2, 2), am
         put(0);
         if (s0 + 1 < s1) fetch(s0 + 1);
         __syncthreads();
+        // Of eight waves, two on a SIMD, one widens the next stage before it multiplies this one and the other after it, so that the SIMD's
+        // vector and matrix unit work at the same time; raised priority keeps the multiplying one fed (8192 x 2048 x 16384: 529 us
+        // without either, 512 with the order alone, 498 with both; 477 with the tokens of a stage indexed as here).
+        const bool first = C::NT == 512 && wave >= 4;
         for (int s = s0; s < s1; ++s) {
             const int slot = (s - s0) & 1;
+            auto next = [&]() {
+                if (s + 1 < s1) put(slot ^ 1);
+                if (s + 2 < s1) fetch(s + 2);
+            };
+            if (first) next();
+            __builtin_amdgcn_s_setprio(1);
             contract(slot);
-            if (s + 1 < s1) put(slot ^ 1);
-            if (s + 2 < s1) fetch(s + 2);
+            __builtin_amdgcn_s_setprio(0);
+            // the MFMAs stay ahead of the branch
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int u = 0; u < NU; ++u) asm volatile("" : "+v"(acc.a[i][u]));
+            if (!first) next();
             __syncthreads();
         }
     }
@@ -128,7 +154,7 @@ __global__ __launch_bounds__(C::NT) __attribute__((amdgpu_waves_per_eu(2, 2), am
                 if (m + i * 16 < p.M && n + u * 16 < p.N) *reinterpret_cast<f32x4 *>(out + (int64_t)(m + i * 16) * p.N + n + u * 16) = acc.get(i, u);
         return;
     }
-    if (m0 + 256 > p.M || n0 + 256 > p.N) run_epilogue<C, Acc16<C>, EPI_ACCUM, true, 2 * SLOT>(acc, g, m0, n0, tn, smem, nullptr, tid);
+    if (m0 + C::BM > p.M || n0 + C::BN > p.N) run_epilogue<C, Acc16<C>, EPI_ACCUM, true, 2 * SLOT>(acc, g, m0, n0, tn, smem, nullptr, tid);
     else run_epilogue<C, Acc16<C>, EPI_ACCUM, false, 2 * SLOT>(acc, g, m0, n0, tn, smem, nullptr, tid);
 }
 

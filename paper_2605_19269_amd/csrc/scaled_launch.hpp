@@ -64,17 +64,24 @@ template <> hipError_t launch_scaled_256<false>(int, bool, const GemmParams &, c
 template <> hipError_t launch_scaled_128<true>(int, bool, const GemmParams &, const Q8Params &, const ScaledParams &, hipStream_t);
 template <> hipError_t launch_scaled_128<false>(int, bool, const GemmParams &, const Q8Params &, const ScaledParams &, hipStream_t);
 
-// Ranges of the tokens of a gradient, so that its 256 x 256 tiles fill the chip; 1: G is added to by the tiles' own kernel
-inline int plan_grad(int64_t M, int64_t N, int64_t K, bool workspace)
+// tile x tile of a gradient, and ranges of its tokens (1: G is added to by the tiles' own kernel).
+// 256: one workgroup a CU, bound by the matrix cores and LDS.  128: two a CU, four waves of 64 x 64, which read a third more from LDS for what they
+// compute but fill the chip with a quarter of the output, end a tile while the other computes, and need fewer partials where the tokens
+// are divided.  8192 x (2048 x 16384) 477 us against 647, 1000 x (5632 x 2048) 43.4 / 46.7; 256 x (4096 x 14336) 127 / 121, 64 x (2048 x 8192) 26.3 / 25.5;
+// with few tiles, in ranges: 8192 x (512 x 1024) 208 undivided / 26.0, 300 x (4800 x 752) 21.2 / 12.0, 2048 x (2048 x 2048) 63 / 37.5.
+struct GradPlan {
+    int tile, nsplit;
+};
+inline GradPlan plan_grad(int64_t M, int64_t N, int64_t K, bool workspace)
 {
-    const int64_t tiles = ((M + 255) / 256) * ((N + 255) / 256), stages = (K + 63) / 64;
-    if (!workspace || tiles >= 128 || tiles <= 0) return 1;
-    int64_t n = 256 / tiles;
+    const int64_t large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128), stages = (K + 63) / 64;
+    if (large >= 128 && K > 256) return GradPlan{256, 1};
+    int64_t n = workspace && small > 0 && small < 256 ? 512 / small : 1;
     if (n > 16) n = 16;
     if (n > stages / 4) n = stages / 4;
-    return n > 1 ? (int)n : 1;
+    return GradPlan{128, n > 1 ? (int)n : 1};
 }
-inline size_t grad_bytes(int nsplit, int64_t M, int64_t N) { return nsplit > 1 ? (size_t)nsplit * (size_t)M * (size_t)N * sizeof(float) : 0; }
-hipError_t launch_grad_scaled(int nsplit, bool b8, const GemmParams &g, const GradParams &p, hipStream_t s);
+inline size_t grad_bytes(const GradPlan &pl, int64_t M, int64_t N) { return pl.nsplit > 1 ? (size_t)pl.nsplit * (size_t)M * (size_t)N * sizeof(float) : 0; }
+hipError_t launch_grad_scaled(const GradPlan &pl, bool b8, const GemmParams &g, const GradParams &p, hipStream_t s);
 
 }  // namespace coda
