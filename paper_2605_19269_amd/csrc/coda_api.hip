@@ -606,7 +606,7 @@ coda_status coda_dequantize(void *stream, const coda_mat *Q, const void *scales,
 size_t coda_gemm_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K)
 {
     if (!sizes_fit(M, N, K) || M == 0 || N == 0) return 0;
-    return coda::scaled_bytes(coda::plan_scaled(M, N, K, true), M, N);
+    return coda::scaled_bytes(coda::plan_scaled(M, N, K, true, false), M, N);
 }
 
 coda_status coda_gemm_scaled(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const void *scales_a, int64_t ld_scales_a,
@@ -626,13 +626,14 @@ coda_status coda_gemm_scaled(void *stream, int64_t M, int64_t N, int64_t K, cons
     Parsed ps;
     if ((st = parse_program(prog, n_ops, M, N, true, ps)) != CODA_OK) return st;
     if (M == 0 || N == 0) return CODA_OK;
-    coda::ScaledPlan plan = coda::plan_scaled(M, N, K, workspace != nullptr);
+    const bool narrow = !ps.q8 && B->trans && ((ps.mode == coda::EPI_LINEAR && ps.p.rowred_mode == coda::ROWRED_NONE && !ps.p.lse_max) || ps.mode == coda::EPI_SWIGLU_FWD);
+    coda::ScaledPlan plan = coda::plan_scaled(M, N, K, workspace != nullptr, narrow);
     if (workspace) {
         if (!aligned16(workspace)) return CODA_ERR_ALIGN;
-        if (workspace_bytes < coda::scaled_bytes(plan, M, N)) return CODA_ERR_WORKSPACE;
+        if (workspace_bytes < coda_gemm_scaled_workspace_bytes(M, N, K)) return CODA_ERR_WORKSPACE;
     }
-    if (plan.nsplit == 0 && !ps.q8 && ps.mode == coda::EPI_RMSNORM_BWD) plan.bm = coda::TILE_M;      // its column partials are per 256 rows
-    if (((M + plan.bm - 1) / plan.bm) * ((N + plan.bn - 1) / plan.bn) > INT32_MAX / 16) return CODA_ERR_SHAPE;
+    if (!plan.few && plan.nsplit == 0 && !ps.q8 && ps.mode == coda::EPI_RMSNORM_BWD) plan.bm = coda::TILE_M;      // its column partials are per 256 rows
+    if (!plan.few && ((M + plan.bm - 1) / plan.bm) * ((N + plan.bn - 1) / plan.bn) > INT32_MAX / 16) return CODA_ERR_SHAPE;
     ps.p.M = (int)M;
     ps.p.N = (int)N;
     ps.p.K = (int)K;

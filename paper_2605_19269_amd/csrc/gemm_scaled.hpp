@@ -840,4 +840,114 @@ __global__ __launch_bounds__(C::NT) __attribute__((amdgpu_waves_per_eu(2, 2), am
     }
 }
 
+
+// ---------------------------------------------------------------------------------
+// Up to 32 rows against a B stored [N x K], in one kernel and without a workspace: a workgroup owns 16 or 32 columns, its eight waves take
+// every eighth block of the contraction and add up in LDS, in wave order.  A block is one v_mfma_scale_f32_16x16x128_f8f6f4, whose fragments
+// come straight from memory: lane l holds bytes 16 (l / 16) .. and 64 + 16 (l / 16) .. of its row's 128, for both operands (which k meets which
+// is free within a block), so that a load takes 64 consecutive bytes of a row.  Four blocks of a wave are in flight.  Bound by HBM and, with
+// few weights, by the launch.  For programs without row reductions, whose partials are per 256 columns.
+// ---------------------------------------------------------------------------------
+template <int EPI>
+__device__ __forceinline__ void few_program(const GemmParams &p, int m, int n, f32x4 v)
+{
+    static_assert(EPI == EPI_LINEAR || EPI == EPI_SWIGLU_FWD, "programs without row reductions");
+    if (p.row_scale) v *= p.row_scale[m];
+    if constexpr (EPI == EPI_SWIGLU_FWD) {
+        const float h0 = v[0] * fast_sigmoid(v[0]) * v[1], h1 = v[2] * fast_sigmoid(v[2]) * v[3];
+        *reinterpret_cast<uint32_t *>(reinterpret_cast<uint16_t *>(p.out) + (int64_t)m * p.ld_out + (n >> 1)) = pack_bf16x2(h0, h1);
+        if (p.out2) *reinterpret_cast<u32x2 *>(p.out2 + (int64_t)m * p.ld_out2 + n) = pack4(v);
+    } else {
+        if (p.rope_cos && n < p.rope_cols)
+            rope_unit(v, p, (int64_t)clampi(p.rope_pos[m], 0, p.rope_T - 1) * p.rope_half, (n >> 1) % p.rope_half);
+        if (p.add) v += unpack4(*reinterpret_cast<const u32x2 *>(p.add + (int64_t)m * p.ld_add + n));
+        if (p.side) *reinterpret_cast<u32x2 *>(p.side + (int64_t)m * p.ld_side + n) = pack4(v * *reinterpret_cast<const f32x4 *>(p.col_scale + n));
+        if (p.out_f32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(p.out) + (int64_t)m * p.ld_out + n) = v;
+        else *reinterpret_cast<u32x2 *>(reinterpret_cast<uint16_t *>(p.out) + (int64_t)m * p.ld_out + n) = pack4(v);
+    }
+}
+
+template <int RB, int CB, int EPI>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(RB + CB > 2 ? 2 : 4, RB + CB > 2 ? 2 : 4))) void gemm_scaled_few(const GemmParams g, const ScaledParams p)
+{
+    constexpr int W = 8, DEPTH = RB + CB > 3 ? 3 : 4, ROWS = RB * 16, COLS = CB * 16;
+    __shared__ f32x4 sums[W][ROWS][COLS / 4 + 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, q = lane >> 4;
+    const int n0 = (int)blockIdx.x * COLS, blocks = (p.K + 127) / 128;
+    struct Block {
+        u32x4 a[RB][2], b[CB][2];
+        int sa[RB], sb[CB];
+    };
+    // rows and columns past the end: the last one's again
+    const unsigned char *ga[RB], *gb[CB], *gsa[RB], *gsb[CB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int m = r * 16 + lr < p.M ? r * 16 + lr : p.M - 1;
+        ga[r] = p.A + (int64_t)m * p.lda + q * 16;
+        gsa[r] = p.sa + m;
+    }
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+        const int n = n0 + c * 16 + lr < p.N ? n0 + c * 16 + lr : p.N - 1;
+        gb[c] = p.B + (int64_t)n * p.ldb + q * 16;
+        gsb[c] = p.sb + n;
+    }
+    auto load = [&](Block &s, int blk) {
+        const int64_t at = (int64_t)blk * 128;
+        const bool lo = at + q * 16 < p.K, hi = at + 64 + q * 16 < p.K;          // K is a multiple of 16
+        auto two = [&](u32x4(&v)[2], const unsigned char *from) {
+            v[0] = v[1] = u32x4{0u, 0u, 0u, 0u};
+            if (lo) v[0] = *reinterpret_cast<const u32x4 *>(from + at);
+            if (hi) v[1] = *reinterpret_cast<const u32x4 *>(from + at + 64);
+        };
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            two(s.b[c], gb[c]);
+            s.sb[c] = gsb[c][blk * p.ld_sb];
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            two(s.a[r], ga[r]);
+            s.sa[r] = gsa[r][blk * p.ld_sa];
+        }
+    };
+    f32x4 acc[RB][CB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) acc[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto join = [](const u32x4(&v)[2]) {
+        return i32x8{(int)v[0][0], (int)v[0][1], (int)v[0][2], (int)v[0][3], (int)v[1][0], (int)v[1][1], (int)v[1][2], (int)v[1][3]};
+    };
+    Block ring[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (wave + d * W < blocks) load(ring[d], wave + d * W);
+    for (int b0 = wave; b0 < blocks; b0 += DEPTH * W) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int blk = b0 + d * W;
+            if (blk >= blocks) break;
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+                    acc[r][c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(join(ring[d].b[c]), join(ring[d].a[r]), acc[r][c], 0, 0, 0, ring[d].sb[c], 0,
+                                                                                 ring[d].sa[r]);
+            if (blk + DEPTH * W < blocks) load(ring[d], blk + DEPTH * W);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int c = 0; c < CB; ++c) sums[wave][r * 16 + lr][c * 4 + q] = acc[r][c];
+    __syncthreads();
+    const int m = tid / (COLS / 4), u = tid % (COLS / 4), n = n0 + u * 4;
+    if (tid >= ROWS * (COLS / 4) || m >= p.M || n >= p.N) return;
+    f32x4 v = sums[0][m][u];
+#pragma unroll
+    for (int w = 1; w < W; ++w) v += sums[w][m][u];
+    few_program<EPI>(g, m, n, v);
+}
+
 }  // namespace coda

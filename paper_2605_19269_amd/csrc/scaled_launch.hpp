@@ -30,23 +30,33 @@ struct GradParams {
     float *part;                         // [nsplit][M][N] where nsplit > 1
 };
 
-// bm x bn tiles; nsplit = 0: tile and program in one kernel, else every tile is cut along the contraction into nsplit ranges whose fp32
-// partials lie in the workspace, and the program runs over those
+// few: up to 32 rows in one kernel.  Else bm x bn tiles; nsplit = 0: tile and program in one kernel, else every tile is cut along the contraction into
+// nsplit ranges whose fp32 partials lie in the workspace, and the program runs over those.
 struct ScaledPlan {
     int bm, bn, nsplit;
+    bool few;
 };
-inline ScaledPlan plan_scaled(int64_t M, int64_t N, int64_t K, bool workspace)
+// `narrow`: a program without row reductions and 8-bit outputs, on a B stored [N x K]
+inline ScaledPlan plan_scaled(int64_t M, int64_t N, int64_t K, bool workspace, bool narrow)
 {
-    const int64_t blocks = (K + 127) / 128, large = ((M + 255) / 256) * ((N + 255) / 256);
+    // Against partials and a second kernel (us): 6144 x 4096, 1 / 8 / 16 / 32 rows 7.2 / 7.8 / 8.7 / 10.5 and 9.6 / 9.7 / 9.9 / 10.1; 4096 x 14336, 1 / 8 / 32 rows
+    // 12.3 / 13.2 / 21.9 and 13.2 / 13.6 / 14.2; 16384 x 2048, one row 9.5 and 10.1; 2048 x 2048, 32 rows 6.8 and 9.7; 28672 x 4096, one row 27 and 20.7 (many
+    // workgroups one after the other, each with its own start; every one fetches the rows of A anew).  Without a workspace against 128-row tiles: 4096 x 14336,
+    // 32 rows 23 and 95.
+    const bool small = (M <= 8 && N <= 8192) || (M <= 16 && N * K <= (int64_t)1 << 25) || N * K <= (int64_t)1 << 23;
+    if (narrow && M <= 32 && (!workspace || small)) return ScaledPlan{0, 0, 0, true};
+    const int64_t blocks = (K + 127) / 128, large = ((M + 255) / 256) * ((N + 255) / 256), half = ((M + 127) / 128) * ((N + 255) / 256);
     if (workspace && blocks > 0 && (M <= 64 || large < 64)) {
         const int bm = M <= 32 ? 32 : (M <= 64 ? 64 : 128);
         const int64_t tiles = ((M + bm - 1) / bm) * ((N + 127) / 128);
         int64_t n = tiles >= 192 ? 1 : (256 + tiles / 2) / tiles;
         if (n > 16) n = 16;
         if (n > blocks / 4) n = blocks / 4 > 0 ? blocks / 4 : 1;
-        return ScaledPlan{bm, 128, (int)n};
+        return ScaledPlan{bm, 128, (int)n, false};
     }
-    return ScaledPlan{large >= 192 ? 256 : 128, 256, 0};
+    // One round of 128-row tiles takes 0.74 to 0.88 of one of 256 (2048 x 4096 x 4096 36.7 us / 41.7, 1000 x 4096 x 14336 94 / 127, 509 x 16384 x 2048 22.2 /
+    // 27.9), two take longer (1000 x 11264 x 2048 with SwiGLU 39.5 / 30.4).
+    return ScaledPlan{half <= 256 ? 128 : 256, 256, 0, false};
 }
 inline size_t scaled_bytes(const ScaledPlan &pl, int64_t M, int64_t N) { return (size_t)pl.nsplit * (size_t)M * (size_t)N * sizeof(float); }
 
