@@ -186,3 +186,24 @@ def test_the_reference_knows_the_format():
     assert ((byte == 1) | (amax > 448 * R.scale(byte - 1))).all()
     x = torch.tensor([17.0, 18.0, 19.0, 2.0 ** -10, 3 * 2.0 ** -10], dtype=torch.float64)
     assert R.round_e4m3(x).tolist() == [16.0, 18.0, 20.0, 0.0, 2.0 ** -8]                                # ties to even, subnormals too
+
+
+def test_kernels_fit_their_registers_and_lds():
+    """What the compiler reported: nothing spills in the whole-tile kernels, the small ones and the gradients; two registers in the ragged 256 x 256 instances of
+    SwiGLU backward into 8 bits."""
+    import os
+    import re
+    from paper_2605_19269_amd import build as B
+    if not os.path.exists(B.RESOURCES):
+        B.build(force=True)
+    seen = {}
+    for line in open(B.RESOURCES):
+        name, vgpr, agpr, scratch, spill, lds = line.split()
+        m = re.match(r"_ZN4coda\d+(gemm_scaled_\w+?|grad_scaled_kernel|epi_rows_q8_kernel|quantize_\w+?_kernel|dequantize_kernel)(I|EP)(.*)", name)
+        if not m:
+            continue
+        seen[m.group(1)] = seen.get(m.group(1), 0) + 1
+        ragged_backward = re.match(r"gemm_scaled_largeILb[01]ELi2ELb1ELb1E", m.group(1) + m.group(2) + m.group(3))
+        assert int(spill) <= (4 if ragged_backward else 0) and int(agpr) == 0 and int(vgpr) <= 256 and int(lds) <= 160 * 1024, line
+    assert seen == {"gemm_scaled_few": 8, "gemm_scaled_large": 28, "gemm_scaled_tile": 12, "gemm_scaled_partial": 6, "grad_scaled_kernel": 4, "epi_rows_q8_kernel": 3,
+                    "quantize_rows_kernel": 2, "quantize_square_kernel": 1, "dequantize_kernel": 2}, seen
