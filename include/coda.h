@@ -330,7 +330,7 @@ CODA_API coda_status coda_quantize(void *stream, const coda_mat *X, int32_t squa
                           int64_t ld_scales, void *scales_t, int64_t ld_scales_t);
 
 /* Q (CODA_F8E4M3, [R x C], trans 0, C a multiple of 8) and its scales -> bf16 [R x C]: a checkpoint for the ops that read bf16 (the C of
-   RMSNORM_BWD).  Exact but for values below 2^-133. */
+   RMSNORM_BWD).  Exact but for values below 2^-133; those from 2^128 on (codes of the largest bf16 numbers may round up to it) become infinite. */
 CODA_API coda_status coda_dequantize(void *stream, const coda_mat *Q, const void *scales, int64_t ld_scales, void *out, int64_t ld_out);
 
 /*
@@ -352,7 +352,7 @@ CODA_API coda_status coda_dequantize(void *stream, const coda_mat *Q, const void
  * workspace / workspace_bytes: device memory, 16-byte aligned; may be NULL.  With coda_gemm_scaled_workspace_bytes(M, N, K) bytes (0: no
  * use for any) shapes with few output tiles divide the contraction among workgroups, which leave fp32 partials there for a second
  * kernel.  A non-NULL workspace that is smaller is CODA_ERR_WORKSPACE.  It holds nothing between calls; two calls that share one must not
- * overlap in time.  The order of additions depends on the sizes, the layout of B and whether a workspace is given.
+ * overlap in time.  The order of additions depends on the sizes, the layout of B, the program and whether a workspace is given.
  */
 CODA_API coda_status coda_gemm_scaled(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const void *scales_a, int64_t ld_scales_a,
                              const coda_mat *B, const void *scales_b, int64_t ld_scales_b, const coda_epi_op *prog /* host */, int32_t n_ops,
@@ -364,7 +364,7 @@ CODA_API size_t coda_gemm_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K
  * A: CODA_F8E4M3 as stored [K x M], trans 1, with its scales [ceil(M / 128)][>= K] (blocks along the features, as the forward pass left
  * them).  B as stored [K x N], trans 0: CODA_F8E4M3 with scales [ceil(N / 128)][>= K], or CODA_BF16 with scales_b NULL.  M, and N of an
  * 8-bit B, are multiples of 16, N of a bf16 B of 8; K is free.  G: f32 [M x N], 16-byte aligned, ld_g a multiple of 4.
- * Elements are widened to bf16 with their scale (exact but below 2^-133) and summed in fp32 by the bf16 matrix instructions.
+ * Elements are widened to bf16 with their scale (as by coda_dequantize) and summed in fp32 by the bf16 matrix instructions.
  * workspace: as above, coda_grad_scaled_workspace_bytes(M, N, K) bytes.
  */
 CODA_API coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_t K, const coda_mat *A, const void *scales_a, int64_t ld_scales_a,
