@@ -39,24 +39,41 @@ struct ScaledPlan {
 // `narrow`: a program without row reductions and 8-bit outputs, on a B stored [N x K]
 inline ScaledPlan plan_scaled(int64_t M, int64_t N, int64_t K, bool workspace, bool narrow)
 {
-    // Against partials and a second kernel (us): 6144 x 4096, 1 / 8 / 16 / 32 rows 7.2 / 7.8 / 8.7 / 10.5 and 9.6 / 9.7 / 9.9 / 10.1; 4096 x 14336, 1 / 8 / 32 rows
-    // 12.3 / 13.2 / 21.9 and 13.2 / 13.6 / 14.2; 16384 x 2048, one row 9.5 and 10.1; 2048 x 2048, 32 rows 6.8 and 9.7; 28672 x 4096, one row 27 and 20.7 (many
+    // Against partials and a second kernel (us): 6144 x 4096, 1 / 8 / 16 / 32 rows 7.2 / 7.8 / 8.7 / 10.5 and 9.6 / 9.7 / 9.9 / 10.1; 4096 x 14336, 1 / 8 / 24 rows
+    // 12.3 / 13.2 / 20.2 and 13.2 / 13.6 / 14.2; 16384 x 2048, one row 9.5 and 10.1; 4096 x 4096, 24 rows 8.4 and 9.0; 28672 x 4096, one row 27 and 20.7 (many
     // workgroups one after the other, each with its own start; every one fetches the rows of A anew).  Without a workspace against 128-row tiles: 4096 x 14336,
     // 32 rows 23 and 95.
-    const bool small = (M <= 8 && N <= 8192) || (M <= 16 && N * K <= (int64_t)1 << 25) || N * K <= (int64_t)1 << 23;
+    const bool small = (M <= 8 && N <= 8192) || (M <= 16 && N * K <= (int64_t)1 << 25) || N * K <= (int64_t)1 << 24;
     if (narrow && M <= 32 && (!workspace || small)) return ScaledPlan{0, 0, 0, true};
-    const int64_t blocks = (K + 127) / 128, large = ((M + 255) / 256) * ((N + 255) / 256), half = ((M + 127) / 128) * ((N + 255) / 256);
-    if (workspace && blocks > 0 && (M <= 64 || large < 64)) {
-        const int bm = M <= 32 ? 32 : (M <= 64 ? 64 : 128);
-        const int64_t tiles = ((M + bm - 1) / bm) * ((N + 127) / 128);
-        int64_t n = tiles >= 192 ? 1 : (256 + tiles / 2) / tiles;
-        if (n > 16) n = 16;
-        if (n > blocks / 4) n = blocks / 4 > 0 ? blocks / 4 : 1;
-        return ScaledPlan{bm, 128, (int)n, false};
+    // What the choices take, in microseconds, as fitted.  A round of 256 tiles of 128 x 256 takes 7 and 0.9 for a block of the contraction, one of 256 x 256, which
+    // reads less for what it computes, 9 and 1.55; with few of the CUs at work a block takes 0.7 and 1.1.  128 and 256 rows: 2048 x 4096 x 4096 35.8 and 42.1,
+    // 1000 x 4096 x 14336 94 and 126, 509 x 16384 x 2048 21.7 and 27.6 (one round each); 2500 x 4608 x 2048 37.8 and 29.3 (two and one); 8192 x 16384 x 2048
+    // 342 (by the formula) and 272; 1039 x 14336 x 4096 69.6 and 102 (two and 1.1).
+    const int64_t blocks = (K + 127) / 128, half = ((M + 127) / 128) * ((N + 255) / 256), large = ((M + 255) / 256) * ((N + 255) / 256);
+    auto rounds = [blocks](int64_t count, double start, double few, double all) {
+        const double rest = (double)(count % 256) / 256;
+        return (double)(count / 256) * (start + all * (double)blocks) + (rest > 0 ? start + (few + (all - few) * rest) * (double)blocks : 0);
+    };
+    const double t128 = rounds(half, 7, 0.7, 0.9), t256 = rounds(large, 9, 1.1, 1.55);
+    const ScaledPlan direct{t128 <= t256 ? 128 : 256, 256, 0, false};
+    if (!workspace || blocks == 0) return direct;
+    // Partials: a block takes 0.33, 0.36 and 0.5 in tiles of 32, 64 and 128 x 128; partials are written and read at 6.5 TB/s; 9 for two launches.  No more than a
+    // workgroup a CU: 215 x 4224 x 10416, 66 tiles in 3 ranges 25.8, in 4 38.1; 33 x 11264 x 2048, 88 tiles in 2 ranges 11.1, in 3 13.4.  Against the
+    // direct tiles: 1821 x 2048 x 8192 47.2 and 56.2, 1000 x 2048 x 5632 24.6 and 41.5, 96 x 2048 x 1024 8.6 and 12.0, 300 x 2048 x 256 7.1 and 7.4 (a launch less
+    // for the host); 614 x 5600 x 1584 23.2 and 19.7.
+    const int bm = M <= 32 ? 32 : (M <= 64 ? 64 : 128);
+    const int64_t tiles = ((M + bm - 1) / bm) * ((N + 127) / 128);
+    const double stage = bm == 32 ? 0.33 : (bm == 64 ? 0.36 : 0.5), join = (double)M * (double)N * 8 / 6.5e6;
+    double best = t128 < t256 ? t128 : t256;
+    int n = 0;
+    for (int i = 1; i <= 16 && i <= blocks && (tiles * i <= 256 || (i == 1 && bm < 128)); ++i) {
+        const double t = 9 + stage * (double)((blocks + i - 1) / i) * (double)((tiles * i + 255) / 256) + join * i;
+        if (t < best) {
+            best = t;
+            n = i;
+        }
     }
-    // One round of 128-row tiles takes 0.74 to 0.88 of one of 256 (2048 x 4096 x 4096 36.7 us / 41.7, 1000 x 4096 x 14336 94 / 127, 509 x 16384 x 2048 22.2 /
-    // 27.9), two take longer (1000 x 11264 x 2048 with SwiGLU 39.5 / 30.4).
-    return ScaledPlan{half <= 256 ? 128 : 256, 256, 0, false};
+    return n ? ScaledPlan{bm, 128, n, false} : direct;
 }
 inline size_t scaled_bytes(const ScaledPlan &pl, int64_t M, int64_t N) { return (size_t)pl.nsplit * (size_t)M * (size_t)N * sizeof(float); }
 
