@@ -7,8 +7,9 @@
 // byte for the lane's row of A and one for its column of B.  So the sums stay in one set of fp32 accumulators and a block costs
 // a few byte reads.  Scales lie [block][row]: the rows of a tile are BM consecutive bytes.
 //
-// Tiles of up to 128 rows: the ring, its loads and waits are those of the small tiles (gemm_small.hpp).  256 x 256: see
-// scaled_contract_large.
+// Tiles of up to 128 rows: the ring and its waits are those of the small tiles (gemm_small.hpp).  The loads of a stage are spread over a whole one: half of
+// them in the second half of the stage whose slot they refill, half in the first of the next, between the MFMAs of each row.  All in one half the waves queue
+// up behind them (1000 x 4096 x 14336 in 128 x 256 tiles 93.4 us, spread 76; 2048 x 4096 x 4096 36.1 and 34.0).  256 x 256: see scaled_contract_large.
 #pragma once
 #include "gemm_small.hpp"
 #include "epi_rows.hpp"
@@ -79,7 +80,7 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
         ++next;
         slot_in = slot_in + C::STAGE == C::LDS ? 0u : slot_in + C::STAGE;
     };
-    // part q of Q of the stage's loads; the last part moves on to the next stage
+    // part q of Q of a stage's loads; the last part moves on to the next stage
     auto issue_part = [&](int q, int Q) {
         const unsigned char *sa = ga + (int64_t)next * 128, *sb = gb + (int64_t)next * stepb;
         const uint32_t la = lds0 + slot_in + (uint32_t)(wave * C::LA * 1024), lb = lds0 + slot_in + (uint32_t)(C::A_BYTES + wave * C::LB * 1024);
@@ -161,8 +162,10 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
     };
-    auto stage = [&](int t, bool steady) {
+    bool pending = false;                            // the second half of a stage's loads is still to come
+    auto stage = [&](int t, bool steady, bool pend) {
         mma(fb, [&](int i) {
+            if (pend) issue_part(NB + i, 2 * NB);
             if (i == 0) read_b(fn, 1);
             read_a(i, 1);
         });
@@ -184,7 +187,7 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
             }
         }
         mma(fn, [&](int i) {
-            if (fill) issue_part(i, NB);
+            if (fill) issue_part(i, 2 * NB);
             if (!more) return;
             if (i == 0) {
                 read_b(fb, 0);
@@ -192,6 +195,7 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
             }
             read_a(i, 0);
         });
+        pending = fill;
         if (more) {
 #pragma unroll
             for (int i = 0; i < NB; ++i) sa[i] = na[i];
@@ -213,8 +217,11 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
 #pragma unroll
     for (int i = 0; i < NB; ++i) read_a(i, 0);
     int t = 0;
-    for (; t + S + (ragged ? 1 : 0) < KT; ++t) stage(t, true);
-    for (; t < KT; ++t) stage(t, false);
+    if (S + (ragged ? 1 : 0) < KT) {
+        stage(t++, true, false);
+        for (; t + S + (ragged ? 1 : 0) < KT; ++t) stage(t, true, true);
+    }
+    for (; t < KT; ++t) stage(t, false, pending);
     __syncthreads();
 }
 

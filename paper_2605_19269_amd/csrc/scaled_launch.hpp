@@ -45,22 +45,22 @@ inline ScaledPlan plan_scaled(int64_t M, int64_t N, int64_t K, bool workspace, b
     // 32 rows 23 and 95.
     const bool small = (M <= 8 && N <= 8192) || (M <= 16 && N * K <= (int64_t)1 << 25) || N * K <= (int64_t)1 << 24;
     if (narrow && M <= 32 && (!workspace || small)) return ScaledPlan{0, 0, 0, true};
-    // What the choices take, in microseconds, as fitted.  A round of 256 tiles of 128 x 256 takes 7 and 0.9 for a block of the contraction, one of 256 x 256, which
-    // reads less for what it computes, 9 and 1.55; with few of the CUs at work a block takes 0.7 and 1.1.  128 and 256 rows: 2048 x 4096 x 4096 35.8 and 42.1,
-    // 1000 x 4096 x 14336 94 and 126, 509 x 16384 x 2048 21.7 and 27.6 (one round each); 2500 x 4608 x 2048 37.8 and 29.3 (two and one); 8192 x 16384 x 2048
-    // 342 (by the formula) and 272; 1039 x 14336 x 4096 69.6 and 102 (two and 1.1).
+    // What the choices take, in microseconds, as fitted.  A round of 256 tiles of 128 x 256 takes 6 and 0.8 for a block of the contraction, one of 256 x 256, which
+    // reads less for what it computes, 8 and 1.43; with few of the CUs at work a block takes 0.63 and 1.05.  Tiles of 128 and 256 rows: 1000 x 4096 x 14336 76 and 126,
+    // 1039 x 14336 x 4096 63.9 and 91.3 (two rounds and 1.1), 4608 x 4608 x 4096 85.7 and 91.3; 2500 x 4608 x 2048 37.8 and 31.5, 2048 x 8192 x 4096 63.0 and
+    // 53.4, 8192 x 16384 x 2048 285 and 242.
     const int64_t blocks = (K + 127) / 128, half = ((M + 127) / 128) * ((N + 255) / 256), large = ((M + 255) / 256) * ((N + 255) / 256);
     auto rounds = [blocks](int64_t count, double start, double few, double all) {
         const double rest = (double)(count % 256) / 256;
         return (double)(count / 256) * (start + all * (double)blocks) + (rest > 0 ? start + (few + (all - few) * rest) * (double)blocks : 0);
     };
-    const double t128 = rounds(half, 7, 0.7, 0.9), t256 = rounds(large, 9, 1.1, 1.55);
+    const double t128 = rounds(half, 6, 0.63, 0.8), t256 = rounds(large, 8, 1.05, 1.43);
     const ScaledPlan direct{t128 <= t256 ? 128 : 256, 256, 0, false};
     if (!workspace || blocks == 0) return direct;
     // Partials: a block takes 0.33, 0.36 and 0.5 in tiles of 32, 64 and 128 x 128; partials are written and read at 6.5 TB/s; 9 for two launches.  No more than a
     // workgroup a CU: 215 x 4224 x 10416, 66 tiles in 3 ranges 25.8, in 4 38.1; 33 x 11264 x 2048, 88 tiles in 2 ranges 11.1, in 3 13.4.  Against the
-    // direct tiles: 1821 x 2048 x 8192 47.2 and 56.2, 1000 x 2048 x 5632 24.6 and 41.5, 96 x 2048 x 1024 8.6 and 12.0, 300 x 2048 x 256 7.1 and 7.4 (a launch less
-    // for the host); 614 x 5600 x 1584 23.2 and 19.7.
+    // direct tiles: 1000 x 2048 x 5632 23.9 and 34.6, 300 x 2048 x 2048 12.9 and 16.3, 96 x 2048 x 1024 8.7 and 11.3; 614 x 5600 x 1584 22.9 and 18.8, 300 x 2048 x 256
+    // 7.1 and 7.5 (but a launch less for the host).
     const int bm = M <= 32 ? 32 : (M <= 64 ? 64 : 128);
     const int64_t tiles = ((M + bm - 1) / bm) * ((N + 127) / 128);
     const double stage = bm == 32 ? 0.33 : (bm == 64 ? 0.36 : 0.5), join = (double)M * (double)N * 8 / 6.5e6;
