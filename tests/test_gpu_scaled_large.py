@@ -245,3 +245,69 @@ def test_offsets_past_32_bits_of_gradients(N):
     out = torch.zeros(COLS, N, device="cuda")
     coda.coda_grad_scaled(A, sa, B, sb, out, workspace=torch.empty(need, dtype=torch.uint8, device="cuda") if need else None)
     assert torch.equal(out.cpu().double(), want)
+
+
+# ---------------------------------------------------------------- calls beside each other
+def prepared(M, N, K, seed):
+    o = Operands(M, N, K, True, seed)
+    dev = [t.cuda() for t in (o.a, o.sa, o.b, o.sb)]
+    D = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    return dev, D, coda.coda_gemm_scaled_workspace_bytes(M, N, K)
+
+
+def multiply(dev, D, workspace, stream=None):
+    coda.coda_gemm_scaled(*dev, [coda.store(D)], transB=True, workspace=workspace, stream=stream)
+
+
+def test_two_graphs_take_turns_with_one_workspace():
+    calls = [prepared(96, 1024, 4096, 1), prepared(64, 2048, 2048, 2)]
+    assert all(need for _, _, need in calls)
+    w = torch.empty(max(need for _, _, need in calls), dtype=torch.uint8, device="cuda")
+    once = []
+    for dev, D, _ in calls:
+        multiply(dev, D, w)
+        once.append(D.clone())
+    graphs = []
+    for dev, D, _ in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            multiply(dev, D, w)
+        graphs.append(g)
+    for k in range(4):
+        for _, D, _ in calls:
+            D.zero_()
+        for g in graphs if k % 2 else reversed(graphs):
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(D, want) for (_, D, _), want in zip(calls, once))
+
+
+def test_two_streams_at_once():
+    calls = [prepared(96, 1024, 4096, 1), prepared(64, 2048, 2048, 2), prepared(8, 4096, 2048, 3)]
+    spaces = [torch.empty(need, dtype=torch.uint8, device="cuda") if need else None for _, _, need in calls]
+    once = []
+    for (dev, D, _), w in zip(calls, spaces):
+        multiply(dev, D, w)
+        once.append(D.clone())
+        D.zero_()
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (dev, D, _), w, s in zip(calls, spaces, streams):
+            multiply(dev, D, w, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(D, want) for (_, D, _), want in zip(calls, once))
+
+
+def test_one_operand_twice():
+    """A product of a matrix with itself, and its gradient form: the same codes and scales on both sides."""
+    o = Operands(256, 256, 384, True, 5)
+    a, sa = o.a.cuda(), o.sa.cuda()
+    A = R.decode(o.a) * R.per_element(o.sa, 256, 384)
+    D = torch.empty(256, 256, dtype=torch.bfloat16, device="cuda")
+    coda.coda_gemm_scaled(a, sa, a, sa, [coda.store(D)], transB=True)
+    assert_near(D, A @ A.t(), 1e-3 * (A.square() @ A.square().t()).sqrt(), "A A^T")
+    out = torch.zeros(384, 384, device="cuda")
+    coda.coda_grad_scaled(a, sa, a, sa, out)
+    want = A.t() @ A
+    assert ((out.cpu().double() - want).abs() <= 257 * 2.0 ** -24 * (A.abs().t() @ A.abs())).all() and torch.equal(out, out.t())
