@@ -5,13 +5,13 @@
 namespace coda {
 
 template <class C, bool BKC, int EPI, bool Q8>
-static static hipError_t launch_tile(const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s)
+static hipError_t launch_tile(const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s)
 {
     hipLaunchKernelGGL((gemm_scaled_tile<C, BKC, EPI, Q8>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(C::NT), 0, s, g, q, p);
     return hipGetLastError();
 }
 template <class C, bool BKC>
-static static hipError_t launch_program(int mode, bool q8, const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s)
+static hipError_t launch_program(int mode, bool q8, const GemmParams &g, const Q8Params &q, const ScaledParams &p, hipStream_t s)
 {
     if (q8) {
         if (mode == Q8_LINEAR) return launch_tile<C, BKC, Q8_LINEAR, true>(g, q, p, s);
