@@ -321,6 +321,9 @@ CODA_API coda_status coda_interleave_pairs(void *stream, const coda_mat *Wa, con
  *
  * The scale of a block is the least power of two, and no less than 2^-126, with |x| <= 448 * scale for every finite x of the block;
  * codes are x / scale to the nearest, ties to even.  A NaN or an infinity becomes the code NaN and has no part in the scale.
+ *
+ * Sizes whose launch would come to 2^32 work items or more are CODA_ERR_SHAPE: rows times blocks of 128 columns from 2^30 on in coda_quantize (square
+ * blocks: 2^31), from 2^29 on in coda_dequantize; no product or gradient that fits in memory is that large.
  */
 
 /* X [R x C] bf16 (trans 0, C a multiple of 8) -> codes and scales.  square == 0: blocks of 1 x 128, for activations, gradients and

@@ -58,6 +58,9 @@ coda_status check_vec(const void *p)
     return aligned4(p) ? CODA_OK : CODA_ERR_ALIGN;
 }
 
+// HIP takes fewer than 2^32 work items along a dimension of a launch.
+bool launch_fits(int64_t workgroups, int threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
+
 // An 8-bit tile [M x width]: codes at `p`, scales [ceil(width / 128)][>= M] at `s`.
 coda_status check_scales(const void *s, int64_t ld, int64_t rows)
 {
@@ -583,7 +586,7 @@ coda_status coda_quantize(void *stream, const coda_mat *X, int32_t square, void 
     coda_status st;
     if ((st = check_q8_tile(codes, ld_codes, X->cols, scales, ld_scales, X->rows)) != CODA_OK) return st;
     if (scales_t && (st = check_scales(scales_t, ld_scales_t, X->cols)) != CODA_OK) return st;
-    if ((X->cols + 127) / 128 * ((X->rows + 15) / 16) > INT32_MAX) return CODA_ERR_SHAPE;
+    if (!launch_fits(coda::quantize_workgroups(X->rows, X->cols, square != 0), 256)) return CODA_ERR_SHAPE;
     return launch_status(coda::launch_quantize(static_cast<hipStream_t>(stream), static_cast<const uint16_t *>(X->ptr), X->rows, X->cols, X->ld, square != 0,
                                                static_cast<uint8_t *>(codes), ld_codes, static_cast<uint8_t *>(scales), ld_scales,
                                                static_cast<uint8_t *>(scales_t), ld_scales_t));
@@ -598,7 +601,7 @@ coda_status coda_dequantize(void *stream, const coda_mat *Q, const void *scales,
     coda_status st;
     if ((st = check_q8_tile(Q->ptr, Q->ld, Q->cols, scales, ld_scales, Q->rows)) != CODA_OK) return st;
     if ((st = check_tile(out, ld_out, Q->cols)) != CODA_OK) return st;
-    if ((Q->cols + 127) / 128 * ((Q->rows + 31) / 32) > INT32_MAX) return CODA_ERR_SHAPE;
+    if (!launch_fits(coda::dequantize_workgroups(Q->rows, Q->cols), 256)) return CODA_ERR_SHAPE;
     return launch_status(coda::launch_dequantize(static_cast<hipStream_t>(stream), static_cast<const uint8_t *>(Q->ptr), Q->rows, Q->cols, Q->ld,
                                                  static_cast<const uint8_t *>(scales), ld_scales, static_cast<uint16_t *>(out), ld_out));
 }
@@ -633,7 +636,7 @@ coda_status coda_gemm_scaled(void *stream, int64_t M, int64_t N, int64_t K, cons
         if (workspace_bytes < coda_gemm_scaled_workspace_bytes(M, N, K)) return CODA_ERR_WORKSPACE;
     }
     if (!plan.few && plan.nsplit == 0 && !ps.q8 && ps.mode == coda::EPI_RMSNORM_BWD) plan.bm = coda::TILE_M;      // its column partials are per 256 rows
-    if (!plan.few && ((M + plan.bm - 1) / plan.bm) * ((N + plan.bn - 1) / plan.bn) > INT32_MAX / 16) return CODA_ERR_SHAPE;
+    if (!plan.few && !launch_fits(((M + plan.bm - 1) / plan.bm) * ((N + plan.bn - 1) / plan.bn) * (plan.nsplit ? plan.nsplit : 1), 512)) return CODA_ERR_SHAPE;
     ps.p.M = (int)M;
     ps.p.N = (int)N;
     ps.p.K = (int)K;
@@ -683,7 +686,7 @@ coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_t K, cons
         if (!aligned16(workspace)) return CODA_ERR_ALIGN;
         if (workspace_bytes < coda::grad_bytes(plan, M, N)) return CODA_ERR_WORKSPACE;
     }
-    if (((M + plan.tile - 1) / plan.tile) * ((N + plan.tile - 1) / plan.tile) > INT32_MAX / 16) return CODA_ERR_SHAPE;
+    if (!launch_fits(((M + plan.tile - 1) / plan.tile) * ((N + plan.tile - 1) / plan.tile) * plan.nsplit, plan.tile * 2)) return CODA_ERR_SHAPE;
     coda::GemmParams g{};
     g.M = (int)M;
     g.N = (int)N;

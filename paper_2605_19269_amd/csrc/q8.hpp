@@ -56,6 +56,16 @@ __device__ __forceinline__ float q8_largest(F each)
     return m;
 }
 
+// Workgroups, of 256, that the launches below come to
+constexpr int QUANTIZE_PASSES = 4, RESTORE_PASSES = 2;
+inline int64_t quantize_workgroups(int64_t R, int64_t C, bool square)
+{
+    const int64_t cb = (C + Q8_BLOCK - 1) / Q8_BLOCK;
+    if (square) return cb * ((R + Q8_BLOCK - 1) / Q8_BLOCK);
+    return R * cb <= 64 * 1024 ? cb * ((R + 15) / 16) : cb * ((R + 16 * QUANTIZE_PASSES - 1) / (16 * QUANTIZE_PASSES));
+}
+inline int64_t dequantize_workgroups(int64_t R, int64_t C) { return (C + Q8_BLOCK - 1) / Q8_BLOCK * ((R + 16 * RESTORE_PASSES - 1) / (16 * RESTORE_PASSES)); }
+
 hipError_t launch_quantize(hipStream_t s, const uint16_t *X, int64_t R, int64_t C, int64_t ld, bool square, uint8_t *q, int64_t ldq, uint8_t *sc,
                            int64_t lds, uint8_t *sct, int64_t ldst);
 hipError_t launch_dequantize(hipStream_t s, const uint8_t *q, int64_t R, int64_t C, int64_t ldq, const uint8_t *sc, int64_t lds, uint16_t *out,

@@ -138,7 +138,6 @@ __global__ __launch_bounds__(256) void quantize_square_kernel(const uint16_t *__
 // Codes -> bf16: sixteen lanes a row of a block, eight codes a lane, so that a store covers whole lines (sixteen codes a lane, two stores at a stride: 16384 x 4096
 // 47.9 us, 38.0 as here).  Every value is a bf16 value (E4M3 has three bits behind the point) unless it lies below 2^-133.  Plain stores: past the caches the kernel
 // alone takes 30.7 us, but with a reader of its output behind it 64.1 instead of 54.0 (and quantising 30.8 instead of 36.0, with a product behind it 254 and 247).
-constexpr int RESTORE_PASSES = 2;
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *__restrict__ q, int64_t R, int64_t C, int64_t ldq, int cblocks,
                                                          const uint8_t *__restrict__ sc, int64_t lds, uint16_t *__restrict__ out, int64_t ld_out)
 {
@@ -176,13 +175,10 @@ hipError_t launch_quantize(hipStream_t s, const uint16_t *X, int64_t R, int64_t 
                            int64_t lds, uint8_t *sct, int64_t ldst)
 {
     const int cb = (int)((C + Q8_BLOCK - 1) / Q8_BLOCK);
-    if (square)
-        hipLaunchKernelGGL(quantize_square_kernel, dim3((unsigned)(cb * ((R + Q8_BLOCK - 1) / Q8_BLOCK))), dim3(256), 0, s, X, R, C, ld, cb, q, ldq, sc,
-                           lds, sct, ldst);
-    else if (R * cb <= 64 * 1024)
-        hipLaunchKernelGGL((quantize_rows_kernel<1>), dim3((unsigned)(cb * ((R + 15) / 16))), dim3(256), 0, s, X, R, C, ld, cb, q, ldq, sc, lds);
-    else
-        hipLaunchKernelGGL((quantize_rows_kernel<4>), dim3((unsigned)(cb * ((R + 63) / 64))), dim3(256), 0, s, X, R, C, ld, cb, q, ldq, sc, lds);
+    const dim3 grid((unsigned)quantize_workgroups(R, C, square));
+    if (square) hipLaunchKernelGGL(quantize_square_kernel, grid, dim3(256), 0, s, X, R, C, ld, cb, q, ldq, sc, lds, sct, ldst);
+    else if (R * cb <= 64 * 1024) hipLaunchKernelGGL((quantize_rows_kernel<1>), grid, dim3(256), 0, s, X, R, C, ld, cb, q, ldq, sc, lds);
+    else hipLaunchKernelGGL((quantize_rows_kernel<QUANTIZE_PASSES>), grid, dim3(256), 0, s, X, R, C, ld, cb, q, ldq, sc, lds);
     return hipGetLastError();
 }
 
@@ -190,8 +186,7 @@ hipError_t launch_dequantize(hipStream_t s, const uint8_t *q, int64_t R, int64_t
                              int64_t ld_out)
 {
     const int cb = (int)((C + Q8_BLOCK - 1) / Q8_BLOCK);
-    constexpr int rows = 16 * RESTORE_PASSES;
-    hipLaunchKernelGGL(dequantize_kernel, dim3((unsigned)(cb * ((R + rows - 1) / rows))), dim3(256), 0, s, q, R, C, ldq, cb, sc, lds, out, ld_out);
+    hipLaunchKernelGGL(dequantize_kernel, dim3((unsigned)dequantize_workgroups(R, C)), dim3(256), 0, s, q, R, C, ldq, cb, sc, lds, out, ld_out);
     return hipGetLastError();
 }
 
