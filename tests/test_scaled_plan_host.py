@@ -1,0 +1,86 @@
+"""Host checks of the plans of the 8-bit products with block scales and of their gradients: which kernels the GPU tests of these operators reach, and where
+the plans draw their lines (sizes at which both sides were timed)."""
+import pytest
+
+from tests import scaled_plan as S
+from tests import test_gpu_scaled as T
+from tests import test_gpu_scaled_large as L
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    return S.load(tmp_path_factory.mktemp("scaled_plan"))
+
+
+def test_shapes_of_the_large_tile_tests_have_large_tiles(lib):
+    for shape in L.LARGE + [(2064, 4112, 400), (2304, 4096, 640), (2064, 4128, 400)]:
+        assert S.product(lib, *shape, workspace=False) == "256x256", shape
+
+
+def test_shapes_of_the_few_row_tests_are_one_kernel(lib):
+    for shape in L.FEW + [(1, 6144, 1024), (9, 528, 400), (30, 4224, 528)]:
+        for ws in (False, True):
+            assert S.product(lib, *shape, workspace=ws, narrow=True) == "few", shape
+
+
+def test_plain_and_8_bit_shapes_without_a_workspace_have_half_tiles(lib):
+    for shape in T.SHAPES + T.Q8_SHAPES:
+        assert S.product(lib, *shape, workspace=False) == "128x256", shape
+
+
+# divided shapes among those of the plain tests: 32, 64 and 128 rows
+@pytest.mark.parametrize("shape,plan", [((1, 272, 4096), ("32x128", 16)), ((33, 528, 1040), ("64x128", 9)), ((64, 1024, 2048), ("64x128", 8)),
+                                        ((65, 272, 784), ("128x128", 7)), ((257, 512, 1168), ("128x128", 5)), ((300, 784, 2064), ("128x128", 6)),
+                                        ((1, 512, 4096), ("32x128", 16))])
+def test_shapes_that_are_divided(lib, shape, plan):
+    assert shape in T.SHAPES + T.Q8_SHAPES
+    assert S.product(lib, *shape, workspace=True) == plan
+
+
+# gradients of the GPU tests: undivided 128 x 128, divided, 256 x 256
+@pytest.mark.parametrize("shape,plan", [((16, 16, 1), (128, 1)), ((400, 144, 1000), (128, 4)), ((2048, 4096, 70), (128, 1)), ((2048, 4096, 320), (256, 1)),
+                                        ((2064, 4112, 333), (256, 1)), ((4112, 2064, 1000), (256, 1)), ((2048, 4096, 257), (256, 1)), ((16384, 16, 140016), (128, 4)),
+                                        ((16384, 528, 140016), (256, 1))])
+def test_tiles_of_gradients(lib, shape, plan):
+    assert S.gradient(lib, *shape, workspace=True) == plan and S.gradient(lib, *shape, workspace=False) == (plan[0], 1)
+
+
+# without a workspace (microseconds: 128 x 256 tiles, 256 x 256 tiles)
+@pytest.mark.parametrize("shape,tile", [((1000, 4096, 14336), "128x256"),          # 76, 126
+                                        ((1039, 14336, 4096), "128x256"),          # 63.9, 91.3
+                                        ((4608, 4608, 4096), "128x256"),           # 85.7, 91.3
+                                        ((2500, 4608, 2048), "256x256"),           # 37.8, 31.5
+                                        ((2048, 8192, 4096), "256x256"),           # 63.0, 53.4
+                                        ((8192, 16384, 2048), "256x256")])         # 285, 242
+def test_tiles_where_they_are_faster(lib, shape, tile):
+    assert S.product(lib, *shape, workspace=False) == tile
+
+
+# with one (microseconds: divided, one kernel)
+@pytest.mark.parametrize("shape,plan", [((215, 4224, 10416), ("128x128", 3)),      # 25.8 (4 ranges: 38.1)
+                                        ((33, 11264, 2048), ("64x128", 2)),        # 11.1 (3 ranges: 13.4)
+                                        ((1000, 2048, 5632), ("128x128", 2)),      # 23.9, 34.6
+                                        ((300, 2048, 2048), ("128x128", 4)),       # 12.9, 16.3
+                                        ((96, 2048, 1024), ("128x128", 4)),        # 8.7, 11.3
+                                        ((614, 5600, 1584), "128x256"),            # 22.9, 18.8
+                                        ((300, 2048, 256), "128x256")])            # 7.1, 7.5
+def test_ranges_where_they_are_faster(lib, shape, plan):
+    assert S.product(lib, *shape, workspace=True) == plan
+
+
+# one kernel for few rows where it was the faster, partials where they were
+@pytest.mark.parametrize("shape,few", [((1, 6144, 4096), True), ((8, 6144, 4096), True), ((16, 6144, 4096), True), ((32, 6144, 4096), False),
+                                       ((1, 4096, 14336), True), ((8, 4096, 14336), True), ((24, 4096, 14336), False), ((1, 16384, 2048), True),
+                                       ((24, 4096, 4096), True), ((1, 28672, 4096), False)])
+def test_few_rows_where_one_kernel_is_faster(lib, shape, few):
+    assert (S.product(lib, *shape, workspace=True, narrow=True) == "few") == few
+
+
+# M, N, tokens (microseconds: 256 x 256 tiles, 128 x 128 tiles, in ranges)
+@pytest.mark.parametrize("shape,plan", [((2048, 16384, 8192), (256, 1)),           # 477, 647
+                                        ((5632, 2048, 1000), (256, 1)),            # 43.4, 46.7
+                                        ((4096, 14336, 256), (128, 1)),            # 127, 121
+                                        ((2048, 8192, 64), (128, 1)),              # 26.3, 25.5
+                                        ((512, 1024, 8192), (128, 16))])           # undivided 208, 26.0
+def test_gradient_tiles_where_they_are_faster(lib, shape, plan):
+    assert S.gradient(lib, *shape, workspace=True) == plan
