@@ -5,6 +5,7 @@ import pytest
 from tests import scaled_plan as S
 from tests import test_gpu_scaled as T
 from tests import test_gpu_scaled_large as L
+from tests import test_gpu_scaled_programs as P
 
 
 @pytest.fixture(scope="module")
@@ -35,6 +36,13 @@ def test_plain_and_8_bit_shapes_without_a_workspace_have_half_tiles(lib):
 def test_shapes_that_are_divided(lib, shape, plan):
     assert shape in T.SHAPES + T.Q8_SHAPES
     assert S.product(lib, *shape, workspace=True) == plan
+
+
+# where the tests of every program take partials
+@pytest.mark.parametrize("shape,tile", zip(P.DIVIDED, ["32x128", "64x128", "128x128", "128x128"]))
+def test_divided_shapes_of_the_program_tests(lib, shape, tile):
+    plan = S.product(lib, *shape, workspace=True)
+    assert plan[0] == tile and plan[1] > 1 and shape[0] % 4 and shape[1] % 256
 
 
 # gradients of the GPU tests: undivided 128 x 128, divided, 256 x 256
