@@ -15,7 +15,11 @@ pytestmark = pytest.mark.gpu
 # block of 128 and inside the wave's columns
 DIVIDED = [(5, 288, 4096), (33, 288, 3088), (70, 544, 2064), (257, 800, 2576)]
 
-SHAPES = [s + (True,) for s in DIVIDED]
+# Undivided: 128 x 256 tiles; 256 x 256 tiles, ragged and whole (instances of their own)
+HALF = [(300, 800, 400), (256, 512, 256)]
+LARGE = [(2064, 4128, 400), (2304, 4096, 640)]
+
+SHAPES = [s + (True,) for s in DIVIDED] + [s + (False,) for s in HALF + LARGE]
 
 
 @pytest.fixture(params=[(s, t) for s in SHAPES for t in (True, False)], ids=lambda p: "%dx%dx%d-%s-%s" % (p[0][:3] + ("ws" if p[0][3] else "none", "NK" if p[1] else "KN")))

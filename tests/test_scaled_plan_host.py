@@ -45,6 +45,13 @@ def test_divided_shapes_of_the_program_tests(lib, shape, tile):
     assert plan[0] == tile and plan[1] > 1 and shape[0] % 4 and shape[1] % 256
 
 
+def test_undivided_shapes_of_the_program_tests(lib):
+    for shapes, tile in ((P.HALF, "128x256"), (P.LARGE, "256x256")):
+        for shape in shapes:
+            assert S.product(lib, *shape, workspace=False) == tile
+    assert any(M % 256 == N % 256 == K % 128 == 0 for M, N, K in P.LARGE) and any(M % 256 and N % 256 and K % 128 for M, N, K in P.LARGE)
+
+
 # gradients of the GPU tests: undivided 128 x 128, divided, 256 x 256
 @pytest.mark.parametrize("shape,plan", [((16, 16, 1), (128, 1)), ((400, 144, 1000), (128, 4)), ((2048, 4096, 70), (128, 1)), ((2048, 4096, 320), (256, 1)),
                                         ((2064, 4112, 333), (256, 1)), ((4112, 2064, 1000), (256, 1)), ((2048, 4096, 257), (256, 1)), ((16384, 16, 140016), (128, 4)),
