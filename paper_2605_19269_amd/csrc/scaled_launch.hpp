@@ -94,15 +94,18 @@ template <> hipError_t launch_scaled_128<false>(int, bool, const GemmParams &, c
 // tile x tile of a gradient, and ranges of its tokens (1: G is added to by the tiles' own kernel).
 // 256: one workgroup a CU, bound by the matrix cores and LDS.  128: two a CU, four waves of 64 x 64, which read a third more from LDS for what they
 // compute but fill the chip with a quarter of the output, end a tile while the other computes, and need fewer partials where the tokens
-// are divided.  8192 x (2048 x 16384) 477 us against 647, 1000 x (5632 x 2048) 43.4 / 46.7; 256 x (4096 x 14336) 127 / 121, 64 x (2048 x 8192) 26.3 / 25.5;
-// with few tiles, in ranges: 8192 x (512 x 1024) 208 undivided / 26.0, 300 x (4800 x 752) 21.2 / 12.0, 2048 x (2048 x 2048) 63 / 37.5.
+// are divided.  So 128 up to the 512 tiles of one round of them, and where there is little to contract (us, 256 / 128): 512 tiles, 1000 x (2048 x 4096) 39.6 / 30.6,
+// 4096 x (2048 x 4096) 114 / 86, 320 x (1024 x 8192) 22.9 / 18.6; 544 and more, 1000 x (256 x 34816) 40.1 / 45.0, 4096 x (2304 x 4096) 114 / 137, 320 x (2304 x 4096)
+// 23.8 / 24.3, 1000 x (5632 x 2048) 43.6 / 48.8, 4096 x (4096 x 4096) 127 / 157, 8192 x (2048 x 16384) 470 / 608; few tokens, 256 x (4096 x 14336) 126 / 115,
+// 64 x (4096 x 14336) 107 / 102, 64 x (2048 x 8192) 25.2 / 26.3.  With few tiles, in ranges: 8192 x (512 x 1024) 208 / 116, in 16 ranges 26.9;
+// 300 x (4800 x 752) 21.4 / 12.1, 2048 x (2048 x 2048) 62 / 38.5.
 struct GradPlan {
     int tile, nsplit;
 };
 inline GradPlan plan_grad(int64_t M, int64_t N, int64_t K, bool workspace)
 {
-    const int64_t large = ((M + 255) / 256) * ((N + 255) / 256), small = ((M + 127) / 128) * ((N + 127) / 128), stages = (K + 63) / 64;
-    if (large >= 128 && K > 256) return GradPlan{256, 1};
+    const int64_t small = ((M + 127) / 128) * ((N + 127) / 128), stages = (K + 63) / 64;
+    if (small > 512 && K > 256) return GradPlan{256, 1};
     int64_t n = workspace && small > 0 && small < 256 ? 512 / small : 1;
     if (n > 16) n = 16;
     if (n > stages / 4) n = stages / 4;

@@ -53,9 +53,9 @@ def test_undivided_shapes_of_the_program_tests(lib):
 
 
 # gradients of the GPU tests: undivided 128 x 128, divided, 256 x 256
-@pytest.mark.parametrize("shape,plan", [((16, 16, 1), (128, 1)), ((400, 144, 1000), (128, 4)), ((2048, 4096, 70), (128, 1)), ((2048, 4096, 320), (256, 1)),
-                                        ((2064, 4112, 333), (256, 1)), ((4112, 2064, 1000), (256, 1)), ((2048, 4096, 257), (256, 1)), ((16384, 16, 140016), (128, 4)),
-                                        ((16384, 528, 140016), (256, 1))])
+@pytest.mark.parametrize("shape,plan", [((16, 16, 1), (128, 1)), ((400, 144, 1000), (128, 4)), ((2048, 4096, 70), (128, 1)), ((2064, 4112, 333), (256, 1)),
+                                        ((4112, 2064, 1000), (256, 1)), ((4096, 4096, 320), (256, 1)), ((4096, 4096, 257), (256, 1)), ((4096, 4104, 320), (256, 1)),
+                                        ((16384, 16, 140016), (128, 4)), ((16384, 528, 140016), (256, 1))])
 def test_tiles_of_gradients(lib, shape, plan):
     assert S.gradient(lib, *shape, workspace=True) == plan and S.gradient(lib, *shape, workspace=False) == (plan[0], 1)
 
@@ -91,11 +91,28 @@ def test_few_rows_where_one_kernel_is_faster(lib, shape, few):
     assert (S.product(lib, *shape, workspace=True, narrow=True) == "few") == few
 
 
-# M, N, tokens (microseconds: 256 x 256 tiles, 128 x 128 tiles, in ranges)
-@pytest.mark.parametrize("shape,plan", [((2048, 16384, 8192), (256, 1)),           # 477, 647
-                                        ((5632, 2048, 1000), (256, 1)),            # 43.4, 46.7
-                                        ((4096, 14336, 256), (128, 1)),            # 127, 121
-                                        ((2048, 8192, 64), (128, 1)),              # 26.3, 25.5
-                                        ((512, 1024, 8192), (128, 16))])           # undivided 208, 26.0
-def test_gradient_tiles_where_they_are_faster(lib, shape, plan):
-    assert S.gradient(lib, *shape, workspace=True) == plan
+# M, N, tokens (microseconds: 256 x 256 tiles, 128 x 128 tiles)
+@pytest.mark.parametrize("shape,tile", [((2048, 4096, 320), 128),            # 22.9, 18.7: 512 tiles of 128 x 128, one round
+                                        ((2048, 4096, 1000), 128),           # 39.6, 30.6
+                                        ((2048, 4096, 4096), 128),           # 114, 86
+                                        ((1024, 8192, 320), 128),            # 22.9, 18.6
+                                        ((256, 32768, 4096), 128),           # 114, 86
+                                        ((256, 34816, 1000), 256),           # 40.1, 45.0: 544
+                                        ((2304, 4096, 320), 256),            # 23.8, 24.3
+                                        ((2304, 4096, 4096), 256),           # 114, 137
+                                        ((5632, 2048, 1000), 256),           # 43.6, 48.8
+                                        ((4096, 4096, 4096), 256),           # 127, 157
+                                        ((2048, 16384, 8192), 256),          # 470, 608
+                                        ((4096, 14336, 256), 128),           # 126, 115
+                                        ((4096, 14336, 64), 128),            # 107, 102
+                                        ((2048, 2048, 2048), 128)])          # 62, 38.5
+def test_gradient_tiles_where_they_are_faster(lib, shape, tile):
+    assert S.gradient(lib, *shape, workspace=True) == S.gradient(lib, *shape, workspace=False) == (tile, 1)
+
+
+def test_gradient_of_few_tiles_in_ranges(lib):
+    assert S.gradient(lib, 512, 1024, 8192, workspace=True) == (128, 16)            # 26.9, undivided 116
+    assert S.gradient(lib, 400, 144, 1000, workspace=True) == (128, 4)              # 10.1, 18.4
+    for M, N, K in ((16, 32528, 1000), (16, 32768, 1000), (128, 65536, 1000)):      # one row of tiles: no more than a round of them
+        tile, ranges = S.gradient(lib, M, N, K, workspace=True)
+        assert tile == 128 and -(-M // 128) * -(-N // 128) * ranges <= 512
