@@ -240,7 +240,7 @@ __device__ __forceinline__ void scaled_contract(Acc32<C> &acc, const ScaledParam
 // phases before; those of the lower rows of T, one phase before, are waited for in the phase that issues them (even M2).
 // Scales come for four pairs at once, a load of 256 bytes from every wave: two waves that fetched them for every pair, under a mask and out
 // of step with the others, cost 5 %.
-// 16384 x 4096 x 28672, B [K x N]: 1394 us, 2.76 PFLOP/s (unscaled 8-bit operands 1304).  Four waves of 256 x 64 with two whole slots: 1750 (their loads are in flight for half to one
+// 16384 x 4096 x 28672, B [K x N]: 1376 us, 2.80 PFLOP/s (unscaled 8-bit operands, in turn with it, 1276).  Four waves of 256 x 64 with two whole slots: 1750 (their loads are in flight for half to one
 // stage, which is less than what memory takes, and one wave on a SIMD has no other to compute while it issues them).
 // ---------------------------------------------------------------------------------
 struct ScaledLargeCfg : DlCfg<256, 256, 2, 4, 4> {

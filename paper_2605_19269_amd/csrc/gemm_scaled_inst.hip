@@ -36,7 +36,8 @@ hipError_t launch_gemm_scaled(const ScaledPlan &pl, int mode, bool q8, bool bkc,
 {
     ScaledParams p = p_in;
     if (pl.few) {
-        // 32 columns a workgroup where that leaves one for more than half of the CUs (6144 x 4096, one row: 7.2 us, 16 columns 8.2; 4096 x 14336: 17.1, 12.3)
+        // 32 columns a workgroup where that leaves one for more than half of the CUs (us, 16 and 32 columns: one row of K = 4096, N = 4096 5.9 and 7.1, 4112 7.1 and 7.1,
+        // 4608 7.6 and 7.2, 6144 8.2 and 7.4, 8192 9.4 and 8.7; 16 rows, 4096 6.7 and 8.3, 4608 10.3 and 8.4; 32 rows of K = 2048, 4096 5.4 and 6.3, 4608 9.1 and 6.5)
         const int cb = p.N > 4096 ? 2 : 1;
         if (p.M <= 16) return cb == 2 ? launch_few<1, 2>(mode, g, p, s) : launch_few<1, 1>(mode, g, p, s);
         return cb == 2 ? launch_few<2, 2>(mode, g, p, s) : launch_few<2, 1>(mode, g, p, s);

@@ -39,16 +39,16 @@ struct ScaledPlan {
 // `narrow`: a program without row reductions and 8-bit outputs, on a B stored [N x K]
 inline ScaledPlan plan_scaled(int64_t M, int64_t N, int64_t K, bool workspace, bool narrow)
 {
-    // Against partials and a second kernel (us): 6144 x 4096, 1 / 8 / 16 / 32 rows 7.2 / 7.8 / 8.7 / 10.5 and 9.6 / 9.7 / 9.9 / 10.1; 4096 x 14336, 1 / 8 / 24 rows
-    // 12.3 / 13.2 / 20.2 and 13.2 / 13.6 / 14.2; 16384 x 2048, one row 9.5 and 10.1; 4096 x 4096, 24 rows 8.4 and 9.0; 28672 x 4096, one row 27 and 20.7 (many
+    // Against partials and a second kernel (us): 6144 x 4096, 1 / 8 / 16 / 32 rows 7.6 / 8.1 / 8.7 / 10.6 and 9.2 / 9.5 / 9.9 / 10.9; 4096 x 14336, 1 / 8 / 24 rows
+    // 12.5 / 13.4 / 19.7 and 13.4 / 13.8 / 14.2; 16384 x 2048, one row 9.6 and 10.1; 4096 x 4096, 24 rows 8.0 and 9.5; 28672 x 4096, one row 27.4 and 21.0 (many
     // workgroups one after the other, each with its own start; every one fetches the rows of A anew).  Without a workspace against 128-row tiles: 4096 x 14336,
-    // 32 rows 23 and 95.
+    // 32 rows 22.6 and 72.8.
     const bool small = (M <= 8 && N <= 8192) || (M <= 16 && N * K <= (int64_t)1 << 25) || N * K <= (int64_t)1 << 24;
     if (narrow && M <= 32 && (!workspace || small)) return ScaledPlan{0, 0, 0, true};
     // What the choices take, in microseconds, as fitted.  A round of 256 tiles of 128 x 256 takes 6 and 0.8 for a block of the contraction, one of 256 x 256, which
-    // reads less for what it computes, 8 and 1.43; with few of the CUs at work a block takes 0.63 and 1.05.  Tiles of 128 and 256 rows: 1000 x 4096 x 14336 76 and 126,
-    // 1039 x 14336 x 4096 63.9 and 91.3 (two rounds and 1.1), 4608 x 4608 x 4096 85.7 and 91.3; 2500 x 4608 x 2048 37.8 and 31.5, 2048 x 8192 x 4096 63.0 and
-    // 53.4, 8192 x 16384 x 2048 285 and 242.
+    // reads less for what it computes, 8 and 1.43; with few of the CUs at work a block takes 0.63 and 1.05.  Tiles of 128 and 256 rows: 1000 x 4096 x 14336 78 and 126,
+    // 1039 x 14336 x 4096 66 and 95 (two rounds and 1.1), 2048 x 4096 x 4096 34.5 and 45.4, 4608 x 4608 x 4096 92 and 95; 2500 x 4608 x 2048 35.7 and 30.8,
+    // 2048 x 8192 x 4096 66 and 56, 8192 x 16384 x 2048 300 and 254.
     const int64_t blocks = (K + 127) / 128, half = ((M + 127) / 128) * ((N + 255) / 256), large = ((M + 255) / 256) * ((N + 255) / 256);
     auto rounds = [blocks](int64_t count, double start, double few, double all) {
         const double rest = (double)(count % 256) / 256;
@@ -58,9 +58,9 @@ inline ScaledPlan plan_scaled(int64_t M, int64_t N, int64_t K, bool workspace, b
     const ScaledPlan direct{t128 <= t256 ? 128 : 256, 256, 0, false};
     if (!workspace || blocks == 0) return direct;
     // Partials: a block takes 0.33, 0.36 and 0.5 in tiles of 32, 64 and 128 x 128; partials are written and read at 6.5 TB/s; 9 for two launches.  No more than a
-    // workgroup a CU: 215 x 4224 x 10416, 66 tiles in 3 ranges 25.8, in 4 38.1; 33 x 11264 x 2048, 88 tiles in 2 ranges 11.1, in 3 13.4.  Against the
-    // direct tiles: 1000 x 2048 x 5632 23.9 and 34.6, 300 x 2048 x 2048 12.9 and 16.3, 96 x 2048 x 1024 8.7 and 11.3; 614 x 5600 x 1584 22.9 and 18.8, 300 x 2048 x 256
-    // 7.1 and 7.5 (but a launch less for the host).
+    // workgroup a CU: 215 x 4224 x 10416, 66 tiles in 3 ranges 26.4, in 4 38.3; 33 x 11264 x 2048, 88 tiles in 2 ranges 10.9, in 3 12.9.  Against the
+    // direct tiles: 1000 x 2048 x 5632 24.8 and 33.9, 300 x 2048 x 2048 14.3 and 16.1, 96 x 2048 x 1024 8.7 and 11.4; 614 x 5600 x 1584 23.0 and 18.7.  Level:
+    // 300 x 2048 x 256 7.1 and 7.4 (direct: a launch less for the host), 1000 x 4096 x 14336 in one range, 256 tiles for 128, 77.1 and 77.8 (partials).
     const int bm = M <= 32 ? 32 : (M <= 64 ? 64 : 128);
     const int64_t tiles = ((M + bm - 1) / bm) * ((N + 127) / 128);
     const double stage = bm == 32 ? 0.33 : (bm == 64 ? 0.36 : 0.5), join = (double)M * (double)N * 8 / 6.5e6;
