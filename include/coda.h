@@ -375,6 +375,85 @@ CODA_API coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_
                              size_t workspace_bytes);
 CODA_API size_t coda_grad_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
+/*
+ * Attention, the step between the QKV projection (ROW_SCALE, ROPE, STORE) and the output projection.
+ *
+ * Q is bf16 [Tq x heads * D] and K, V are [Tk x kv_heads * D], one row a token, head h in columns h * D ..; they may be column blocks of one
+ * QKV matrix.  D, the head dimension, is Q->cols / heads: a multiple of 8, at most 128.  heads is a multiple of kv_heads, and query heads
+ * h * heads / kv_heads .. read key / value head h.  Sequences are packed: seq_q is int32 [n_seqs + 1] (device), sequence s has rows seq_q[s] ..
+ * seq_q[s + 1] - 1 of Q, and seq_k says the same for K and V (NULL: seq_q, with Tk == Tq).  Offsets do not decrease; they are read on the
+ * device, so that a captured graph serves other lengths, and taken between 0 and the number of rows there, whatever they hold.  Rows of
+ * outputs that belong to no sequence are left as they are.
+ *
+ *     S_ij = scale * q_i . k_j       lse_i = log sum_j exp S_ij       out_i = sum_j exp(S_ij - lse_i) v_j
+ *
+ * over the keys j of row i's sequence, with causal != 0 those up to j = i + keys - rows (both counted from the sequence's start: the last row
+ * sees all keys).  A row that sees no key is zeros with lse = -inf.  What a row does not see has no effect on it, infinities and NaN included.
+ * lse (natural logarithm): f32 [heads x Tq], may be NULL.  scale is positive and finite (CODA_ERR_SHAPE).
+ *
+ * Products are exact, sums, maxima and lse in fp32; the weights exp(S - max) are rounded to bf16 for their product with V (error of an output: about that of one
+ * rounding to bf16 again), their sum is taken before.  The order of additions depends on the sizes only.
+ */
+CODA_API coda_status coda_attention(void *stream, const coda_mat *Q, const coda_mat *K, const coda_mat *V, const int32_t *seq_q, const int32_t *seq_k,
+                           int32_t n_seqs, int32_t heads, int32_t kv_heads, float scale, int32_t causal, void *out, int64_t ld_out, float *lse);
+
+/* The rotation that the ROPE epilogue gave Q and K: the tables and positions handed to it. */
+typedef struct coda_rope {
+    const float *cos, *sin;             /* f32 [rows x D / 2], 8-byte aligned; rows * D / 2 < 2^31 */
+    const int32_t *pos_q, *pos_k;       /* int32 [Tq], [Tk]; taken to the nearest table row */
+    int64_t rows;
+} coda_rope;
+
+/*
+ * Backward pass of coda_attention.  O and lse are its outputs, dO the gradient of O (all [Tq x heads * D]).  With P = exp(S - lse) and
+ * delta_i = sum_d dO_id O_id:
+ *     dV_j = sum_i P_ij dO_i      dS_ij = P_ij (dO_i . v_j - delta_i)      dQ_i = scale sum_j dS_ij k_j      dK_j = scale sum_i dS_ij q_i
+ * dK and dV are summed over the query heads of their group.  rope (host, may be NULL): dQ and dK are turned back, i.e. are the gradients of
+ * the QKV projection's outputs before its ROPE epilogue (pairs of columns of all D; D a multiple of 8 as there).
+ * dQ, dK, dV: bf16 of the shapes of Q, K, V, overwritten; they may be column blocks of one matrix.  Rows of no sequence are left as they are; a key
+ * that no row sees has gradients of zero.  P and dS are rounded to bf16 for their products, sums are fp32; the order of additions depends on the
+ * sizes only (no atomics).  A row of dO that is not finite makes NaN or infinities of what it reaches, and of nothing else.
+ * workspace: device memory, 16-byte aligned, coda_attention_bwd_workspace_bytes(...) bytes (CODA_ERR_WORKSPACE below that); it holds nothing
+ * between calls, and two calls that share one must not overlap in time.
+ */
+CODA_API coda_status coda_attention_bwd(void *stream, const coda_mat *Q, const coda_mat *K, const coda_mat *V, const coda_mat *O, const coda_mat *dO,
+                               const float *lse, const int32_t *seq_q, const int32_t *seq_k, int32_t n_seqs, int32_t heads, int32_t kv_heads,
+                               float scale, int32_t causal, const coda_rope *rope /* host */, void *dQ, int64_t ld_dq, void *dK, int64_t ld_dk,
+                               void *dV, int64_t ld_dv, void *workspace, size_t workspace_bytes);
+CODA_API size_t coda_attention_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seqs, int32_t heads, int32_t kv_heads, int32_t head_dim);
+
+/*
+ * A paged cache of keys and values: k and v are bf16 [pages][kv_heads][page][head_dim], dense, 16-byte aligned.  page, the keys of a page, is a power of
+ * two; head_dim as above; pages * page < 2^31.  Slot page * p + i is place i of page p.
+ */
+typedef struct coda_cache {
+    void *k, *v;                        /* device */
+    int64_t pages;
+    int32_t page, kv_heads, head_dim;
+} coda_cache;
+
+/* Rows of K and V [T x kv_heads * head_dim] into the cache: row t to slot slots[t] (int32 [T], device).  A slot that is not one of the cache's
+   (-1 for a row that is not kept, such as padding or a draft that was turned down) stores nothing.  The slots of one call differ from each other. */
+CODA_API coda_status coda_cache_store(void *stream, const coda_mat *K, const coda_mat *V, const int32_t *slots, const coda_cache *cache /* host */);
+
+/*
+ * Attention of new tokens over the cache, as coda_attention: single tokens, chains of them (a part of a prompt) or trees of drafted tokens.  Sequence s has lens[s]
+ * keys (int32 [n_seqs], device), key j at place j % page of page table[s * ld_table + j / page] (int32, device; table_pages entries a
+ * sequence), and rows seq_q[s] .. seq_q[s + 1] - 1 of Q.  The last of its keys are those of its rows, in their order (coda_cache_store comes first).
+ * Row i sees all keys before those, and key j of them if j <= i, or, with tree (uint64 [Tq], device; NULL for none), where bit j of the row's tree is
+ * set; with a tree, rows and bits from 64 on have no key of their own.  Where lens[s] is below the number of rows the keys are those of the last rows.
+ * lens are taken between 0 and table_pages * page and entries of the table to the nearest page, whatever they hold; entries behind a sequence's keys are
+ * not read, nor are places of the last page behind them.
+ *
+ * The keys of all sequences, laid end to end, are cut into equal ranges, a workgroup each, whatever the lengths; where a range ends within a
+ * sequence, partial results in the workspace are joined by a second kernel in their order.  workspace: as above,
+ * coda_attention_cached_workspace_bytes(...) bytes.  The order of additions depends on the sizes and on lens and seq_q.
+ */
+CODA_API coda_status coda_attention_cached(void *stream, const coda_mat *Q, const coda_cache *cache /* host */, const int32_t *table, int64_t ld_table,
+                                  int64_t table_pages, const int32_t *lens, const int32_t *seq_q, int32_t n_seqs, int32_t heads, float scale,
+                                  const uint64_t *tree, void *out, int64_t ld_out, float *lse, void *workspace, size_t workspace_bytes);
+CODA_API size_t coda_attention_cached_workspace_bytes(int64_t Tq, int32_t n_seqs, int32_t heads, int32_t kv_heads, int32_t head_dim);
+
 CODA_API const char *coda_status_string(coda_status s);
 /* The hipError_t (as int) recorded by the most recent CODA_ERR_LAUNCH on this thread. */
 CODA_API int coda_last_hip_error(void);

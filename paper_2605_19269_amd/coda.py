@@ -43,8 +43,9 @@ CODA_REDUCE_PARTIALS, CODA_REDUCE_ATOMIC, CODA_STORE_F32 = 0, 1, 2
 EXPORTS = ["coda_gemm", "coda_gemm_static_ws", "coda_gemm_workspace_bytes", "coda_row_partial_blocks", "coda_row_finalize",
            "coda_col_partial_blocks", "coda_col_finalize", "coda_lse_finalize",
            "coda_row_sumsq", "coda_fold_gamma", "coda_interleave_pairs", "coda_quantize", "coda_dequantize",
-           "coda_gemm_scaled", "coda_gemm_scaled_workspace_bytes", "coda_grad_scaled", "coda_grad_scaled_workspace_bytes", "coda_status_string",
-           "coda_last_hip_error"]
+           "coda_gemm_scaled", "coda_gemm_scaled_workspace_bytes", "coda_grad_scaled", "coda_grad_scaled_workspace_bytes",
+           "coda_attention", "coda_attention_bwd", "coda_attention_bwd_workspace_bytes", "coda_cache_store", "coda_attention_cached",
+           "coda_attention_cached_workspace_bytes", "coda_status_string", "coda_last_hip_error"]
 EXPORTS_UNFUSED = ["coda_unfused_rmsnorm_apply", "coda_unfused_swiglu_fwd", "coda_unfused_swiglu_bwd",
                    "coda_unfused_add_sumsq", "coda_unfused_accumulate"]
 EXPORTS_CALIB = ["coda_calib_mfma_loop", "coda_calib_mfma_loop16"]
@@ -60,6 +61,15 @@ class coda_epi_op(ctypes.Structure):
                 ("out", ctypes.c_void_p), ("out2", ctypes.c_void_p), ("ld_in", ctypes.c_int64),
                 ("ld_out", ctypes.c_int64), ("in2", ctypes.c_void_p), ("in3", ctypes.c_void_p),
                 ("in4", ctypes.c_void_p), ("out3", ctypes.c_void_p), ("i0", ctypes.c_int64), ("i1", ctypes.c_int64)]
+
+
+class coda_rope(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("pos_q", ctypes.c_void_p), ("pos_k", ctypes.c_void_p), ("rows", ctypes.c_int64)]
+
+
+class coda_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
 
 
 _vp, _i64, _i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
@@ -98,6 +108,19 @@ _lib.coda_grad_scaled.restype = ctypes.c_int
 _lib.coda_grad_scaled.argtypes = [_vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, ctypes.c_size_t]
 _lib.coda_grad_scaled_workspace_bytes.restype = ctypes.c_size_t
 _lib.coda_grad_scaled_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_f32, _size = ctypes.c_float, ctypes.c_size_t
+_lib.coda_attention.restype = ctypes.c_int
+_lib.coda_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _f32, _i32, _vp, _i64, _vp]
+_lib.coda_attention_bwd.restype = ctypes.c_int
+_lib.coda_attention_bwd.argtypes = [_vp] * 9 + [_i32, _i32, _i32, _f32, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _size]
+_lib.coda_attention_bwd_workspace_bytes.restype = _size
+_lib.coda_attention_bwd_workspace_bytes.argtypes = [_i64, _i64, _i32, _i32, _i32, _i32]
+_lib.coda_cache_store.restype = ctypes.c_int
+_lib.coda_cache_store.argtypes = [_vp] * 5
+_lib.coda_attention_cached.restype = ctypes.c_int
+_lib.coda_attention_cached.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _i32, _i32, _f32, _vp, _vp, _i64, _vp, _vp, _size]
+_lib.coda_attention_cached_workspace_bytes.restype = _size
+_lib.coda_attention_cached_workspace_bytes.argtypes = [_i64, _i32, _i32, _i32, _i32]
 _lib.coda_status_string.restype = ctypes.c_char_p
 _lib.coda_status_string.argtypes = [ctypes.c_int]
 _lib.coda_last_hip_error.restype = ctypes.c_int
@@ -404,6 +427,102 @@ def coda_grad_scaled(A, scales_a, B, scales_b, G, stream=None, workspace=None):
 
 def coda_grad_scaled_workspace_bytes(M, N, K):
     return _lib.coda_grad_scaled_workspace_bytes(M, N, K)
+
+
+# --- attention: Q, K, V and their gradients are bf16 [tokens x heads * dim] (column blocks of a QKV matrix too), seq_q, seq_k int32 [sequences + 1] ---
+def _ints(t, shape, what):
+    """The address of an int32 tensor, dense, of `shape`."""
+    if t is None:
+        return None
+    assert t.dtype == _torch.int32 and t.shape == shape and t.is_contiguous(), "%s: a dense int32 tensor of shape %s expected" % (what, tuple(shape))
+    return t.data_ptr()
+
+
+def _sequences(seq_q, seq_k):
+    n = seq_q.shape[0] - 1
+    assert n >= 0, "seq_q: sequences + 1 offsets expected"
+    return _ints(seq_q, (n + 1,), "seq_q"), _ints(seq_k, (n + 1,), "seq_k"), n
+
+
+def _output(t, shape, what):
+    """The address and the pitch of a bf16 output."""
+    assert t.dtype == _torch.bfloat16 and t.shape == shape and (t.shape[1] <= 1 or t.stride(1) == 1), "%s: a row-major bf16 tensor of shape %s expected" % (what, tuple(shape))
+    return t.data_ptr(), t.stride(0)
+
+
+def _row_stats(t, heads, rows, what):
+    if t is None:
+        return None
+    assert t.dtype == _torch.float32 and t.shape == (heads, rows) and t.is_contiguous(), "%s: a dense f32 tensor [heads x rows] expected" % what
+    return t.data_ptr()
+
+
+def coda_attention(Q, K, V, seq_q, out, heads, kv_heads, scale, lse=None, seq_k=None, causal=True, stream=None):
+    """out: bf16 [Tq x heads * dim]; lse: f32 [heads x Tq] or None; seq_k: None where K and V are packed as Q is."""
+    _torch or _import_torch()
+    at_q, at_k, n = _sequences(seq_q, seq_k)
+    o, ldo = _output(out, Q.shape, "out")
+    _check(_lib.coda_attention(_stream(stream), _binding.mat(Q, False, _DTYPES), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES), at_q, at_k, n,
+                               heads, kv_heads, scale, 1 if causal else 0, o, ldo, _row_stats(lse, heads, Q.shape[0], "lse")))
+
+
+def coda_attention_bwd(Q, K, V, out, dout, lse, seq_q, dQ, dK, dV, heads, kv_heads, scale, workspace, seq_k=None, causal=True, rope=None, stream=None):
+    """out, lse: what coda_attention left; dout: the gradient of out.  rope: (cos, sin, pos_q, pos_k) to turn dQ and dK back, pos_k None for pos_q;
+    cos / sin: f32 [rows x dim / 2] dense tables, pos_q: int32 [Tq], pos_k: int32 [Tk].  workspace: coda_attention_bwd_workspace_bytes(...) bytes."""
+    torch = _torch or _import_torch()
+    at_q, at_k, n = _sequences(seq_q, seq_k)
+    grads = _output(dQ, Q.shape, "dQ") + _output(dK, K.shape, "dK") + _output(dV, V.shape, "dV")
+    turn = None
+    if rope is not None:
+        cos, sin, pos_q, pos_k = tuple(rope) if len(rope) == 4 else tuple(rope) + (None,)
+        for t in (cos, sin):
+            assert t.dtype == torch.float32 and t.is_contiguous() and t.shape == (cos.shape[0], Q.shape[1] // heads // 2), "dense f32 tables [rows x dim / 2] expected"
+        turn = ctypes.byref(coda_rope(cos.data_ptr(), sin.data_ptr(), _ints(pos_q, (Q.shape[0],), "pos_q"),
+                                      _ints(pos_q if pos_k is None else pos_k, (K.shape[0],), "pos_k"), cos.shape[0]))
+    _check(_lib.coda_attention_bwd(_stream(stream), _binding.mat(Q, False, _DTYPES), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES),
+                                   _binding.mat(out, False, _DTYPES), _binding.mat(dout, False, _DTYPES), _row_stats(lse, heads, Q.shape[0], "lse"), at_q, at_k, n,
+                                   heads, kv_heads, scale, 1 if causal else 0, turn, *grads, *_at(workspace)))
+
+
+def coda_attention_bwd_workspace_bytes(Tq, Tk, n_seqs, heads, kv_heads, head_dim):
+    return _lib.coda_attention_bwd_workspace_bytes(Tq, Tk, n_seqs, heads, kv_heads, head_dim)
+
+
+def _cache(k, v):
+    assert k.dtype == v.dtype == _torch.bfloat16 and k.dim() == 4 and k.shape == v.shape and k.is_contiguous() and v.is_contiguous(), \
+        "dense bf16 caches [pages x kv_heads x page x dim] expected"
+    pages, kv_heads, page, dim = k.shape
+    return coda_cache(k.data_ptr(), v.data_ptr(), pages, page, kv_heads, dim)
+
+
+def coda_cache_store(K, V, slots, cache_k, cache_v, stream=None):
+    """Rows of K, V: bf16 [T x kv_heads * dim] to slots: int32 [T] (page * places + place, or -1 to leave a row out) of the caches
+    [pages x kv_heads x places x dim]."""
+    _torch or _import_torch()
+    cache = _cache(cache_k, cache_v)
+    _check(_lib.coda_cache_store(_stream(stream), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES), _ints(slots, (K.shape[0],), "slots"),
+                                 ctypes.byref(cache)))
+
+
+def coda_attention_cached(Q, cache_k, cache_v, table, lens, seq_q, out, heads, scale, workspace, tree=None, lse=None, stream=None):
+    """Q: bf16 [Tq x heads * dim], rows seq_q[s] .. of sequence s; table: int32 [sequences x pages], row-major; lens: int32 [sequences], keys in the cache with
+    those of the rows; tree: int64 or uint64 [Tq] bits of the sequence's rows that each row sees, None for a chain; workspace:
+    coda_attention_cached_workspace_bytes(...) bytes."""
+    torch = _torch or _import_torch()
+    cache = _cache(cache_k, cache_v)
+    at_q, _, n = _sequences(seq_q, None)
+    assert table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and (table.shape[1] <= 1 or table.stride(1) == 1) and \
+        (n <= 1 or table.stride(0) >= table.shape[1]), \
+        "table: a row-major int32 tensor [sequences x pages] expected"
+    assert tree is None or (tree.dtype in (torch.int64, torch.uint64) and tree.shape == Q.shape[:1] and tree.is_contiguous()), "tree: a 64-bit integer for each row expected"
+    o, ldo = _output(out, Q.shape, "out")
+    _check(_lib.coda_attention_cached(_stream(stream), _binding.mat(Q, False, _DTYPES), ctypes.byref(cache), table.data_ptr(), max(table.stride(0), table.shape[1]),
+                                      table.shape[1], _ints(lens, (n,), "lens"), at_q, n, heads, scale, _ptr(tree), o, ldo,
+                                      _row_stats(lse, heads, Q.shape[0], "lse"), *_at(workspace)))
+
+
+def coda_attention_cached_workspace_bytes(Tq, n_seqs, heads, kv_heads, head_dim):
+    return _lib.coda_attention_cached_workspace_bytes(Tq, n_seqs, heads, kv_heads, head_dim)
 
 
 def coda_status_string(status):

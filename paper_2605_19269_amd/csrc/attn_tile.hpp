@@ -1,0 +1,298 @@
+// attn_tile.hpp -- tiles, fragments and the softmax step that the attention kernels share (gfx950).
+//
+// One head's rows of Q, K, V or dO are tiles [rows x DP] of bf16 in LDS, DP = 64 or 128 columns (a head dimension below that leaves the
+// chunks behind it zero).  All products are v_mfma_f32_32x32x16_bf16, written so that what one product leaves in the accumulators is an
+// operand of the next as it stands: S^T = K Q^T leaves lane l with query l % 32 and, in register r, key (r & 3) + 8 (r >> 2) + 4 (l / 32);
+// the contraction of O^T = V^T P^T may run over the keys in any order that both operands share, so eight registers, rounded to bf16, are
+// the operand of 16 keys, and the transposing LDS read of V takes its keys in the same order: 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 for
+// the lanes of half h.  No element of P ever moves between lanes, and a row's maximum and sum are in-lane but for one swap of the halves.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace coda {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// Chunk c (16 bytes) of row r lies at chunk position c ^ attn_swizzle(r).  Both reads below are then free of bank conflicts: 16 consecutive
+// rows of one chunk, and four rows (r % 4 == 0) of 64 bytes each, cover all 64 banks.
+template <int DP>
+__device__ __forceinline__ int attn_swizzle(int r)
+{
+    return DP == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+
+__device__ __forceinline__ uint32_t attn_lds(const unsigned char *p)
+{
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const unsigned char *)p;
+}
+
+// 16 bytes a lane from its own address straight to LDS, lane l to lds + 16 l.  Not seen by the compiler's wait counts: attn_wait().
+__device__ __forceinline__ void attn_load16(const void *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void attn_load4(const void *p, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
+}
+// All loads of this wave have arrived, all its LDS reads are done
+__device__ __forceinline__ void attn_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void attn_barrier()
+{
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Rows row0 .. row0 + ROWS - 1 (those from n on: row n - 1 again) of one head, `base` its element (0, 0), into a tile; the workgroup's NW
+// waves share the work.  PAD: D < DP, the chunks behind D are left as attn_zero() made them.
+template <int DP, bool PAD, int ROWS, int NW>
+__device__ __forceinline__ void attn_load_tile(const uint16_t *base, int64_t ld, int row0, int n, unsigned char *tile, int wave, int lane, int D)
+{
+    constexpr int CH = DP / 8, RPL = 64 / CH;
+    static_assert(ROWS % (NW * RPL) == 0, "whole wave-loads");
+#pragma unroll
+    for (int i = 0; i < ROWS / (NW * RPL); ++i) {
+        const int r = (i * NW + wave) * RPL + lane / CH;
+        const int c = (lane % CH) ^ attn_swizzle<DP>(r);
+        const int row = min(row0 + r, n - 1);
+        if (!PAD || c * 8 < D) attn_load16(base + row * ld + c * 8, __builtin_amdgcn_readfirstlane(attn_lds(tile) + (i * NW + wave) * 1024));
+    }
+}
+
+// Clears `bytes` (a multiple of 16) of LDS for PAD kernels, before their first tile
+__device__ __forceinline__ void attn_zero(unsigned char *p, int bytes, int threads)
+{
+    for (int i = threadIdx.x * 16; i < bytes; i += threads * 16) *reinterpret_cast<u32x4 *>(p + i) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+}
+
+// Operand of 32 tile rows x 16 columns: row row_base + lane % 32, columns 16 t + 8 (lane / 32) ..
+template <int DP>
+__device__ __forceinline__ bf16x8 attn_rows(const unsigned char *tile, int row_base, int t, int lane)
+{
+    const int r = row_base + (lane & 31), c = 2 * t + (lane >> 5);
+    return *reinterpret_cast<const bf16x8 *>(tile + r * (DP * 2) + ((c ^ attn_swizzle<DP>(lane & 31)) << 4));
+}
+
+// Operand of the transposed tile, 32 columns x 16 rows: column 32 db + lane % 32, rows 16 t + 4 (lane / 32) + {0 1 2 3, 8 9 10 11}.  Within 16
+// lanes, lane i of a transposing read supplies the address of row i / 4, columns 4 (i % 4) .. and receives column i of the four rows.
+template <int DP>
+__device__ __forceinline__ bf16x8 attn_cols(const unsigned char *tile, int t, int db, int lane)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int i = lane & 15, c = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+    const int r = 4 * (lane >> 5) + (i >> 2);
+    const unsigned char *p = tile + t * 16 * DP * 2 + (i & 1) * 8;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + r * (DP * 2) + ((c ^ attn_swizzle<DP>(r)) << 4)));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + (r + 8) * (DP * 2) + ((c ^ attn_swizzle<DP>(r + 8)) << 4)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+__device__ __forceinline__ f32x16 attn_mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ uint32_t attn_pack(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+// Registers 8 half .. 8 half + 7 of an accumulator as an operand, to the nearest bf16
+__device__ __forceinline__ bf16x8 attn_operand(const f32x16 &x, int half)
+{
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = attn_pack(x[half * 8 + 2 * e], x[half * 8 + 2 * e + 1]);
+    return __builtin_bit_cast(bf16x8, v);
+}
+// Row of the accumulator that register r of a lane of half h holds
+__device__ __forceinline__ int attn_acc_row(int r, int h) { return (r & 3) + 8 * (r >> 2) + 4 * h; }
+
+// x of this lane combined with that of lane ^ 32
+__device__ __forceinline__ f32x2 attn_halves(float x)
+{
+    const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    const uint32_t a = p[0], b = p[1];                     // a bit cast of an element of the pair takes the first one both times
+    return f32x2{__builtin_bit_cast(float, a), __builtin_bit_cast(float, b)};
+}
+
+// Four consecutive values of a column of the accumulators, groups g and g + 1 (rows 8 g + 4 h .. and 8 g + 8 + 4 h ..), rounded and exchanged
+// between the halves: a lane of half h is left with rows 8 (g + h) .. 8 (g + h) + 7, 16 contiguous bytes of a row-major output.
+__device__ __forceinline__ u32x4 attn_store_unit(const float (&lo)[4], const float (&hi)[4])
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(attn_pack(lo[0], lo[1]), attn_pack(hi[0], hi[1]), false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(attn_pack(lo[2], lo[3]), attn_pack(hi[2], hi[3]), false, false);
+    return u32x4{a[0], b[0], a[1], b[1]};
+}
+
+// ---------------------------------------------------------------- infinities and NaN behind a mask
+// A weight of zero times an infinity or a NaN is NaN, so a row of V that is not finite would reach rows that do not see it.  Tiles that no mask
+// touches need nothing.  In the others (one or two for a tile of rows) what is not finite is replaced by zero in LDS before the products, and
+// only where there was any, its effect on the rows that do see it is added at the end: a product of the mask (0 or 1) with marks (+inf 1, -inf 2^10,
+// NaN 2^20; sums over a tile are exact in fp32) tells for each output whether it met +inf, -inf, both or a NaN.  Whatever order a sum takes
+// these in, the result is the same, so the end is early enough.
+
+// `bytes` of a tile from `tile` on (a multiple of 1024) by one wave; true if something was not finite
+__device__ __forceinline__ bool attn_clean(unsigned char *tile, int bytes, int lane)
+{
+    bool found = false;
+    for (int i = lane * 16; i < bytes; i += 1024) {
+        u32x4 v = *reinterpret_cast<const u32x4 *>(tile + i);
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top |= ((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        if (top) {
+            found = true;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;
+                if ((v[e] & 0x7f800000u) == 0x7f800000u) v[e] &= 0xffffu;
+            }
+            *reinterpret_cast<u32x4 *>(tile + i) = v;
+        }
+    }
+    return __ballot(found) != 0;
+}
+__device__ __forceinline__ bf16x8 attn_marks(bf16x8 x)
+{
+    s16x8 v = __builtin_bit_cast(s16x8, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int w = (uint16_t)v[e];
+        v[e] = (w & 0x7f80) != 0x7f80 ? 0 : (w & 0x7f) ? 0x4980 : (w & 0x8000) ? 0x4480 : 0x3f80;   // 2^20, 2^10, 1
+    }
+    return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ float attn_marked(float o, float marks)
+{
+    const int n = (int)fminf(marks, 1048576.0f);
+    if (n == 0) return o;
+    const bool plus = n & 1023, minus = (n >> 10) & 1023;
+    if (n >= 1048576 || (plus && minus)) return __builtin_nanf("");
+    return o + (plus ? __builtin_inff() : -__builtin_inff());
+}
+// What the elements of an uncleaned tile of NT x 16 rows that are not finite come to in acc; vis(k): the lane's row sees row k of the tile
+template <int DP, int NT, class Vis>
+__device__ __forceinline__ void attn_add_marks(const unsigned char *tile, f32x16 (&acc)[DP / 32], int lane, Vis vis)
+{
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b) {
+        f32x16 marks = {};
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            s16x8 see;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) see[e] = vis(16 * t + (e & 3) + 8 * (e >> 2) + 4 * (lane >> 5)) ? 0x3f80 : 0;
+            marks = attn_mfma(attn_marks(attn_cols<DP>(tile, t, b, lane)), __builtin_bit_cast(bf16x8, see), marks);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[b][r] = attn_marked(acc[b][r], marks[r]);
+    }
+}
+
+// ---------------------------------------------------------------- one tile of keys
+// What a wave holds of 32 rows: O^T, and for the lane's row the running maximum of the raw scores and the sum of this half's weights
+template <int DP>
+struct AttnRows {
+    f32x16 o[DP / 32];
+    float m, l;
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b) o[b] = f32x16{};
+        m = -__builtin_inff();
+        l = 0.0f;
+    }
+};
+
+// Keys of a tile (NB x 32 of them) for 32 rows: S^T, the softmax step, O^T += V^T P^T.  c = scale * log2(e) > 0.  `masked`: some position is not
+// visible; vis(k) says whether key k of the tile is, for the lane's row.  The maximum that the weights are taken relative to is renewed only
+// when some row's has grown by more than 2^8 in weight: weights up to 2^8 cost no accuracy in bf16 or fp32, and the 64 multiplications of O^T
+// fall away for nearly all tiles.
+template <int DP, int NB, class Vis>
+__device__ __forceinline__ void attn_step(const unsigned char *kt, const unsigned char *vt, const bf16x8 (&q)[DP / 16], AttnRows<DP> &rows, float c, int lane,
+                                          bool masked, Vis vis)
+{
+    const int h = lane >> 5;
+    f32x16 s[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = attn_mfma(attn_rows<DP>(kt, b * 32, t, lane), q[t], s[b]);
+    if (masked) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = vis(b * 32 + attn_acc_row(r, h)) ? s[b][r] : -__builtin_inff();
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+    const f32x2 tops = attn_halves(top);
+    top = fmaxf(rows.m, fmaxf(tops[0], tops[1]));
+    if (__ballot((top - rows.m) * c > 8.0f)) {             // -inf - -inf is NaN: no row that has seen nothing asks for it
+        const float alpha = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((rows.m - top) * c);
+        rows.l *= alpha;
+        rows.m = top;
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) rows.o[b][r] *= alpha;
+    }
+    const float mc = rows.m == -__builtin_inff() ? 0.0f : rows.m * c;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r], c, -mc));
+            sum[r & 3] += s[b][r];
+        }
+    rows.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    bf16x8 p[2 * NB];
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t) p[t] = attn_operand(s[t >> 1], t & 1);
+#pragma unroll
+    for (int t = 0; t < 2 * NB; ++t)
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b) rows.o[b] = attn_mfma(attn_cols<DP>(vt, t, b, lane), p[t], rows.o[b]);
+}
+
+// ---------------------------------------------------------------- packed sequences
+struct AttnSpan {
+    int begin, count;
+};
+// Rows of sequence s of `total`, whatever the offsets hold
+__device__ __forceinline__ AttnSpan attn_span(const int32_t *at, int s, int total)
+{
+    const int a = min(max(at[s], 0), total), b = min(max(at[s + 1], a), total);
+    return {a, b - a};
+}
+// Tiles of `rows` rows are numbered from begin / rows + s in sequence s, so that the number of a tile gives its sequence without anyone having
+// counted the tiles: the next sequence's first number is never below this one's last plus one.  Numbers that no sequence uses do nothing.
+// Returns the last sequence whose first number is not above t; 64 candidates are looked at at once.
+__device__ __forceinline__ int attn_find(const int32_t *at, int n_seqs, int64_t unit, int rows, int64_t t, int lane)
+{
+    int lo = 0, width = n_seqs;
+    while (width > 1) {
+        const int step = (width + 63) / 64, i = lane * step;
+        const bool below = i < width && (int64_t)max(at[lo + i], 0) * unit / rows + lo + i <= t;
+        const int k = __popcll(__ballot(below));
+        if (k > 1) lo += (k - 1) * step;
+        width = min(step, n_seqs - lo);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+}  // namespace coda

@@ -3,6 +3,7 @@
 // Nothing here allocates, synchronises or keeps state beyond the last HIP error.
 #include "../../include/coda.h"
 
+#include "attn_launch.hpp"
 #include "aux_kernels.hpp"
 #include "gemm_launch.hpp"
 #include "narrow_launch.hpp"
@@ -458,6 +459,62 @@ hipError_t static_scratch(void **out)
     return hipSuccess;
 }
 
+// ---- attention ----------------------------------------------------------------------------------------------------------
+// bf16 [r x c], one row a token
+coda_status check_rows(const coda_mat *X, int64_t r, int64_t c)
+{
+    if (!X) return CODA_ERR_NULL;
+    if (X->dtype != CODA_BF16) return CODA_ERR_DTYPE;
+    if (X->trans || X->rows < 0 || X->rows > INT32_MAX) return CODA_ERR_SHAPE;
+    return check_operand(X, r, c);
+}
+bool heads_fit(int32_t heads, int32_t kv_heads, int64_t head_dim)
+{
+    return kv_heads > 0 && heads > 0 && heads % kv_heads == 0 && head_dim >= 8 && head_dim <= 128 && head_dim % 8 == 0 && heads * head_dim <= MAX_LD;
+}
+bool scale_fits(float scale) { return scale > 0.0f && scale < __builtin_inff(); }
+
+coda_status check_heads(const coda_mat *Q, const coda_mat *K, const coda_mat *V, const int32_t *seq_q, const int32_t *seq_k, int32_t n_seqs, int32_t heads,
+                        int32_t kv_heads, float scale, coda::AttnParams &p)
+{
+    if (!Q || !K || !V) return CODA_ERR_NULL;
+    if (heads <= 0 || Q->cols % heads || !heads_fit(heads, kv_heads, Q->cols / heads) || n_seqs < 0 || !scale_fits(scale)) return CODA_ERR_SHAPE;
+    const int64_t D = Q->cols / heads;
+    coda_status st;
+    if ((st = check_rows(Q, Q->rows, heads * D)) != CODA_OK) return st;
+    if ((st = check_rows(K, K->rows, kv_heads * D)) != CODA_OK) return st;
+    if ((st = check_rows(V, K->rows, kv_heads * D)) != CODA_OK) return st;
+    if ((!seq_k && K->rows != Q->rows) || Q->rows * (heads / kv_heads) > INT32_MAX) return CODA_ERR_SHAPE;
+    if (n_seqs > 0 && (Q->rows > 0 || K->rows > 0)) {
+        if ((st = check_vec(seq_q)) != CODA_OK) return st;
+        if (seq_k && !aligned4(seq_k)) return CODA_ERR_ALIGN;
+    }
+    p.Q = static_cast<const uint16_t *>(Q->ptr);
+    p.K = static_cast<const uint16_t *>(K->ptr);
+    p.V = static_cast<const uint16_t *>(V->ptr);
+    p.ldq = Q->ld;
+    p.ldk = K->ld;
+    p.ldv = V->ld;
+    p.seq_q = seq_q;
+    p.seq_k = seq_k ? seq_k : seq_q;
+    p.n_seqs = n_seqs;
+    p.heads = heads;
+    p.kv_heads = kv_heads;
+    p.D = (int)D;
+    p.Tq = (int)Q->rows;
+    p.Tk = (int)K->rows;
+    p.scale = scale;
+    return CODA_OK;
+}
+
+coda_status check_cache(const coda_cache *c)
+{
+    if (!c) return CODA_ERR_NULL;
+    if (c->pages < 0 || c->page <= 0 || (c->page & (c->page - 1)) || c->pages >= (int64_t(1) << 31) / c->page || !heads_fit(c->kv_heads, c->kv_heads, c->head_dim))
+        return CODA_ERR_SHAPE;
+    return aligned16(c->k) && aligned16(c->v) ? CODA_OK : CODA_ERR_ALIGN;
+}
+
 }  // namespace
 
 extern "C" {
@@ -708,6 +765,154 @@ coda_status coda_grad_scaled(void *stream, int64_t M, int64_t N, int64_t K, cons
     p.K = (int)K;
     p.part = static_cast<float *>(workspace);
     return launch_status(coda::launch_grad_scaled(plan, b8, g, p, static_cast<hipStream_t>(stream)));
+}
+
+coda_status coda_attention(void *stream, const coda_mat *Q, const coda_mat *K, const coda_mat *V, const int32_t *seq_q, const int32_t *seq_k, int32_t n_seqs,
+                           int32_t heads, int32_t kv_heads, float scale, int32_t causal, void *out, int64_t ld_out, float *lse)
+{
+    coda::AttnParams p{};
+    coda_status st;
+    if ((st = check_heads(Q, K, V, seq_q, seq_k, n_seqs, heads, kv_heads, scale, p)) != CODA_OK) return st;
+    p.causal = causal != 0;
+    if (p.Tq == 0 || n_seqs == 0) return CODA_OK;
+    if ((st = check_tile(out, ld_out, Q->cols)) != CODA_OK) return st;
+    if (lse && !aligned4(lse)) return CODA_ERR_ALIGN;
+    p.out = static_cast<uint16_t *>(out);
+    p.ldo = ld_out;
+    p.lse = lse;
+    if (!launch_fits(coda::attn_workgroups(p), 256)) return CODA_ERR_SHAPE;
+    return launch_status(coda::launch_attention(p, static_cast<hipStream_t>(stream)));
+}
+
+size_t coda_attention_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seqs, int32_t heads, int32_t kv_heads, int32_t head_dim)
+{
+    if (Tq <= 0 || Tq > INT32_MAX || Tk < 0 || n_seqs <= 0 || !heads_fit(heads, kv_heads, head_dim)) return 0;
+    return coda::bwd_bytes(Tq, heads);
+}
+
+coda_status coda_attention_bwd(void *stream, const coda_mat *Q, const coda_mat *K, const coda_mat *V, const coda_mat *O, const coda_mat *dO, const float *lse,
+                               const int32_t *seq_q, const int32_t *seq_k, int32_t n_seqs, int32_t heads, int32_t kv_heads, float scale, int32_t causal,
+                               const coda_rope *rope, void *dQ, int64_t ld_dq, void *dK, int64_t ld_dk, void *dV, int64_t ld_dv, void *workspace,
+                               size_t workspace_bytes)
+{
+    coda::BwdParams p{};
+    coda_status st;
+    if ((st = check_heads(Q, K, V, seq_q, seq_k, n_seqs, heads, kv_heads, scale, p.f)) != CODA_OK) return st;
+    p.f.causal = causal != 0;
+    if (!O || !dO) return CODA_ERR_NULL;
+    if ((st = check_rows(O, Q->rows, Q->cols)) != CODA_OK) return st;
+    if ((st = check_rows(dO, Q->rows, Q->cols)) != CODA_OK) return st;
+    if ((p.f.Tq == 0 && p.f.Tk == 0) || n_seqs == 0) return CODA_OK;
+    if (p.f.Tq > 0) {
+        if ((st = check_vec(lse)) != CODA_OK) return st;
+        if ((st = check_tile(dQ, ld_dq, Q->cols)) != CODA_OK) return st;
+    }
+    if (p.f.Tk > 0 && ((st = check_tile(dK, ld_dk, K->cols)) != CODA_OK || (st = check_tile(dV, ld_dv, K->cols)) != CODA_OK)) return st;
+    if (rope) {
+        if (!rope->cos || !rope->sin || (p.f.Tq > 0 && !rope->pos_q) || (p.f.Tk > 0 && !rope->pos_k)) return CODA_ERR_NULL;
+        if (rope->rows < 1 || rope->rows > INT32_MAX / (p.f.D / 2)) return CODA_ERR_SHAPE;
+        if ((reinterpret_cast<uintptr_t>(rope->cos) & 7u) || (reinterpret_cast<uintptr_t>(rope->sin) & 7u) || !aligned4(rope->pos_q) || !aligned4(rope->pos_k))
+            return CODA_ERR_ALIGN;
+        p.cos = rope->cos;
+        p.sin = rope->sin;
+        p.pos_q = rope->pos_q;
+        p.pos_k = rope->pos_k;
+        p.rope_rows = (int)rope->rows;
+    }
+    if (p.f.Tq > 0) {
+        if (!workspace) return CODA_ERR_NULL;
+        if (!aligned16(workspace)) return CODA_ERR_ALIGN;
+        if (workspace_bytes < coda::bwd_bytes(p.f.Tq, heads)) return CODA_ERR_WORKSPACE;
+    }
+    p.f.lse = const_cast<float *>(lse);
+    p.O = static_cast<const uint16_t *>(O->ptr);
+    p.dO = static_cast<const uint16_t *>(dO->ptr);
+    p.ldo = O->ld;
+    p.lddo = dO->ld;
+    p.dQ = static_cast<uint16_t *>(dQ);
+    p.dK = static_cast<uint16_t *>(dK);
+    p.dV = static_cast<uint16_t *>(dV);
+    p.lddq = ld_dq;
+    p.lddk = ld_dk;
+    p.lddv = ld_dv;
+    p.stats = static_cast<float *>(workspace);
+    if (!launch_fits(coda::bwd_workgroups(p), 256)) return CODA_ERR_SHAPE;
+    return launch_status(coda::launch_attention_bwd(p, static_cast<hipStream_t>(stream)));
+}
+
+coda_status coda_cache_store(void *stream, const coda_mat *K, const coda_mat *V, const int32_t *slots, const coda_cache *cache)
+{
+    coda_status st;
+    if ((st = check_cache(cache)) != CODA_OK) return st;
+    const int64_t cols = (int64_t)cache->kv_heads * cache->head_dim;
+    if (!K || !V) return CODA_ERR_NULL;
+    if ((st = check_rows(K, K->rows, cols)) != CODA_OK) return st;
+    if ((st = check_rows(V, K->rows, cols)) != CODA_OK) return st;
+    if (K->rows == 0) return CODA_OK;
+    if ((st = check_vec(slots)) != CODA_OK) return st;
+    if (cache->pages == 0) return CODA_OK;                 // no slot is one of the cache's
+    if (!cache->k || !cache->v) return CODA_ERR_NULL;
+    if (!launch_fits(coda::cache_store_workgroups(K->rows, (int)cols), 256)) return CODA_ERR_SHAPE;
+    return launch_status(coda::launch_cache_store(static_cast<const uint16_t *>(K->ptr), K->ld, static_cast<const uint16_t *>(V->ptr), V->ld, K->rows, (int)cols,
+                                                  cache->head_dim, slots, static_cast<uint16_t *>(cache->k), static_cast<uint16_t *>(cache->v),
+                                                  cache->pages * cache->page, __builtin_ctz((unsigned)cache->page), static_cast<hipStream_t>(stream)));
+}
+
+size_t coda_attention_cached_workspace_bytes(int64_t Tq, int32_t n_seqs, int32_t heads, int32_t kv_heads, int32_t head_dim)
+{
+    if (Tq <= 0 || Tq > INT32_MAX || n_seqs <= 0 || !heads_fit(heads, kv_heads, head_dim)) return 0;
+    return coda::cached_bytes(Tq, n_seqs, heads, kv_heads, head_dim);
+}
+
+coda_status coda_attention_cached(void *stream, const coda_mat *Q, const coda_cache *cache, const int32_t *table, int64_t ld_table, int64_t table_pages,
+                                  const int32_t *lens, const int32_t *seq_q, int32_t n_seqs, int32_t heads, float scale, const uint64_t *tree, void *out,
+                                  int64_t ld_out, float *lse, void *workspace, size_t workspace_bytes)
+{
+    coda_status st;
+    if ((st = check_cache(cache)) != CODA_OK) return st;
+    if (!Q) return CODA_ERR_NULL;
+    if (!heads_fit(heads, cache->kv_heads, cache->head_dim) || n_seqs < 0 || !scale_fits(scale)) return CODA_ERR_SHAPE;
+    if ((st = check_rows(Q, Q->rows, (int64_t)heads * cache->head_dim)) != CODA_OK) return st;
+    const int group = heads / cache->kv_heads;
+    if (Q->rows * group > INT32_MAX || table_pages < 0 || ld_table < table_pages || table_pages > (int64_t(1) << 30) / cache->page) return CODA_ERR_SHAPE;
+    if (Q->rows == 0 || n_seqs == 0) return CODA_OK;
+    if ((st = check_vec(lens)) != CODA_OK || (st = check_vec(seq_q)) != CODA_OK) return st;
+    const int64_t capacity = cache->pages ? table_pages * cache->page : 0;
+    if (capacity) {
+        if (!cache->k || !cache->v) return CODA_ERR_NULL;
+        if ((st = check_vec(table)) != CODA_OK) return st;
+    }
+    if ((st = check_tile(out, ld_out, Q->cols)) != CODA_OK) return st;
+    if (lse && !aligned4(lse)) return CODA_ERR_ALIGN;
+    if (tree && (reinterpret_cast<uintptr_t>(tree) & 7u)) return CODA_ERR_ALIGN;
+    if (!workspace) return CODA_ERR_NULL;
+    if (!aligned16(workspace)) return CODA_ERR_ALIGN;
+    if (workspace_bytes < coda::cached_bytes(Q->rows, n_seqs, heads, cache->kv_heads, cache->head_dim)) return CODA_ERR_WORKSPACE;
+    coda::CachedParams p{};
+    p.Q = static_cast<const uint16_t *>(Q->ptr);
+    p.K = static_cast<const uint16_t *>(cache->k);
+    p.V = static_cast<const uint16_t *>(cache->v);
+    p.ldq = Q->ld;
+    p.ld_table = ld_table;
+    p.table = table;
+    p.lens = lens;
+    p.seq_q = seq_q;
+    p.tree = tree;
+    p.n_seqs = n_seqs;
+    p.kv_heads = cache->kv_heads;
+    p.group = group;
+    p.D = cache->head_dim;
+    p.Tq = (int)Q->rows;
+    p.page_bits = __builtin_ctz((unsigned)cache->page);
+    p.pages = (int)cache->pages;
+    p.capacity = (int)capacity;
+    p.scale = scale;
+    p.out = static_cast<uint16_t *>(out);
+    p.ldo = ld_out;
+    p.lse = lse;
+    p.part = static_cast<float *>(workspace);
+    if (!launch_fits(coda::cached_workgroups(p), 256)) return CODA_ERR_SHAPE;
+    return launch_status(coda::launch_attention_cached(p, static_cast<hipStream_t>(stream)));
 }
 
 const char *coda_status_string(coda_status s)
