@@ -48,10 +48,11 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, float c
     if (threadIdx.x == 0) dirty = 0;
     if (PAD) attn_zero(smem, sizeof(smem), 256);
     const int n = (keys + FWD_KEYS - 1) / FWD_KEYS;
+    const AttnLoad<DP, PAD, FWD_KEYS, FWD_WAVES> load_k(K, p.ldk, wave, lane, p.D), load_v(V, p.ldv, wave, lane, p.D);
     const auto load = [&](int j) {
         unsigned char *at = smem + (j & 1) * 2 * TILE;
-        attn_load_tile<DP, PAD, FWD_KEYS, FWD_WAVES>(K, p.ldk, j * FWD_KEYS, k.count, at, wave, lane, p.D);
-        attn_load_tile<DP, PAD, FWD_KEYS, FWD_WAVES>(V, p.ldv, j * FWD_KEYS, k.count, at + TILE, wave, lane, p.D);
+        load_k(j * FWD_KEYS, k.count, at, lane);
+        load_v(j * FWD_KEYS, k.count, at + TILE, lane);
     };
     if (n > 0) load(0);
     for (int j = 0; j < n; ++j) {
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, float c
         unsigned char *at = smem + (j & 1) * 2 * TILE;
         if (k0 + FWD_KEYS > whole) {
             if (attn_clean(at + TILE + wave * (TILE / FWD_WAVES), TILE / FWD_WAVES, lane)) dirty = 1;
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            attn_reads_done();
             attn_barrier();
         }
         if (k0 >= high) continue;
@@ -73,7 +74,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, float c
         __syncthreads();
         if (dirty)
             for (int j = whole / FWD_KEYS; j < n; ++j) {
-                attn_load_tile<DP, PAD, FWD_KEYS, FWD_WAVES>(V, p.ldv, j * FWD_KEYS, k.count, smem, wave, lane, p.D);
+                load_v(j * FWD_KEYS, k.count, smem, lane);
                 attn_wait();
                 attn_barrier();
                 const int lim = mine - j * FWD_KEYS;

@@ -12,6 +12,9 @@
 namespace coda {
 
 constexpr int BWD_WAVES = 4;
+#ifndef DKV_NS
+#define DKV_NS 4
+#endif
 
 // stats[0][h][t] = lse * log2(e), stats[1][h][t] = delta.  16 (8) lanes a row of a head.
 template <int DP>
@@ -38,49 +41,51 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(BwdParams p)
     }
 }
 
-// The accumulators of 32 columns (rows of dQ or dK, dV) out: times `scale`, turned back by the angle of position `pos` where there are tables
-template <int DP, bool PAD>
-__device__ __forceinline__ void bwd_store(const f32x16 (&acc)[DP / 32], float scale, const BwdParams &p, const float *cos, const int32_t *pos, uint16_t *out, bool there,
-                                          int h)
+// Columns 32 b .. of 32 rows of dQ, dK or dV out of their accumulators: times `scale`, turned back by the angle of table row `at` where there are tables
+template <bool PAD>
+__device__ __forceinline__ void bwd_store(const f32x16 &acc, int b, float scale, const BwdParams &p, const float *cos, int64_t at, uint16_t *out, bool there, int h)
 {
-    int64_t at = 0;
-    if (cos && there) at = (int64_t)min(max(*pos, 0), p.rope_rows - 1) * (p.f.D / 2);
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
+    for (int g = 0; g < 4; g += 2) {
+        float v[2][4];
 #pragma unroll
-        for (int g = 0; g < 4; g += 2) {
-            float v[2][4];
+        for (int i = 0; i < 2; ++i) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int e = 0; e < 4; ++e) v[i][e] = acc[4 * (g + i) + e] * scale;
+            const int d = 32 * b + 8 * (g + i) + 4 * h;
+            if (cos && there && (!PAD || d < p.f.D)) {
+                const f32x2 c = *reinterpret_cast<const f32x2 *>(cos + at + d / 2), s = *reinterpret_cast<const f32x2 *>(p.sin + at + d / 2);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[i][e] = acc[b][4 * (g + i) + e] * scale;
-                const int d = 32 * b + 8 * (g + i) + 4 * h;
-                if (cos && there && (!PAD || d < p.f.D)) {
-                    const f32x2 c = *reinterpret_cast<const f32x2 *>(cos + at + d / 2), s = *reinterpret_cast<const f32x2 *>(p.sin + at + d / 2);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float x = v[i][2 * e], y = v[i][2 * e + 1];
-                        v[i][2 * e] = x * c[e] + y * s[e];
-                        v[i][2 * e + 1] = y * c[e] - x * s[e];
-                    }
+                for (int e = 0; e < 2; ++e) {
+                    const float x = v[i][2 * e], y = v[i][2 * e + 1];
+                    v[i][2 * e] = x * c[e] + y * s[e];
+                    v[i][2 * e + 1] = y * c[e] - x * s[e];
                 }
             }
-            const u32x4 u = attn_store_unit(v[0], v[1]);
-            const int d = 32 * b + 8 * (g + h);
-            if (there && (!PAD || d < p.f.D)) *reinterpret_cast<u32x4 *>(out + d) = u;
         }
+        const u32x4 u = attn_store_unit(v[0], v[1]);
+        const int d = 32 * b + 8 * (g + h);
+        if (there && (!PAD || d < p.f.D)) *reinterpret_cast<u32x4 *>(out + d) = u;
+    }
+}
+
+// The table row of a token, times D / 2
+__device__ __forceinline__ int64_t bwd_angle(const BwdParams &p, const int32_t *pos, bool there)
+{
+    return p.cos && there ? (int64_t)min(max(*pos, 0), p.rope_rows - 1) * (p.f.D / 2) : 0;
 }
 
 // dK and dV.  The four waves are two blocks of 32 keys times two streams: a stream takes every second of the (head of the group, 32 rows) pairs that
 // see the keys, and the two are added up at the end.  S = Q K^T and dP = dO V^T have the lane's key in their columns, so P and dS are
 // operands of dV^T += dO^T P and dK^T += Q^T dS as they stand.
-template <int DP, bool PAD>
-__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdParams p, float c)
+template <int DP, bool PAD, int KB, int NS>
+__global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParams p, float c)
 {
-    constexpr int ROWS = 32, TILE = ROWS * DP * 2, STAGE = 2 * TILE + 256, KEYS = 64;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * STAGE];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int kb = wave & 1, stream = wave >> 1;
+    constexpr int ROWS = 32, TILE = ROWS * DP * 2, STAGE = 2 * TILE + 256, KEYS = KB * 32;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * NS * STAGE];
+    int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int kb = wave % KB, stream = wave / KB;
     const int64_t t = blockIdx.x / p.f.kv_heads;
     const int kv = blockIdx.x % p.f.kv_heads;
     const int s = attn_find(p.f.seq_k, p.f.n_seqs, 1, KEYS, t, lane);
@@ -102,42 +107,64 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdParams p, floa
     f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dk[b] = dv[b] = f32x16{};
-    if (PAD) attn_zero(smem, sizeof(smem), 256);
-    // tiles of rows from the first that sees key0
-    const int t0 = p.f.causal ? max(0, key0 - ahead) / ROWS : 0, per_head = max(0, (q.count + ROWS - 1) / ROWS - t0);
-    const int items = per_head * group, rounds = (items + 1) / 2;
-    const auto load = [&](int x, int buf) {
-        if (x >= items) return;
-        const int head = kv * group + x / per_head, row0 = (t0 + x % per_head) * ROWS;
-        unsigned char *at = smem + (buf * 2 + stream) * STAGE;
-        attn_load_tile<DP, PAD, ROWS, 2>(p.f.Q + (int64_t)q.begin * p.f.ldq + (int64_t)head * p.f.D, p.f.ldq, row0, q.count, at, kb, lane, p.f.D);
-        attn_load_tile<DP, PAD, ROWS, 2>(p.dO + (int64_t)q.begin * p.lddo + (int64_t)head * p.f.D, p.lddo, row0, q.count, at + TILE, kb, lane, p.f.D);
+    if (PAD) attn_zero(smem, sizeof(smem), KB * NS * 64);
+    // A stream's places are (tile of rows, head of the group), tiles from the first that sees key0
+    const int t0 = p.f.causal ? max(0, key0 - ahead) / ROWS : 0, tiles = (q.count + ROWS - 1) / ROWS;
+    const int rounds = tiles > t0 ? ((tiles - t0) * group + NS - 1) / NS : 0;
+    struct Place {
+        int tile, head;
+    };
+    const auto place = [&](int x) { return Place{t0 + x / group, x % group}; };
+    const int step_tile = NS / group, step_head = NS % group;
+    const auto step = [&](Place &x) {
+        x.tile += step_tile;
+        x.head += step_head;
+        if (x.head >= group) {
+            x.head -= group;
+            ++x.tile;
+        }
+    };
+    AttnLoad<DP, PAD, ROWS, KB> load_q(p.f.Q + (int64_t)q.begin * p.f.ldq + (int64_t)kv * group * p.f.D, p.f.ldq, kb, lane, p.f.D),
+        load_do(p.dO + (int64_t)q.begin * p.lddo + (int64_t)kv * group * p.f.D, p.lddo, kb, lane, p.f.D);
+    const uint16_t *const q_base = load_q.base, *const do_base = load_do.base;
+    const float *const stats_base = p.stats + (int64_t)kv * group * p.f.Tq + q.begin;
+    const auto load = [&](const Place &x, int buf) {
+        if (x.tile >= tiles) return;
+        unsigned char *at = smem + (buf * NS + stream) * STAGE;
+        load_q.base = q_base + x.head * p.f.D;
+        load_do.base = do_base + x.head * p.f.D;
+        load_q(x.tile * ROWS, q.count, at, lane);
+        load_do(x.tile * ROWS, q.count, at + TILE, lane);
         if (kb == 0)
-            attn_load4(p.stats + ((int64_t)(h * p.f.heads + head) * p.f.Tq + q.begin + min(row0 + (lane & 31), q.count - 1)),
+            attn_load4(stats_base + (int64_t)x.head * p.f.Tq + ((int64_t)h * p.f.heads * p.f.Tq + min(x.tile * ROWS + (lane & 31), q.count - 1)),
                        __builtin_amdgcn_readfirstlane(attn_lds(at + 2 * TILE)));
     };
-    // some of the tile's rows do not see all of the workgroup's keys
-    const auto partly = [&](int x) {
-        const int row0 = (t0 + x % per_head) * ROWS;
-        return x < items && (row0 + ROWS > q.count || (p.f.causal && row0 + ahead < key0 + KEYS - 1));
-    };
-    load(stream, 0);
+    // some of the tile's rows do not see all of the workgroup's keys, or are none
+    const auto ahead_of_keys = [&](int tile) { return p.f.causal && tile * ROWS + ahead < key0 + KEYS - 1; };
+    const auto ragged = [&](int tile) { return tile * ROWS + ROWS > q.count; };
+    Place lead = place(0), x = place(stream), next = x;   // the first stream's and this one's
+    if (rounds) load(x, 0);
     for (int i = 0; i < rounds; ++i) {
         attn_wait();
         attn_barrier();
-        if (i + 1 < rounds) load(2 * (i + 1) + stream, (i + 1) & 1);
-        const int x = 2 * i + stream;
-        unsigned char *at = smem + ((i & 1) * 2 + stream) * STAGE;
-        const bool mine = partly(x);
-        if (partly(2 * i) || partly(2 * i + 1)) {
+        step(next);
+        if (i + 1 < rounds) load(next, (i + 1) & 1);
+        unsigned char *at = smem + ((i & 1) * NS + stream) * STAGE;
+        const Place now = x;
+        x = next;
+        const bool mine = now.tile < tiles && (ahead_of_keys(now.tile) || ragged(now.tile));
+        // where any stream has a masked tile all wait while it is cleaned: theirs are tiles lead.tile to (NS - 1) / group + 1 further
+        if (ahead_of_keys(lead.tile) || ragged(lead.tile + (NS - 1) / group + 1)) {
             if (mine) {
-                attn_clean(at + kb * TILE, TILE, lane);    // Q by one wave of the stream, dO by the other
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, lane);
+                attn_reads_done();
             }
             attn_barrier();
         }
-        const int row0 = (t0 + x % per_head) * ROWS;
-        if (x >= items || (p.f.causal && row0 + ROWS - 1 + ahead < key0 + kb * 32)) continue;
+        step(lead);
+        if (DP == 128) asm volatile("" : "+v"(lane));      // the addresses of the LDS reads are formed again each round: 16 registers that the kernel has not
+        const int row0 = now.tile * ROWS;
+        if (now.tile >= tiles || (p.f.causal && row0 + ROWS - 1 + ahead < key0 + kb * 32)) continue;
         f32x16 sc = {}, dp = {};
 #pragma unroll
         for (int u = 0; u < DP / 16; ++u) sc = attn_mfma(attn_rows<DP>(at, 0, u, lane), kf[u], sc);
@@ -178,30 +205,37 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(BwdParams p, floa
             for (int b = 0; b < DP / 32; ++b) dk[b] = attn_mfma(attn_cols<DP>(at, u, b, lane), w, dk[b]);
         }
     }
-    // Stream 0 finishes dK, stream 1 dV: each hands the other its part
-    __syncthreads();
-    f32x4 *swap = reinterpret_cast<f32x4 *>(smem) + wave * (DP / 32 * 4) * 64 + lane;
-#pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x16 &v = stream ? dk[b] : dv[b];
-            swap[(b * 4 + g) * 64] = f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
-        }
-    __syncthreads();
-    const f32x4 *other = reinterpret_cast<const f32x4 *>(smem) + (wave ^ 2) * (DP / 32 * 4) * 64 + lane;
-    f32x16 sum[DP / 32];
-#pragma unroll
-    for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const f32x4 v = other[(b * 4 + g) * 64];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[b][4 * g + e] = (stream ? dv[b][4 * g + e] : dk[b][4 * g + e]) + v[e];
-        }
+    // The streams' parts are added up in their order: all of dK, then all of dV through LDS, and a stream finishes every NS-th 32 columns
     const int64_t row = (int64_t)k.begin + key;
-    if (stream) bwd_store<DP, PAD>(sum, 1.0f, p, nullptr, nullptr, p.dV + row * p.lddv + (int64_t)kv * p.f.D, key < k.count, h);
-    else bwd_store<DP, PAD>(sum, p.f.scale, p, p.cos, p.pos_k + row, p.dK + row * p.lddk + (int64_t)kv * p.f.D, key < k.count, h);
+    const bool there = key < k.count;
+    const int64_t angle = bwd_angle(p, p.pos_k + row, there);
+    f32x4 *parts = reinterpret_cast<f32x4 *>(smem) + lane;
+    constexpr int UNITS = DP / 32 * 4;                     // of four registers, 1 KB each
+    static_assert(KB * NS * UNITS * 1024 <= 2 * NS * STAGE, "the parts take the place of the tiles");
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const f32x16 &v = which ? dv[u / 4] : dk[u / 4];
+            const int g = u % 4 * 4;
+            parts[(wave * UNITS + u) * 64] = f32x4{v[g], v[g + 1], v[g + 2], v[g + 3]};
+        }
+        __syncthreads();
+        for (int b = stream; b < DP / 32; b += NS) {
+            f32x16 sum = {};
+#pragma unroll
+            for (int j = 0; j < NS; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 v = parts[((j * KB + kb) * UNITS + b * 4 + g) * 64];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[4 * g + e] += v[e];
+                }
+            if (which) bwd_store<PAD>(sum, b, 1.0f, p, nullptr, 0, p.dV + row * p.lddv + (int64_t)kv * p.f.D, there, h);
+            else bwd_store<PAD>(sum, b, p.f.scale, p, p.cos, angle, p.dK + row * p.lddk + (int64_t)kv * p.f.D, there, h);
+        }
+    }
 }
 
 // dQ, as the forward kernel goes: S^T = K Q^T and dP^T = V dO^T with the lane's row in their columns, dQ^T += K^T dS^T
@@ -242,10 +276,11 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
     for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
     if (PAD) attn_zero(smem, sizeof(smem), 256);
     const int n = (keys + KEYS - 1) / KEYS;
+    const AttnLoad<DP, PAD, KEYS, BWD_WAVES> load_k(K, p.f.ldk, wave, lane, p.f.D), load_v(V, p.f.ldv, wave, lane, p.f.D);
     const auto load = [&](int j) {
         unsigned char *at = smem + (j & 1) * 2 * TILE;
-        attn_load_tile<DP, PAD, KEYS, BWD_WAVES>(K, p.f.ldk, j * KEYS, k.count, at, wave, lane, p.f.D);
-        attn_load_tile<DP, PAD, KEYS, BWD_WAVES>(V, p.f.ldv, j * KEYS, k.count, at + TILE, wave, lane, p.f.D);
+        load_k(j * KEYS, k.count, at, lane);
+        load_v(j * KEYS, k.count, at + TILE, lane);
     };
     if (n > 0) load(0);
     for (int j = 0; j < n; ++j) {
@@ -256,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
         unsigned char *at = smem + (j & 1) * 2 * TILE;
         if (k0 + KEYS > whole) {
             attn_clean(at + wave * (TILE / BWD_WAVES), TILE / BWD_WAVES, lane);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            attn_reads_done();
             attn_barrier();
         }
         if (k0 >= high) continue;
@@ -285,7 +320,10 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
         }
     }
     const int64_t at = (int64_t)q.begin + row;
-    bwd_store<DP, PAD>(dq, p.f.scale, p, p.cos, p.pos_q + at, p.dQ + at * p.lddq + (int64_t)head * p.f.D, row < q.count, h);
+    const bool there = row < q.count;
+    const int64_t angle = bwd_angle(p, p.pos_q + at, there);
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b) bwd_store<PAD>(dq[b], b, p.f.scale, p, p.cos, angle, p.dQ + at * p.lddq + (int64_t)head * p.f.D, there, h);
 }
 
 static int64_t delta_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tq * p.f.heads * (p.f.D > 64 ? 16 : 8) + 255) / 256; }
@@ -309,7 +347,7 @@ static hipError_t launch_bwd(const BwdParams &p, hipStream_t s)
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.f.Tk > 0) {
-        hipLaunchKernelGGL((attention_dkv_kernel<DP, PAD>), dim3((unsigned)dkv_workgroups(p)), dim3(256), 0, s, p, c);
+        hipLaunchKernelGGL((attention_dkv_kernel<DP, PAD, 2, DKV_NS>), dim3((unsigned)dkv_workgroups(p)), dim3(128 * DKV_NS), 0, s, p, c);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.f.Tq > 0) {

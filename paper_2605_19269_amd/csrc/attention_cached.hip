@@ -3,42 +3,59 @@
 // The rows of one key / value head are the tokens of a sequence times the query heads of the group, so that every key is read once for all of
 // them.  Bound by HBM for few rows: 4 D bytes a key and key / value head, and 4 D operations a key and row.
 //
-//  * Rows are cut into tiles of 32 (the workgroup's four waves take a quarter of the keys of a tile each, from LDS of their own, without a
-//    barrier, and are joined in LDS at the end) or of 128 (a wave has 32 rows, the keys are shared).
+//  * Rows are cut into tiles of 32 or 128.  With 32 (a few tokens) the workgroup's four waves take a quarter of the keys of a tile each, from LDS of their
+//    own without a barrier: four slots of K or V a wave, three of them on their way (24 KB a wave, 96 KB a CU) while one is read.  With 128 (trees) four
+//    waves have 32 rows each and share the keys, and the workgroup's two such groups take the halves of a tile of 128 keys.  At the end the waves of a row
+//    are joined in LDS.
 //  * The tiles of keys of all tiles of rows, laid end to end, are cut into equal ranges, a workgroup each: lengths may differ as they like and
-//    the host needs to know none of them.  A range that covers a tile of rows whole writes its outputs; otherwise fp32 partials go to slot
+//    the host needs to know none of them; a tile of rows counts for two or three steps more than it has, which is what a range loses between two (64 sequences' last workgroups
+//    ended 12 us behind the first without).  A range that covers a tile of rows whole writes its outputs; otherwise fp32 partials go to slot
 //    (range + number of the tile of rows), which no other pair has, since both only grow, and a second kernel joins them in order.
 #include "attn_launch.hpp"
 #include "attn_tile.hpp"
 
 namespace coda {
 
-constexpr int CACHED_WAVES = 4;
-
-template <int DP, bool SHARED>
+template <int DP, bool MANY>
 struct CachedTile {
-    static constexpr int ROWS = SHARED ? 128 : 32;
-    static constexpr int WAVE_KEYS = SHARED ? 64 : DP == 128 ? 32 : 64;             // keys of a wave's step
-    static constexpr int KEYS = SHARED ? 64 : CACHED_WAVES * WAVE_KEYS;             // of the workgroup's
-    static constexpr int TILE = WAVE_KEYS * DP * 2;                                // bytes of K, or of V
-    static constexpr int LDS = (SHARED ? 1 : CACHED_WAVES) * 4 * TILE;
-    static constexpr int LOAD_WAVES = SHARED ? CACHED_WAVES : 1;
-    static constexpr int LOADS = TILE / 1024 / LOAD_WAVES;
+    static constexpr int GROUP = MANY ? 4 : 1;             // waves that share their keys
+    static constexpr int GROUPS = MANY ? 2 : 4;            // of the workgroup
+    static constexpr int WAVES = GROUP * GROUPS;
+    static constexpr int ROWS = GROUP * 32;
+    static constexpr int WAVE_KEYS = MANY || DP == 64 ? 64 : 32;
+    static constexpr int KEYS = GROUPS * WAVE_KEYS;        // of a step of the workgroup
+    static constexpr int TILE = WAVE_KEYS * DP * 2;        // bytes of K, or of V, of a group
+    static constexpr int LDS = GROUPS * 4 * TILE;
+    static constexpr int LOADS = TILE / 1024 / GROUP;      // 1 KB each, of a wave
+    static constexpr int RESTART = MANY ? 3 : 2;           // steps that a range's next tile of rows costs on top of its own
+    static constexpr int UNITS = DP / 8;                   // fours of columns that a lane holds; each wave finishes UNITS / GROUPS of them
+    static constexpr int PART = (MANY ? UNITS * 1024 : 4 * TILE) / 16;              // from one wave's part to the next, in fours: a lone wave's takes the place of its tiles
+    static_assert(WAVES * PART * 16 <= LDS && UNITS * 64 <= PART, "the parts of all waves take the place of the tiles");
 };
+constexpr int CACHED_SEQS = 256;                           // sequences kept in LDS
 
+// Numbers of tiles of rows, as attn_find() counts them
+__host__ __device__ __forceinline__ int64_t cached_items(int64_t Tq, int n_seqs, int group, bool many) { return Tq * group / (many ? 128 : 32) + n_seqs; }
 struct CachedSeq {
     int q0, nq, len, tiles, steps;     // first row, rows, keys, tiles of rows, tiles of keys
 };
+__device__ __forceinline__ CachedSeq cached_seq_of(const CachedParams &p, int q0, int nq, int len, int rows, int keys)
+{
+    return {q0, nq, len, (int)(((int64_t)nq * p.group + rows - 1) / rows), max(1, (len + keys - 1) / keys)};
+}
 __device__ __forceinline__ CachedSeq cached_seq(const CachedParams &p, int s, int rows, int keys)
 {
     const AttnSpan q = attn_span(p.seq_q, s, p.Tq);
-    const int len = min(max(p.lens[s], 0), p.capacity);
-    const int tiles = (int)(((int64_t)q.count * p.group + rows - 1) / rows);
-    return {q.begin, q.count, len, tiles, max(1, (len + keys - 1) / keys)};
+    return cached_seq_of(p, q.begin, q.count, min(max(p.lens[s], 0), p.capacity), rows, keys);
 }
 __device__ __forceinline__ int64_t cached_item(const CachedParams &p, const CachedSeq &q, int s, int rows) { return (int64_t)q.q0 * p.group / rows + s; }
 
-// Sum over the workgroup's 256 threads of each one's value, and of those before it
+__device__ __forceinline__ int64_t cached_uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+}
+// Sum over the workgroup's threads of each one's value, and of those before it
+template <int WAVES>
 __device__ __forceinline__ int64_t cached_scan(int64_t v, int64_t *part, int64_t &before)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -48,47 +65,71 @@ __device__ __forceinline__ int64_t cached_scan(int64_t v, int64_t *part, int64_t
         const int64_t o = __shfl_up(run, off, 64);
         if (lane >= off) run += o;
     }
-    __syncthreads();
     if (lane == 63) part[wave] = run;
     __syncthreads();
     int64_t total = 0;
     before = run - v;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         if (w < wave) before += part[w];
         total += part[w];
     }
     return total;
 }
 
-template <int DP, bool PAD, bool SHARED>
-__global__ __launch_bounds__(256, SHARED ? 2 : 1) void attention_cached_kernel(CachedParams p, float c)
+template <int DP, bool PAD, bool MANY>
+__global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) void attention_cached_kernel(CachedParams p, float c)
 {
-    typedef CachedTile<DP, SHARED> C;
+    typedef CachedTile<DP, MANY> C;
+    constexpr int THREADS = C::WAVES * 64, CH = DP / 8, RPL = 64 / CH, NB = C::WAVE_KEYS / 32;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[C::LDS];
-    __shared__ float stats[2][CACHED_WAVES][32];
-    __shared__ int64_t part[4], found[2];
+    __shared__ int32_t ids[C::WAVES][4][64];               // pages of the keys of four steps
+    __shared__ uint64_t rows_at[C::WAVES][64];
+    __shared__ float stats[2][C::GROUPS][C::ROWS];
+    __shared__ int32_t seqs[CACHED_SEQS][3];
+    __shared__ int64_t part[C::WAVES], found[2];
     __shared__ int dirty;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int member = wave % C::GROUP, kg = wave / C::GROUP;
     const int kv = blockIdx.x % p.kv_heads, range = blockIdx.x / p.kv_heads;
 
     // This workgroup's range, and the sequence that it begins in
+    const auto cost_of = [](const CachedSeq &q) { return (int64_t)q.tiles * (q.steps + C::RESTART); };
     int64_t mine = 0, before;
-    const int each = (p.n_seqs + 255) / 256, s0 = min((int)threadIdx.x * each, p.n_seqs), s1 = min(s0 + each, p.n_seqs);
+    const int each = (p.n_seqs + THREADS - 1) / THREADS, s0 = min((int)threadIdx.x * each, p.n_seqs), s1 = min(s0 + each, p.n_seqs);
     for (int s = s0; s < s1; ++s) {
         const CachedSeq q = cached_seq(p, s, C::ROWS, C::KEYS);
-        mine += (int64_t)q.tiles * q.steps;
+        mine += cost_of(q);
+        if (s < CACHED_SEQS) {
+            seqs[s][0] = q.q0;
+            seqs[s][1] = q.nq;
+            seqs[s][2] = q.len;
+        }
     }
-    const int64_t total = cached_scan(mine, part, before);
+    const int64_t total = cached_uniform(cached_scan<C::WAVES>(mine, part, before));
     const int64_t ranges = min((int64_t)p.ranges, total);
+    if (blockIdx.x == 0) {                                 // numbers that no tile of rows has
+        const int64_t items = cached_items(p.Tq, p.n_seqs, p.group, MANY);
+        for (int s = s0; s < s1; ++s) {
+            const CachedSeq q = cached_seq(p, s, C::ROWS, C::KEYS);
+            const int64_t next = s + 1 < p.n_seqs ? min(items, cached_item(p, cached_seq(p, s + 1, C::ROWS, C::KEYS), s + 1, C::ROWS)) : items;
+            for (int64_t i = cached_item(p, q, s, C::ROWS) + q.tiles; i < next; ++i) p.spans[i].parts = 0;
+            if (s == 0)
+                for (int64_t i = 0; i < cached_item(p, q, 0, C::ROWS); ++i) p.spans[i].parts = 0;
+        }
+    }
     if (range >= ranges) return;
     int64_t at = range * total / ranges;
     const int64_t end = (range + 1) * total / ranges;
+    const auto sequence = [&](int s) {
+        if (s >= CACHED_SEQS) return cached_seq(p, s, C::ROWS, C::KEYS);
+        return cached_seq_of(p, __builtin_amdgcn_readfirstlane(seqs[s][0]), __builtin_amdgcn_readfirstlane(seqs[s][1]), __builtin_amdgcn_readfirstlane(seqs[s][2]),
+                             C::ROWS, C::KEYS);
+    };
     if (before <= at && at < before + mine) {
         int s = s0;
         for (;; ++s) {
-            const CachedSeq q = cached_seq(p, s, C::ROWS, C::KEYS);
-            const int64_t cost = (int64_t)q.tiles * q.steps;
+            const int64_t cost = cost_of(cached_seq(p, s, C::ROWS, C::KEYS));
             if (at < before + cost) break;
             before += cost;
         }
@@ -96,24 +137,32 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void attention_cached_kernel(C
         found[1] = before;
     }
     __syncthreads();
-    int s = (int)found[0];
-    int64_t base = found[1];
+    int s = __builtin_amdgcn_readfirstlane((int)found[0]);
+    int64_t base = cached_uniform(found[1]);
 
     while (at < end) {
-        const CachedSeq seq = cached_seq(p, s, C::ROWS, C::KEYS);
-        const int64_t cost = (int64_t)seq.tiles * seq.steps;
-        if (at >= base + cost) {
-            base += cost;
+        const CachedSeq seq = sequence(s);
+        if (at >= base + cost_of(seq)) {
+            base += cost_of(seq);
             ++s;
             continue;
         }
-        const int tile = (int)((at - base) / seq.steps), j0 = (int)((at - base) % seq.steps), j1 = (int)min((int64_t)seq.steps, j0 + (end - at));
-        at += j1 - j0;
+        const int length = seq.steps + C::RESTART;         // of a tile of rows: its restart, then its steps
+        const int tile = __builtin_amdgcn_readfirstlane((int)((at - base) / length)), from = __builtin_amdgcn_readfirstlane((int)(at - base - (int64_t)tile * length));
+        const int to_step = __builtin_amdgcn_readfirstlane((int)min((int64_t)length, from + (end - at)));
+        const int j0 = max(0, from - C::RESTART), j1 = to_step - C::RESTART;
+        at += to_step - from;
+        if (j1 <= 0) continue;                             // the range ends ahead of the first step
+        const int64_t item = cached_item(p, seq, s, C::ROWS) + tile;
+        if (j0 == 0 && kv == 0 && threadIdx.x == 0) {      // the last step's range is the last that begins at or before it, at floor(range * total / ranges)
+            const int last = j1 == seq.steps ? range : (int)(((base + (int64_t)(tile + 1) * length) * ranges - 1) / total);
+            p.spans[item] = {range, last - range + 1, seq.q0, tile * C::ROWS, seq.nq * p.group};
+        }
         __syncthreads();                                   // the LDS of the range's last piece is free
         if (threadIdx.x == 0) dirty = 0;
-        if (PAD) attn_zero(smem, sizeof(smem), 256);
+        if (PAD) attn_zero(smem, sizeof(smem), THREADS);
 
-        const int nrows = seq.nq * p.group, row0 = tile * C::ROWS + (SHARED ? wave * 32 : 0);
+        const int nrows = seq.nq * p.group, row0 = tile * C::ROWS + member * 32;
         const int row = row0 + (lane & 31), last = min(row, nrows - 1);
         const int token = last / p.group, head = kv * p.group + last % p.group;
         const uint16_t *Q = p.Q + (int64_t)(seq.q0 + token) * p.ldq + (int64_t)head * p.D;
@@ -136,225 +185,281 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void attention_cached_kernel(C
             return bool((int)(k < lim) | (int)((word >> (d & 31)) & (uint32_t)(d < 64u)));
         };
 
-        unsigned char *own = smem + (SHARED ? 0 : wave * 4 * C::TILE);
+        const int64_t head_at = (((int64_t)kv << p.page_bits) * p.D) * 2;
+        const unsigned char *K = reinterpret_cast<const unsigned char *>(p.K) + head_at, *V = reinterpret_cast<const unsigned char *>(p.V) + head_at;
+        unsigned char *own = smem + kg * 4 * C::TILE;      // the group's four slots
         const int32_t *table = p.table + (int64_t)s * p.ld_table;
-        const auto first_key = [&](int j) { return j * C::KEYS + (SHARED ? 0 : wave * C::WAVE_KEYS); };
-        constexpr int CH = DP / 8, RPL = 64 / CH;
-        const auto tile_row = [&](int i) { return (i * C::LOAD_WAVES + (SHARED ? wave : 0)) * RPL + lane / CH; };
-        // The pages of the rows that this lane loads, a step ahead of the loads
-        int32_t page[C::LOADS];
-        const auto look_up = [&](int j) {
-#pragma unroll
-            for (int i = 0; i < C::LOADS; ++i) {
-                const int key = max(0, min(first_key(j) + tile_row(i), seq.len - 1));
-                page[i] = table[key >> p.page_bits];
-            }
+        const auto first_key = [&](int j) { return j * C::KEYS + kg * C::WAVE_KEYS; };
+        const auto clamped = [&](int k) { return max(0, min(k, seq.len - 1)); };
+        const auto tile_row = [&](int i) { return (i * C::GROUP + member) * RPL + lane / CH; };
+        const auto lane_chunk = [&](int i) { return (lane % CH) ^ attn_swizzle<DP>(tile_row(i)); };
+        // Where the rows of a step's keys begin in the cache: a lane finds that of one key and leaves it in LDS for the lanes that load
+        const auto find_rows = [&](int j) {
+            const uint64_t pg = (uint64_t)(uint32_t)min(max(ids[wave][j & 3][lane], 0), p.pages - 1);
+            rows_at[wave][lane] = pg * p.page_bytes + ((uint32_t)clamped(first_key(j) + lane) & p.page_mask) * (uint32_t)(p.D * 2);
+            __builtin_amdgcn_wave_barrier();               // a wave's LDS operations stay in order
         };
-        const auto load = [&](const uint16_t *cache, int j, unsigned char *to) {
+        const auto load = [&](const unsigned char *cache, unsigned char *to) {
 #pragma unroll
-            for (int i = 0; i < C::LOADS; ++i) {
-                const int r = tile_row(i), ch = (lane % CH) ^ attn_swizzle<DP>(r);
-                const int key = max(0, min(first_key(j) + r, seq.len - 1));
-                const int64_t pg = min(max(page[i], 0), p.pages - 1);
-                const uint16_t *from = cache + ((((pg * p.kv_heads + kv) << p.page_bits) + (key & ((1 << p.page_bits) - 1))) * p.D + ch * 8);
-                if (!PAD || ch * 8 < p.D) attn_load16(from, __builtin_amdgcn_readfirstlane(attn_lds(to) + (i * C::LOAD_WAVES + (SHARED ? wave : 0)) * 1024));
-            }
+            for (int i = 0; i < C::LOADS; ++i)
+                if (!PAD || lane_chunk(i) * 8 < p.D)
+                    attn_load16(cache + lane_chunk(i) * 16 + rows_at[wave][tile_row(i)], __builtin_amdgcn_readfirstlane(attn_lds(to) + (i * C::GROUP + member) * 1024));
         };
+        // V's tiles that are cleaned: masked ones, and where groups wait for each other also what lies beside one
+        const auto cleaned = [&](int j) { return (MANY ? j * C::KEYS + C::KEYS : first_key(j) + C::WAVE_KEYS) > whole; };
         AttnRows<DP> acc;
         acc.clear();
         bool bad = false;
         if (seq.len > 0) {
-            look_up(j0);
-            load(p.K, j0, own);
-            load(p.V, j0, own + C::TILE);
-            if (j0 + 1 < j1) look_up(j0 + 1);
-            for (int j = j0; j < j1; ++j) {
-                unsigned char *now = own + ((j - j0) & 1) * 2 * C::TILE, *next = own + ((j - j0 + 1) & 1) * 2 * C::TILE;
-                attn_wait();
-                if (SHARED) attn_barrier();
-                if (j + 1 < j1) {
-                    load(p.K, j + 1, next);
-                    load(p.V, j + 1, next + C::TILE);
-                    if (j + 2 < j1) look_up(j + 2);
-                }
-                const int k0 = first_key(j);
-                const bool masked = k0 + C::WAVE_KEYS > whole;
-                if (masked) {
-                    constexpr int PART = C::TILE / C::LOAD_WAVES;
-                    if (attn_clean(now + C::TILE + (SHARED ? wave * PART : 0), PART, lane)) {
-                        bad = true;
-                        if (SHARED) dirty = 1;
-                    }
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    if (SHARED) attn_barrier();
-                }
-                if (k0 >= seq.len || row0 >= nrows) continue;
-                attn_step<DP, C::WAVE_KEYS / 32>(now, now + C::TILE, qf, acc, c, lane, masked, [&](int k) { return sees(k0 + k); });
-            }
+            // Four slots: step j has K in slot 2 j % 4 and V in the next.  The pages of a step's keys come to LDS steps ahead.  Loads arrive in order, so a
+            // wait says how many of the later ones may be on their way.
+            constexpr int L = C::LOADS;
+            const auto slot = [&](int j, int v) { return own + ((2 * (j - j0) + v) & 3) * C::TILE; };
+            const auto fetch_ids = [&](int j) {
+                attn_load4(table + (clamped(first_key(j) + lane) >> p.page_bits), __builtin_amdgcn_readfirstlane(attn_lds(reinterpret_cast<unsigned char *>(ids[wave][j & 3]))));
+            };
+            const auto fetch = [&](const unsigned char *cache, int j, int v) { load(cache, slot(j, v)); };
+            fetch_ids(j0);
+            fetch_ids(j0 + 1);
             attn_wait();
-            if (SHARED) {
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) asm volatile("" : "+v"(qf[i]));      // the compiler waits for Q here, and not behind the loads of K and V
+            asm volatile("" : : "v"(bits0), "v"(bits1));
+            find_rows(j0);
+            fetch(K, j0, 0);
+            fetch_ids(j0 + 2);
+            fetch(V, j0, 1);
+            if (j0 + 1 < j1) {
+                find_rows(j0 + 1);
+                fetch(K, j0 + 1, 0);
+                fetch_ids(j0 + 3);
+                if (!MANY) fetch(V, j0 + 1, 1);
+            }
+            for (int j = j0; j < j1; ++j) {
+                const int k0 = first_key(j);
+                const bool here = k0 < seq.len && row0 < nrows;                    // the last step's keys may leave nothing for this wave
+                const bool masked = k0 + C::WAVE_KEYS > whole;
+                f32x16 sc[NB];
+                bf16x8 w[2 * NB];
+                const auto see = [&](int k) { return sees(k0 + k); };
+                if constexpr (MANY) {
+                    // Two barriers a step: K of j is there and V of j - 1 read, V of j + 1 may come; V of j is there and K of j read, K of j + 2 may come
+                    if (j + 1 < j1) attn_wait_but<2 * L + 2>();                    // pages, V, K, pages are to come
+                    else attn_wait_but<L + 1>();
+                    attn_reads_done();
+                    attn_barrier();
+                    if (j + 1 < j1) fetch(V, j + 1, 1);
+                    if (here) {
+                        attn_scores<DP, NB, 4>(slot(j, 0), qf, sc, lane);
+                        attn_weights<DP, NB>(sc, w, acc, c, lane, masked, see);
+                    }
+                    if (j + 1 < j1) attn_wait_but<2 * L + 1>();                    // K, pages, V are to come
+                    else attn_wait_but<0>();
+                    attn_reads_done();
+                    attn_barrier();
+                    if (j + 2 < j1) {
+                        find_rows(j + 2);
+                        fetch(K, j + 2, 0);
+                        fetch_ids(j + 4);
+                    }
+                    if (cleaned(j)) {
+                        constexpr int PART = C::TILE / C::GROUP;
+                        if (attn_clean(slot(j, 1) + member * PART, PART, lane)) dirty = 1;
+                        attn_reads_done();
+                        attn_barrier();
+                    }
+                    if (here) attn_values<DP, NB, 4>(slot(j, 1), w, acc, lane);
+                } else {
+                    if (j + 1 < j1) attn_wait_but<3 * L + 1>();                    // K and the pages of step j + 2 are there; V, K, pages, V are to come
+                    else attn_wait_but<L>();
+                    attn_scores<DP, NB, 4>(slot(j, 0), qf, sc, lane);
+                    attn_reads_done();
+                    if (j + 2 < j1) {
+                        find_rows(j + 2);
+                        fetch(K, j + 2, 0);
+                        fetch_ids(j + 4);
+                    }
+                    if (here) attn_weights<DP, NB>(sc, w, acc, c, lane, masked, see);
+                    if (j + 2 < j1) attn_wait_but<3 * L + 2>();                    // V is there; K, pages, V, K, pages are to come
+                    else if (j + 1 < j1) attn_wait_but<2 * L + 1>();
+                    else attn_wait_but<0>();
+                    if (here) {
+                        if (cleaned(j)) {
+                            if (attn_clean(slot(j, 1), C::TILE, lane)) bad = true;
+                            attn_reads_done();
+                        }
+                        attn_values<DP, NB, 4>(slot(j, 1), w, acc, lane);
+                    }
+                    attn_reads_done();
+                    if (j + 2 < j1) fetch(V, j + 2, 1);
+                }
+            }
+            if (MANY) {
                 __syncthreads();
                 bad = dirty != 0;
             }
             if (bad)
-                for (int j = max(j0, (whole - (SHARED ? 0 : wave * C::WAVE_KEYS)) / C::KEYS); j < j1; ++j) {
+                for (int j = j0; j < j1; ++j) {
+                    if (!cleaned(j)) continue;
                     const int k0 = first_key(j);
-                    if (k0 + C::WAVE_KEYS <= whole) continue;
-                    look_up(j);
-                    load(p.V, j, own);
+                    fetch_ids(j);
                     attn_wait();
-                    if (SHARED) attn_barrier();
+                    find_rows(j);
+                    load(V, own);
+                    attn_wait();
+                    if (MANY) attn_barrier();
                     attn_add_marks<DP, C::WAVE_KEYS / 16>(own, acc.o, lane, [&](int k) { return sees(k0 + k); });
-                    attn_wait();
-                    if (SHARED) attn_barrier();
+                    attn_reads_done();
+                    if (MANY) attn_barrier();
                 }
         }
+        // The groups' parts of each row side by side in LDS; then each wave joins UNITS / GROUPS of the fours of columns of its rows
         const f32x2 halves = attn_halves(acc.l);
-        acc.l = halves[0] + halves[1];
-        acc.m *= c;                                        // log2 units from here on
-        const bool partial = j0 > 0 || j1 < seq.steps;
+        f32x4 *parts = reinterpret_cast<f32x4 *>(smem) + lane;
+        if (MANY) __syncthreads();                         // tiles are shared
+#pragma unroll
+        for (int u = 0; u < C::UNITS; ++u) {
+            const f32x16 &o = acc.o[u / 4];
+            const int g = u % 4 * 4;
+            parts[wave * C::PART + u * 64] = f32x4{o[g], o[g + 1], o[g + 2], o[g + 3]};
+        }
+        if (h == 0) {
+            stats[0][kg][member * 32 + lane] = acc.m * c;  // log2 units from here on
+            stats[1][kg][member * 32 + lane] = halves[0] + halves[1];
+        }
+        __syncthreads();
+        float m = -__builtin_inff(), l = 0.0f, w[C::GROUPS];
+#pragma unroll
+        for (int i = 0; i < C::GROUPS; ++i) m = fmaxf(m, stats[0][i][member * 32 + (lane & 31)]);
+        const float ms = m == -__builtin_inff() ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < C::GROUPS; ++i) {
+            w[i] = __builtin_amdgcn_exp2f(stats[0][i][member * 32 + (lane & 31)] - ms);
+            l += w[i] * stats[1][i][member * 32 + (lane & 31)];
+        }
+        const bool partial = j0 > 0 || j1 < seq.steps, there = row < nrows, none = m == -__builtin_inff() && l == 0.0f;
+        const float inv = partial ? 1.0f : none ? 0.0f : 1.0f / l;
         float *to = nullptr;
-        if (partial) to = p.part + ((range + cached_item(p, seq, s, C::ROWS) + tile) * p.kv_heads + kv) * (C::ROWS * (DP + 2));
-        if (!SHARED) {
-            // The four waves' outputs [DP][32] side by side in LDS; then a thread joins DP / 8 columns of one row
-            float *o = reinterpret_cast<float *>(own);
+        if (partial) to = p.part + ((range + item) * p.kv_heads + kv) * (C::ROWS * (DP + 2));
+        if (there && h == 0 && kg == 0) {
+            if (partial) {
+                to[member * 32 + lane] = m;
+                to[C::ROWS + member * 32 + lane] = l;
+            } else if (p.lse)
+                p.lse[(int64_t)head * p.Tq + seq.q0 + token] = none ? -__builtin_inff() : LN2 * (m + __builtin_amdgcn_logf(l));
+        }
+        uint16_t *out = p.out + (int64_t)(seq.q0 + token) * p.ldo + (int64_t)head * p.D;
+        constexpr int OWN = C::UNITS / C::GROUPS;
+        static_assert(OWN % 2 == 0, "pairs of fours make 16 bytes of output");
 #pragma unroll
-            for (int b = 0; b < DP / 32; ++b)
+        for (int u = 0; u < OWN; u += 2) {
+            float v[2][4];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[(b * 32 + attn_acc_row(r, h)) * 32 + (lane & 31)] = acc.o[b][r];
-            if (h == 0) {
-                stats[0][wave][lane] = acc.m;
-                stats[1][wave][lane] = acc.l;
-            }
-            __syncthreads();
-            const int r = threadIdx.x & 31, d0 = (threadIdx.x >> 5) * (DP / 8);
-            float m = stats[0][0][r], l = 0.0f, w[CACHED_WAVES], v[DP / 8];
+            for (int i = 0; i < 2; ++i) {
+                f32x4 sum = {};
 #pragma unroll
-            for (int i = 1; i < CACHED_WAVES; ++i) m = fmaxf(m, stats[0][i][r]);
-            const float ms = m == -__builtin_inff() ? 0.0f : m;
+                for (int k = 0; k < C::GROUPS; ++k) {
+                    const f32x4 x = parts[(k * C::GROUP + member) * C::PART + (kg * OWN + u + i) * 64];
 #pragma unroll
-            for (int i = 0; i < CACHED_WAVES; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(stats[0][i][r] - ms);
-                l += w[i] * stats[1][i][r];
-            }
-#pragma unroll
-            for (int d = 0; d < DP / 8; ++d) {
-                v[d] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < CACHED_WAVES; ++i) v[d] += w[i] * reinterpret_cast<const float *>(smem + i * 4 * C::TILE)[(d0 + d) * 32 + r];
-            }
-            const bool there = tile * C::ROWS + r < nrows;
-            const bool none = m == -__builtin_inff() && l == 0.0f;
-            const float inv = none ? 0.0f : 1.0f / l;
-            if (there && partial) {
-                if (d0 == 0) {
-                    to[r] = m;
-                    to[C::ROWS + r] = l;
+                    for (int e = 0; e < 4; ++e) sum[e] += w[k] * x[e];
                 }
-                float *po = to + 2 * C::ROWS + r * DP + d0;
 #pragma unroll
-                for (int d = 0; d < DP / 8; d += 4) *reinterpret_cast<f32x4 *>(po + d) = f32x4{v[d], v[d + 1], v[d + 2], v[d + 3]};
-            } else if (there) {                            // r is this lane's row as above: token and head are its
-                if (d0 == 0 && p.lse) p.lse[(int64_t)head * p.Tq + seq.q0 + token] = none ? -__builtin_inff() : LN2 * (m + __builtin_amdgcn_logf(l));
-                uint16_t *out = p.out + (int64_t)(seq.q0 + token) * p.ldo + (int64_t)head * p.D;
-#pragma unroll
-                for (int d = 0; d < DP / 8; d += 8) {
-                    u32x4 u;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) u[e] = attn_pack(v[d + 2 * e] * inv, v[d + 2 * e + 1] * inv);
-                    if (!PAD || d0 + d < p.D) *reinterpret_cast<u32x4 *>(out + d0 + d) = u;
-                }
+                for (int e = 0; e < 4; ++e) v[i][e] = sum[e] * inv;
             }
-        } else {
-            const bool there = row < nrows;
-            const bool none = acc.m == -__builtin_inff() && acc.l == 0.0f;
-            const float inv = partial ? 1.0f : none ? 0.0f : 1.0f / acc.l;
-            if (there && h == 0) {
-                if (partial) {
-                    to[wave * 32 + lane] = acc.m;
-                    to[C::ROWS + wave * 32 + lane] = acc.l;
-                } else if (p.lse)
-                    p.lse[(int64_t)head * p.Tq + seq.q0 + token] = none ? -__builtin_inff() : LN2 * (acc.m + __builtin_amdgcn_logf(acc.l));
-            }
-            uint16_t *out = p.out + (int64_t)(seq.q0 + token) * p.ldo + (int64_t)head * p.D;
-#pragma unroll
-            for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-                for (int g = 0; g < 4; g += 2) {
-                    float lo[4], hi[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        lo[e] = acc.o[b][4 * g + e] * inv;
-                        hi[e] = acc.o[b][4 * g + 4 + e] * inv;
-                    }
-                    if (partial) {
-                        float *po = to + 2 * C::ROWS + (wave * 32 + (lane & 31)) * DP + 32 * b + 8 * g + 4 * h;
-                        if (there) {
-                            *reinterpret_cast<f32x4 *>(po) = f32x4{lo[0], lo[1], lo[2], lo[3]};
-                            *reinterpret_cast<f32x4 *>(po + 8) = f32x4{hi[0], hi[1], hi[2], hi[3]};
-                        }
-                    } else {
-                        const u32x4 u = attn_store_unit(lo, hi);
-                        const int d = 32 * b + 8 * (g + h);
-                        if (there && (!PAD || d < p.D)) *reinterpret_cast<u32x4 *>(out + d) = u;
-                    }
+            const int f = 2 * (kg * OWN + u);              // unit (kg OWN + u), half h: four f + h of the row's columns
+            if (partial) {
+                f32x4 *po = reinterpret_cast<f32x4 *>(to + 2 * C::ROWS) + (f + h) * C::ROWS + member * 32 + (lane & 31);
+                if (there) {
+                    po[0] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
+                    po[2 * C::ROWS] = f32x4{v[1][0], v[1][1], v[1][2], v[1][3]};
                 }
+            } else {
+                const u32x4 o = attn_store_unit(v[0], v[1]);
+                const int d = 4 * f + 8 * h;
+                if (there && (!PAD || d < p.D)) *reinterpret_cast<u32x4 *>(out + d) = o;
+            }
         }
     }
 }
 
-// Joins the partials of the tiles of rows that more than one range had a part of.  A wave has a row, a lane DP / 64 columns.
-template <int DP, bool SHARED>
+// Joins the partials of the tiles of rows that more than one range had a part of, in the order of the ranges.  They lie [slot][kv head]: the rows' maxima and
+// sums, then [DP / 4][rows] fours of columns.  A workgroup has 32 rows and 4 FOURS columns; its eight half waves take every eighth partial, all columns at once, since
+// a trip to memory is what this kernel takes its time for, and are added up in LDS four fours at a time.
+template <int DP, bool MANY, int FOURS>
 __global__ __launch_bounds__(256) void attention_join_kernel(CachedParams p)
 {
-    typedef CachedTile<DP, SHARED> C;
-    __shared__ int64_t part[4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    typedef CachedTile<DP, MANY> C;
+    __shared__ f32x4 sums[8][4][32];
+    __shared__ float stats[2][8][32];
+    const int r = threadIdx.x & 31, part = threadIdx.x >> 5;
     const int64_t item = blockIdx.x / p.kv_heads;
     const int kv = blockIdx.x % p.kv_heads;
-    const int s = attn_find(p.seq_q, p.n_seqs, p.group, C::ROWS, item, lane);
-    const CachedSeq seq = cached_seq(p, s, C::ROWS, C::KEYS);
-    const int64_t tile = item - cached_item(p, seq, s, C::ROWS);
-    if (tile < 0 || tile >= seq.tiles) return;
-    const int r = (int)blockIdx.y * 4 + wave, row = (int)tile * C::ROWS + r;
-    if ((int)tile * C::ROWS + (int)blockIdx.y * 4 >= seq.nq * p.group) return;
-    int64_t mine = 0, ahead = 0, unused;
-    for (int i = threadIdx.x; i < p.n_seqs; i += 256) {
-        const CachedSeq q = cached_seq(p, i, C::ROWS, C::KEYS);
-        const int64_t cost = (int64_t)q.tiles * q.steps;
-        mine += cost;
-        if (i < s) ahead += cost;
-    }
-    const int64_t total = cached_scan(mine, part, unused), ranges = min((int64_t)p.ranges, total);
-    const int64_t first = cached_scan(ahead, part, unused) + tile * seq.steps;
-    // the range that holds step x is the last that begins at or before it, at floor(range * total / ranges)
-    const int64_t w0 = ((first + 1) * ranges - 1) / total, w1 = ((first + seq.steps) * ranges - 1) / total;
-    if (w0 == w1 || row >= seq.nq * p.group) return;
+    const CachedSpan span = p.spans[item];
+    // within the workspace and the outputs, whatever seq_q holds
+    const int w0 = min(max(span.first, 0), p.ranges - 1), n = min(span.parts, p.ranges - w0), q0 = min(max(span.q0, 0), p.Tq);
+    const int row0 = max(span.row, 0) + (int)blockIdx.y * 32, row = row0 + r, nrows = (int)min((int64_t)span.rows, ((int64_t)p.Tq - q0) * p.group);
+    if (n <= 1 || row0 >= nrows) return;
     const int64_t stride = (int64_t)p.kv_heads * (C::ROWS * (DP + 2));
-    const float *from = p.part + ((w0 + item) * p.kv_heads + kv) * (C::ROWS * (DP + 2));
-    const int n = (int)(w1 - w0 + 1);
-    float m = -__builtin_inff();
-    for (int i = lane; i < n; i += 64) m = fmaxf(m, from[i * stride + r]);
+    const float *from = p.part + ((w0 + item) * p.kv_heads + kv) * (C::ROWS * (DP + 2)) + blockIdx.y * 32 + r;
+    float m = -__builtin_inff(), l = 0.0f;
+    f32x4 v[FOURS] = {};
+    if (row < nrows) {
+#pragma unroll 2
+        for (int i = part; i < n; i += 8) {
+            const float mi = from[i * stride], li = from[i * stride + C::ROWS];
+            const f32x4 *o = reinterpret_cast<const f32x4 *>(from - r - blockIdx.y * 32 + i * stride + 2 * C::ROWS) + blockIdx.z * FOURS * C::ROWS + blockIdx.y * 32 + r;
+            const float top = fmaxf(m, mi), ms = top == -__builtin_inff() ? 0.0f : top;
+            const float a = __builtin_amdgcn_exp2f(m - ms), b = __builtin_amdgcn_exp2f(mi - ms);
+            m = top;
+            l = l * a + li * b;
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-    const float ms = m == -__builtin_inff() ? 0.0f : m;
-    float l = 0.0f, v[DP / 64] = {};
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-        const float w = __builtin_amdgcn_exp2f(from[i * stride + r] - ms);
-        l += w * from[i * stride + C::ROWS + r];
+            for (int u = 0; u < FOURS; ++u) {
+                const f32x4 x = o[u * C::ROWS];
 #pragma unroll
-        for (int d = 0; d < DP / 64; ++d) v[d] += w * from[i * stride + 2 * C::ROWS + r * DP + lane * (DP / 64) + d];
+                for (int e = 0; e < 4; ++e) v[u][e] = v[u][e] * a + x[e] * b;
+            }
+        }
     }
-    const bool none = m == -__builtin_inff() && l == 0.0f;
-    const float inv = none ? 0.0f : 1.0f / l;
-    const int token = seq.q0 + row / p.group, head = kv * p.group + row % p.group, col = lane * (DP / 64);
-    if (lane == 0 && p.lse) p.lse[(int64_t)head * p.Tq + token] = none ? -__builtin_inff() : LN2 * (m + __builtin_amdgcn_logf(l));
-    if (col >= p.D) return;
-    uint16_t *out = p.out + (int64_t)token * p.ldo + (int64_t)head * p.D + col;
-    const uint32_t u = attn_pack(v[0] * inv, v[DP / 64 - 1] * inv);
-    if (DP == 128) *reinterpret_cast<uint32_t *>(out) = u;
-    else *out = (uint16_t)u;
+    stats[0][part][r] = m;
+    stats[1][part][r] = l;
+    const int token = q0 + row / p.group, head = kv * p.group + row % p.group;
+    float w[8], inv = 0.0f;
+#pragma unroll
+    for (int z = 0; z < FOURS / 4; ++z) {
+        if (z) __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sums[part][u][r] = v[4 * z + u];
+        __syncthreads();
+        if (z == 0) {
+            m = stats[0][0][r];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) m = fmaxf(m, stats[0][i][r]);
+            const float ms = m == -__builtin_inff() ? 0.0f : m;
+            l = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(stats[0][i][r] - ms);
+                l += w[i] * stats[1][i][r];
+            }
+            const bool none = m == -__builtin_inff() && l == 0.0f;
+            inv = none ? 0.0f : 1.0f / l;
+            if (blockIdx.z == 0 && part == 0 && row < nrows && p.lse)
+                p.lse[(int64_t)head * p.Tq + token] = none ? -__builtin_inff() : LN2 * (m + __builtin_amdgcn_logf(l));
+        }
+        const int col = (blockIdx.z * FOURS + 4 * z + part) * 4;
+        if (part < 4 && row < nrows && col < p.D) {        // four half waves finish four columns each
+            f32x4 sum = {};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const f32x4 x = sums[i][part][r];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += w[i] * x[e];
+            }
+            typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+            *reinterpret_cast<u32x2 *>(p.out + (int64_t)token * p.ldo + (int64_t)head * p.D + col) =
+                u32x2{attn_pack(sum[0] * inv, sum[1] * inv), attn_pack(sum[2] * inv, sum[3] * inv)};
+        }
+    }
 }
 
 // 16 bytes of K and of V a thread
@@ -374,45 +479,51 @@ __global__ __launch_bounds__(256) void cache_store_kernel(const uint16_t *K, int
 }
 
 // Tiles of 128 rows once a sequence has more than 32 on average
-static bool cached_shared(int64_t Tq, int n_seqs, int group) { return Tq * group > 32 * (int64_t)n_seqs; }
-static int cached_ranges(int kv_heads, bool shared) { return ((shared ? 512 : 256) + kv_heads - 1) / kv_heads; }
-
-int64_t cached_items(int64_t Tq, int n_seqs, int group, bool shared) { return Tq * group / (shared ? 128 : 32) + n_seqs; }
+static bool cached_many(int64_t Tq, int n_seqs, int group) { return Tq * group > 32 * (int64_t)n_seqs; }
+// One workgroup for each CU
+static int cached_ranges(int kv_heads) { return (256 + kv_heads - 1) / kv_heads; }
+static int64_t cached_part_floats(int64_t Tq, int n_seqs, int kv_heads, int group, int D)
+{
+    const bool many = cached_many(Tq, n_seqs, group);
+    return (cached_items(Tq, n_seqs, group, many) + cached_ranges(kv_heads)) * kv_heads * ((many ? 128 : 32) * ((D > 64 ? 128 : 64) + 2));
+}
 
 size_t cached_bytes(int64_t Tq, int n_seqs, int heads, int kv_heads, int D)
 {
-    const int group = heads / kv_heads, DP = D > 64 ? 128 : 64;
-    const bool shared = cached_shared(Tq, n_seqs, group);
-    return (size_t)(cached_items(Tq, n_seqs, group, shared) + cached_ranges(kv_heads, shared)) * kv_heads * ((shared ? 128 : 32) * (DP + 2) * 4);
+    const int group = heads / kv_heads;
+    return (size_t)cached_part_floats(Tq, n_seqs, kv_heads, group, D) * 4 + (size_t)cached_items(Tq, n_seqs, group, cached_many(Tq, n_seqs, group)) * sizeof(CachedSpan);
 }
 
 int64_t cached_workgroups(const CachedParams &p)
 {
-    const bool shared = cached_shared(p.Tq, p.n_seqs, p.group);
-    const int64_t join = cached_items(p.Tq, p.n_seqs, p.group, shared) * p.kv_heads * (shared ? 32 : 8);
-    const int64_t main = (int64_t)cached_ranges(p.kv_heads, shared) * p.kv_heads;
+    const bool many = cached_many(p.Tq, p.n_seqs, p.group);
+    const int64_t join = cached_items(p.Tq, p.n_seqs, p.group, many) * p.kv_heads * (many ? 4 : 1) * 8, main = (int64_t)cached_ranges(p.kv_heads) * p.kv_heads * 2;
     return join > main ? join : main;
 }
 
-template <int DP, bool PAD>
+template <int DP, bool PAD, bool MANY>
 static hipError_t launch_cached(CachedParams p, hipStream_t s)
 {
-    const bool shared = cached_shared(p.Tq, p.n_seqs, p.group);
-    p.ranges = cached_ranges(p.kv_heads, shared);
-    const float c = p.scale * LOG2E;
-    const dim3 grid((unsigned)(p.ranges * p.kv_heads)), join((unsigned)(cached_items(p.Tq, p.n_seqs, p.group, shared) * p.kv_heads), shared ? 32 : 8);
-    if (shared) {
-        hipLaunchKernelGGL((attention_cached_kernel<DP, PAD, true>), grid, dim3(256), 0, s, p, c);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((attention_join_kernel<DP, true>), join, dim3(256), 0, s, p);
-    } else {
-        hipLaunchKernelGGL((attention_cached_kernel<DP, PAD, false>), grid, dim3(256), 0, s, p, c);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((attention_join_kernel<DP, false>), join, dim3(256), 0, s, p);
-    }
+    p.ranges = cached_ranges(p.kv_heads);
+    p.spans = reinterpret_cast<CachedSpan *>(p.part + cached_part_floats(p.Tq, p.n_seqs, p.kv_heads, p.group, p.D));
+    hipLaunchKernelGGL((attention_cached_kernel<DP, PAD, MANY>), dim3((unsigned)(p.ranges * p.kv_heads)), dim3(CachedTile<DP, MANY>::WAVES * 64), 0, s, p, p.scale * LOG2E);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    // 64 columns a workgroup where that leaves one for every CU, else 16
+    const int64_t tiles = cached_items(p.Tq, p.n_seqs, p.group, MANY) * p.kv_heads * (MANY ? 4 : 1);
+    dim3 join((unsigned)(tiles / (MANY ? 4 : 1)), MANY ? 4 : 1, DP / 16);
+    if (tiles >= 256) {
+        join.z = DP / 64;
+        hipLaunchKernelGGL((attention_join_kernel<DP, MANY, 16>), join, dim3(256), 0, s, p);
+    } else
+        hipLaunchKernelGGL((attention_join_kernel<DP, MANY, 4>), join, dim3(256), 0, s, p);
     return hipGetLastError();
+}
+
+template <int DP, bool PAD>
+static hipError_t launch_cached(const CachedParams &p, hipStream_t s)
+{
+    return cached_many(p.Tq, p.n_seqs, p.group) ? launch_cached<DP, PAD, true>(p, s) : launch_cached<DP, PAD, false>(p, s);
 }
 
 hipError_t launch_attention_cached(const CachedParams &p, hipStream_t s)

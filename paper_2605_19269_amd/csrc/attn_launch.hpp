@@ -36,6 +36,10 @@ int64_t bwd_workgroups(const BwdParams &p);
 size_t bwd_bytes(int64_t Tq, int heads);
 hipError_t launch_attention_bwd(const BwdParams &p, hipStream_t s);
 
+// Who has a part of a tile of rows: the first range and how many ranges; the sequence's first row of Q, the tile's first row and the sequence's number of rows (times the group)
+struct CachedSpan {
+    int32_t first, parts, q0, row, rows;
+};
 // Rows of Q over a paged cache
 struct CachedParams {
     const uint16_t *Q, *K, *V;         // K, V: [pages][kv_heads][page][D]
@@ -43,7 +47,9 @@ struct CachedParams {
     const int32_t *table, *lens, *seq_q;
     const uint64_t *tree;              // or null
     int n_seqs, kv_heads, group, D, Tq, page_bits, pages, capacity;   // capacity: keys that a row of the table has room for
-    int ranges;                        // set by the launch
+    uint32_t page_mask, page_bytes;    // page - 1, bytes of a page of all heads
+    int ranges;                        // this and spans: set by the launch
+    CachedSpan *spans;                 // of each tile of rows
     float scale;
     uint16_t *out;
     int64_t ldo;

@@ -41,33 +41,71 @@ __device__ __forceinline__ void attn_load16(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
+// The same from a uniform address and a lane's offset
+__device__ __forceinline__ void attn_load16(const void *uniform, uint32_t off, uint32_t lds)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(uniform);
+    const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
 __device__ __forceinline__ void attn_load4(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
 // All loads of this wave have arrived, all its LDS reads are done
 __device__ __forceinline__ void attn_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+// All but the last N of them
+template <int N>
+__device__ __forceinline__ void attn_wait_but()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void attn_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void attn_barrier()
 {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// Rows row0 .. row0 + ROWS - 1 (those from n on: row n - 1 again) of one head, `base` its element (0, 0), into a tile; the workgroup's NW
-// waves share the work.  PAD: D < DP, the chunks behind D are left as attn_zero() made them.
+// Tiles of ROWS rows of one head, loaded by NW waves together.  PAD: D < DP, the chunks behind D are left as attn_zero() made them.
 template <int DP, bool PAD, int ROWS, int NW>
-__device__ __forceinline__ void attn_load_tile(const uint16_t *base, int64_t ld, int row0, int n, unsigned char *tile, int wave, int lane, int D)
-{
-    constexpr int CH = DP / 8, RPL = 64 / CH;
+struct AttnLoad {
+    static constexpr int CH = DP / 8, RPL = 64 / CH, LOADS = ROWS / (NW * RPL);
     static_assert(ROWS % (NW * RPL) == 0, "whole wave-loads");
-#pragma unroll
-    for (int i = 0; i < ROWS / (NW * RPL); ++i) {
-        const int r = (i * NW + wave) * RPL + lane / CH;
-        const int c = (lane % CH) ^ attn_swizzle<DP>(r);
-        const int row = min(row0 + r, n - 1);
-        if (!PAD || c * 8 < D) attn_load16(base + row * ld + c * 8, __builtin_amdgcn_readfirstlane(attn_lds(tile) + (i * NW + wave) * 1024));
+    const uint16_t *base;              // element (0, 0) of the head's rows
+    int64_t ld;
+    int wave, D;
+    uint32_t off;                      // of the lane's chunk within its wave's loads
+
+    static __device__ __forceinline__ int chunk(int i, int wave, int lane) { return (lane % CH) ^ attn_swizzle<DP>((i * NW + wave) * RPL + lane / CH); }
+    __device__ __forceinline__ AttnLoad(const uint16_t *base, int64_t ld, int wave, int lane, int D)
+        : base(base), ld(ld), wave(wave), D(D), off((uint32_t)((lane / CH) * (int)ld + chunk(0, wave, lane) * 8) * 2)
+    {
     }
-}
+    // Rows row0 .. of n (those from n on: row n - 1 again).  Whole tiles take uniform addresses, one addition for a lane's 1 KB; a load's chunks are
+    // those of the first one but where four rows times the waves are fewer than the swizzle's 16: there two chunks to the side every other time.
+    __device__ __forceinline__ void operator()(int row0, int n, unsigned char *tile, int lane) const
+    {
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(attn_lds(tile) + wave * 1024);
+        if (row0 + ROWS <= n) {
+            const uint16_t *from = base + (int64_t)(row0 + wave * RPL) * ld;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                uint32_t o = off;
+                if (RPL * NW < 16 && (i & 1)) o += chunk(0, wave, lane) & 2 ? -32 : 32;
+                static_assert(RPL * NW >= 16 || (DP == 128 && NW == 2), "chunks of later loads");
+                if (!PAD || chunk(i, wave, lane) * 8 < D) attn_load16(from, o, lds + i * NW * 1024);
+                from += (int64_t)(NW * RPL) * ld;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int c = chunk(i, wave, lane), row = min(row0 + (i * NW + wave) * RPL + lane / CH, n - 1);
+                if (!PAD || c * 8 < D) attn_load16(base + row * ld + c * 8, lds + i * NW * 1024);
+            }
+        }
+    }
+};
 
 // Clears `bytes` (a multiple of 16) of LDS for PAD kernels, before their first tile
 __device__ __forceinline__ void attn_zero(unsigned char *p, int bytes, int threads)
@@ -212,22 +250,38 @@ struct AttnRows {
     }
 };
 
-// Keys of a tile (NB x 32 of them) for 32 rows: S^T, the softmax step, O^T += V^T P^T.  c = scale * log2(e) > 0.  `masked`: some position is not
-// visible; vis(k) says whether key k of the tile is, for the lane's row.  The maximum that the weights are taken relative to is renewed only
-// when some row's has grown by more than 2^8 in weight: weights up to 2^8 cost no accuracy in bf16 or fp32, and the 64 multiplications of O^T
-// fall away for nearly all tiles.
-template <int DP, int NB, class Vis>
-__device__ __forceinline__ void attn_step(const unsigned char *kt, const unsigned char *vt, const bf16x8 (&q)[DP / 16], AttnRows<DP> &rows, float c, int lane,
-                                          bool masked, Vis vis)
+// S^T of NB x 32 keys and 32 rows.  The operands are read a batch of BATCH ahead of their products: left to itself the compiler reads each one where it
+// is used and waits for it there.
+template <int DP, int NB, int BATCH>
+__device__ __forceinline__ void attn_scores(const unsigned char *kt, const bf16x8 (&q)[DP / 16], f32x16 (&s)[NB], int lane)
 {
-    const int h = lane >> 5;
-    f32x16 s[NB];
+    constexpr int T = DP / 16, N = T * NB / BATCH;         // batches; product i is step i / NB of block i % NB
+    static_assert(T * NB % BATCH == 0, "whole batches");
+    bf16x8 a[2][BATCH];
+    const auto read = [&](int n) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) a[n & 1][i] = attn_rows<DP>(kt, (n * BATCH + i) % NB * 32, (n * BATCH + i) / NB, lane);
+    };
+    read(0);
 #pragma unroll
     for (int b = 0; b < NB; ++b) s[b] = f32x16{};
 #pragma unroll
-    for (int t = 0; t < DP / 16; ++t)
+    for (int n = 0; n < N; ++n) {
+        if (n + 1 < N) read(n + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) s[b] = attn_mfma(attn_rows<DP>(kt, b * 32, t, lane), q[t], s[b]);
+        for (int i = 0; i < BATCH; ++i) s[(n * BATCH + i) % NB] = attn_mfma(a[n & 1][i], q[(n * BATCH + i) / NB], s[(n * BATCH + i) % NB]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+// The softmax step: scores to weights, rounded, and the rows' maxima and sums.  c = scale * log2(e) > 0.  `masked`: some position is not visible;
+// vis(k) says whether key k of the tile is, for the lane's row.  The maximum that the weights are taken relative to is renewed only when some row's
+// has grown by more than 2^8 in weight: weights up to 2^8 cost no accuracy in bf16 or fp32, and the multiplications of O^T fall away for nearly
+// all tiles.
+template <int DP, int NB, class Vis>
+__device__ __forceinline__ void attn_weights(f32x16 (&s)[NB], bf16x8 (&p)[2 * NB], AttnRows<DP> &rows, float c, int lane, bool masked, Vis vis)
+{
+    const int h = lane >> 5;
     if (masked) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -260,13 +314,40 @@ __device__ __forceinline__ void attn_step(const unsigned char *kt, const unsigne
             sum[r & 3] += s[b][r];
         }
     rows.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    bf16x8 p[2 * NB];
 #pragma unroll
     for (int t = 0; t < 2 * NB; ++t) p[t] = attn_operand(s[t >> 1], t & 1);
+}
+// O^T += V^T P^T, operands a batch ahead too
+template <int DP, int NB, int BATCH>
+__device__ __forceinline__ void attn_values(const unsigned char *vt, const bf16x8 (&p)[2 * NB], AttnRows<DP> &rows, int lane)
+{
+    constexpr int D = DP / 32, N = 2 * NB * D / BATCH;     // product i is step i / D of block i % D
+    static_assert(2 * NB * D % BATCH == 0, "whole batches");
+    bf16x8 a[2][BATCH];
+    const auto read = [&](int n) {
 #pragma unroll
-    for (int t = 0; t < 2 * NB; ++t)
+        for (int i = 0; i < BATCH; ++i) a[n & 1][i] = attn_cols<DP>(vt, (n * BATCH + i) / D, (n * BATCH + i) % D, lane);
+    };
+    read(0);
 #pragma unroll
-        for (int b = 0; b < DP / 32; ++b) rows.o[b] = attn_mfma(attn_cols<DP>(vt, t, b, lane), p[t], rows.o[b]);
+    for (int n = 0; n < N; ++n) {
+        if (n + 1 < N) read(n + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) rows.o[(n * BATCH + i) % D] = attn_mfma(a[n & 1][i], p[(n * BATCH + i) / D], rows.o[(n * BATCH + i) % D]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+// Keys of a tile (NB x 32 of them) for 32 rows
+template <int DP, int NB, class Vis>
+__device__ __forceinline__ void attn_step(const unsigned char *kt, const unsigned char *vt, const bf16x8 (&q)[DP / 16], AttnRows<DP> &rows, float c, int lane,
+                                          bool masked, Vis vis)
+{
+    f32x16 s[NB];
+    bf16x8 p[2 * NB];
+    attn_scores<DP, NB, 4>(kt, q, s, lane);
+    attn_weights<DP, NB>(s, p, rows, c, lane, masked, vis);
+    attn_values<DP, NB, 4>(vt, p, rows, lane);
 }
 
 // ---------------------------------------------------------------- packed sequences

@@ -510,7 +510,8 @@ coda_status check_heads(const coda_mat *Q, const coda_mat *K, const coda_mat *V,
 coda_status check_cache(const coda_cache *c)
 {
     if (!c) return CODA_ERR_NULL;
-    if (c->pages < 0 || c->page <= 0 || (c->page & (c->page - 1)) || c->pages >= (int64_t(1) << 31) / c->page || !heads_fit(c->kv_heads, c->kv_heads, c->head_dim))
+    if (c->pages < 0 || c->page <= 0 || (c->page & (c->page - 1)) || c->pages >= (int64_t(1) << 31) / c->page || !heads_fit(c->kv_heads, c->kv_heads, c->head_dim) ||
+        (int64_t)c->page * c->kv_heads * c->head_dim >= int64_t(1) << 31)
         return CODA_ERR_SHAPE;
     return aligned16(c->k) && aligned16(c->v) ? CODA_OK : CODA_ERR_ALIGN;
 }
@@ -905,6 +906,8 @@ coda_status coda_attention_cached(void *stream, const coda_mat *Q, const coda_ca
     p.Tq = (int)Q->rows;
     p.page_bits = __builtin_ctz((unsigned)cache->page);
     p.pages = (int)cache->pages;
+    p.page_mask = (uint32_t)cache->page - 1;
+    p.page_bytes = (uint32_t)((int64_t)cache->page * cache->kv_heads * cache->head_dim * 2);
     p.capacity = (int)capacity;
     p.scale = scale;
     p.out = static_cast<uint16_t *>(out);
