@@ -35,7 +35,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
 # The small-tile and the attention kernels: MFMA accumulators in ordinary registers.  Workgroups of few waves and much LDS leave a wave 512
 # registers, and the compiler then keeps the accumulators in the upper half and copies them around every MFMA.
 FLAGS_SMALL = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-SMALL = ("gemm_small", "gemm_direct", "gemm_scaled_inst", "gemm_scaled_tile_128", "grad_scaled", "attention")
+SMALL = ("gemm_small", "gemm_direct", "gemm_scaled_inst", "gemm_scaled_tile_128", "grad_scaled", "attention.", "attention_cached")
 
 SOURCES = ["coda_api.hip", "aux_kernels.hip", "q8_kernels.hip", "attention.hip", "attention_bwd.hip", "attention_cached.hip", "gemm_scaled_inst.hip", "grad_scaled_inst.hip",
            "gemm_scaled_tile_256_nt.hip", "gemm_scaled_tile_256_nn.hip", "gemm_scaled_tile_128_nt.hip", "gemm_scaled_tile_128_nn.hip",

@@ -43,22 +43,33 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, float c
     const auto sees = [&](int r) { return p.causal ? min(max(r + ahead + 1, 0), k.count) : k.count; };
     const int mine = sees(last), low = sees(min(row0 + wave * 32, q.count - 1)), high = row0 + wave * 32 < q.count ? sees(min(row0 + wave * 32 + 31, q.count - 1)) : 0;
     const int keys = sees(min(row0 + FWD_ROWS - 1, q.count - 1)), whole = sees(row0);
+    const AttnLane<DP> in(lane);
     AttnRows<DP> acc;
     acc.clear();
     if (threadIdx.x == 0) dirty = 0;
     if (PAD) attn_zero(smem, sizeof(smem), 256);
     const int n = (keys + FWD_KEYS - 1) / FWD_KEYS;
-    const AttnLoad<DP, PAD, FWD_KEYS, FWD_WAVES> load_k(K, p.ldk, wave, lane, p.D), load_v(V, p.ldv, wave, lane, p.D);
-    const auto load = [&](int j) {
+    AttnLoad<DP, PAD, FWD_KEYS, FWD_WAVES> load_k(K, p.ldk, wave, lane, p.D), load_v(V, p.ldv, wave, lane, p.D);
+    // Tile j in parts, that a step issues among its products: all waves' at once after the barrier would hold each other up
+    constexpr int PARTS = 2 * load_k.LOADS;
+    const auto load = [&](int j, int part) {
         unsigned char *at = smem + (j & 1) * 2 * TILE;
-        load_k(j * FWD_KEYS, k.count, at, lane);
-        load_v(j * FWD_KEYS, k.count, at + TILE, lane);
+        if (part == 0) {
+            load_k.begin(j * FWD_KEYS, k.count, attn_lds(at));
+            load_v.begin(j * FWD_KEYS, k.count, attn_lds(at + TILE));
+        }
+        if (part < PARTS / 2) load_k.next(part);
+        else load_v.next(part - PARTS / 2);
     };
-    if (n > 0) load(0);
+    const auto load_all = [&](int j) {
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) load(j, i);
+    };
+    if (n > 0) load_all(0);
+    attn_arrived(qf);
     for (int j = 0; j < n; ++j) {
         attn_wait();
         attn_barrier();                                    // tile j is there, and nobody reads tile j - 1 any more
-        if (j + 1 < n) load(j + 1);
         const int k0 = j * FWD_KEYS;
         unsigned char *at = smem + (j & 1) * 2 * TILE;
         if (k0 + FWD_KEYS > whole) {
@@ -66,19 +77,25 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p, float c
             attn_reads_done();
             attn_barrier();
         }
-        if (k0 >= high) continue;
-        const int lim = mine - k0;
-        attn_step<DP, FWD_KEYS / 32>(at, at + TILE, qf, acc, c, lane, k0 + FWD_KEYS > low, [&](int key) { return key < lim; });
+        if (k0 < high) {
+            const int lim = mine - k0;
+            static_assert(DP / 16 * (FWD_KEYS / 32) == 2 * PARTS, "a place for every load");
+            attn_step<DP, FWD_KEYS / 32>(attn_lds(at) + in.rows, attn_lds(at + TILE) + in.cols, qf, acc, c, lane, k0 + FWD_KEYS > low, [&](int key) { return key < lim; },
+                                         [&](int i) {
+                                             if (i % 2 == 0) load(j + 1, i / 2);           // past the last key there is nothing to load
+                                         });
+        } else
+            load_all(j + 1);
     }
     if (n * FWD_KEYS > whole) {
         __syncthreads();
         if (dirty)
             for (int j = whole / FWD_KEYS; j < n; ++j) {
-                load_v(j * FWD_KEYS, k.count, smem, lane);
+                load_v(j * FWD_KEYS, k.count, smem);
                 attn_wait();
                 attn_barrier();
                 const int lim = mine - j * FWD_KEYS;
-                attn_add_marks<DP, FWD_KEYS / 16>(smem, acc.o, lane, [&](int key) { return key < lim; });
+                attn_add_marks<DP, FWD_KEYS / 16>(attn_lds(smem) + in.cols, acc.o, lane, [&](int key) { return key < lim; });
                 __syncthreads();
             }
     }

@@ -3,43 +3,17 @@
 //   P = exp(S - lse),  delta_i = sum_d dO_id O_id,  dS = P (dO V^T - delta)
 //   dV = P^T dO,  dQ = scale dS K,  dK = scale dS^T Q
 //
-// Three kernels, no atomics: the row statistics; dK and dV, a workgroup for 64 keys of a key / value head, over all rows of all heads of the
-// group; dQ, a workgroup for 128 rows, over the keys.  S and dO V^T are formed in both (seven products where five would do): the
+// Two kernels, no atomics: dQ, a workgroup for 128 rows, over the keys, which also leaves the row statistics; dK and dV, a workgroup for 64 keys of a key / value
+// head, over all rows of all heads of the group.  S and dO V^T are formed in both (seven products where five would do): the
 // alternative, dQ added up in fp32 across workgroups, is either of no fixed order or a partial of every row for every tile of keys.
 #include "attn_launch.hpp"
 #include "attn_tile.hpp"
 
+#include <type_traits>
+
 namespace coda {
 
 constexpr int BWD_WAVES = 4;
-#ifndef DKV_NS
-#define DKV_NS 4
-#endif
-
-// stats[0][h][t] = lse * log2(e), stats[1][h][t] = delta.  16 (8) lanes a row of a head.
-template <int DP>
-__global__ __launch_bounds__(256) void attention_delta_kernel(BwdParams p)
-{
-    constexpr int CH = DP / 8;
-    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / CH;
-    const int64_t t = id % p.f.Tq;                          // neighbours share a head: their statistics are neighbours too
-    const int head = (int)(id / p.f.Tq), ch = threadIdx.x % CH;
-    if (head >= p.f.heads) return;
-    float sum = 0.0f;
-    if (ch * 8 < p.f.D) {
-        const int64_t col = (int64_t)head * p.f.D + ch * 8;
-        const bf16x8 a = *reinterpret_cast<const bf16x8 *>(p.O + t * p.ldo + col), b = *reinterpret_cast<const bf16x8 *>(p.dO + t * p.lddo + col);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += (float)a[e] * (float)b[e];
-    }
-#pragma unroll
-    for (int off = CH / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    if (ch == 0) {
-        const int64_t at = (int64_t)head * p.f.Tq + t;
-        p.stats[at] = p.f.lse[at] * LOG2E;
-        p.stats[(int64_t)p.f.heads * p.f.Tq + at] = sum;
-    }
-}
 
 // Columns 32 b .. of 32 rows of dQ, dK or dV out of their accumulators: times `scale`, turned back by the angle of table row `at` where there are tables
 template <bool PAD>
@@ -81,10 +55,11 @@ __device__ __forceinline__ int64_t bwd_angle(const BwdParams &p, const int32_t *
 template <int DP, bool PAD, int KB, int NS>
 __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParams p, float c)
 {
+    constexpr bool VLDS = DP == 128;                       // 32 registers that there are not
     constexpr int ROWS = 32, TILE = ROWS * DP * 2, STAGE = 2 * TILE + 256, KEYS = KB * 32;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * NS * STAGE];
-    int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * NS * STAGE + (VLDS ? KEYS * DP * 2 : 0)];
+    unsigned char *const v_tile = smem + 2 * NS * STAGE;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int kb = wave % KB, stream = wave / KB;
     const int64_t t = blockIdx.x / p.f.kv_heads;
     const int kv = blockIdx.x % p.f.kv_heads;
@@ -94,14 +69,14 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
     if (first < 0 || first >= k.count) return;
     const int key0 = (int)first, ahead = k.count - q.count, group = p.f.heads / p.f.kv_heads;
     const int key = key0 + kb * 32 + (lane & 31), last = min(key, k.count - 1);
-    bf16x8 kf[DP / 16], vf[DP / 16];
+    bf16x8 kf[DP / 16], vf[VLDS ? 1 : DP / 16];
     {
         const uint16_t *K = p.f.K + ((int64_t)k.begin + last) * p.f.ldk + (int64_t)kv * p.f.D, *V = p.f.V + ((int64_t)k.begin + last) * p.f.ldv + (int64_t)kv * p.f.D;
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             const int d = 16 * i + 8 * h;
             kf[i] = !PAD || d < p.f.D ? *reinterpret_cast<const bf16x8 *>(K + d) : bf16x8{};
-            vf[i] = !PAD || d < p.f.D ? *reinterpret_cast<const bf16x8 *>(V + d) : bf16x8{};
+            if constexpr (!VLDS) vf[i] = !PAD || d < p.f.D ? *reinterpret_cast<const bf16x8 *>(V + d) : bf16x8{};
         }
     }
     f32x16 dk[DP / 32], dv[DP / 32];
@@ -127,84 +102,133 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
     AttnLoad<DP, PAD, ROWS, KB> load_q(p.f.Q + (int64_t)q.begin * p.f.ldq + (int64_t)kv * group * p.f.D, p.f.ldq, kb, lane, p.f.D),
         load_do(p.dO + (int64_t)q.begin * p.lddo + (int64_t)kv * group * p.f.D, p.lddo, kb, lane, p.f.D);
     const uint16_t *const q_base = load_q.base, *const do_base = load_do.base;
-    const float *const stats_base = p.stats + (int64_t)kv * group * p.f.Tq + q.begin;
-    const auto load = [&](const Place &x, int buf) {
-        if (x.tile >= tiles) return;
-        unsigned char *at = smem + (buf * NS + stream) * STAGE;
-        load_q.base = q_base + x.head * p.f.D;
-        load_do.base = do_base + x.head * p.f.D;
-        load_q(x.tile * ROWS, q.count, at, lane);
-        load_do(x.tile * ROWS, q.count, at + TILE, lane);
-        if (kb == 0)
-            attn_load4(stats_base + (int64_t)x.head * p.f.Tq + ((int64_t)h * p.f.heads * p.f.Tq + min(x.tile * ROWS + (lane & 31), q.count - 1)),
-                       __builtin_amdgcn_readfirstlane(attn_lds(at + 2 * TILE)));
+    const uint32_t stats_off = (lane & 31) * 4;
+    static_assert(KB == 2, "a wave for each statistic");
+    const float *const stats_base = p.stats + ((int64_t)kb * p.f.heads + (int64_t)kv * group) * p.f.Tq + q.begin;
+    // In parts, that a round issues among its products: all waves' at once after the barrier would hold each other up
+    constexpr int PARTS = ROWS * DP * 2 / 1024 / KB;       // 1 KB loads of Q, and of dO, of a wave
+    const auto load = [&](const Place &x, int buf, int part) {
+        const uint32_t at = attn_lds(smem) + (buf * NS + stream) * STAGE;
+        const int row0 = x.tile * ROWS;                    // past the last row where there is no such place
+        if (part == 0) {
+            load_q.base = q_base + x.head * p.f.D;
+            load_q.begin(row0, q.count, at);
+        }
+        if (part == PARTS) {
+            load_do.base = do_base + x.head * p.f.D;
+            load_do.begin(row0, q.count, at + TILE);
+        }
+        if (part < PARTS) load_q.next(part);
+        else if (part < 2 * PARTS) load_do.next(part - PARTS);
+        else                                               // one wave has lse, the other delta
+            attn_load4(stats_base + (int64_t)x.head * p.f.Tq + row0, lane * 4, __builtin_amdgcn_readfirstlane(at + 2 * TILE + kb * ROWS * 4),
+                       attn_first_lanes(max(0, min(q.count - row0, ROWS))));
     };
     // some of the tile's rows do not see all of the workgroup's keys, or are none
     const auto ahead_of_keys = [&](int tile) { return p.f.causal && tile * ROWS + ahead < key0 + KEYS - 1; };
     const auto ragged = [&](int tile) { return tile * ROWS + ROWS > q.count; };
-    Place lead = place(0), x = place(stream), next = x;   // the first stream's and this one's
-    if (rounds) load(x, 0);
+    if (VLDS) AttnLoad<DP, PAD, KEYS, KB * NS>(p.f.V + (int64_t)k.begin * p.f.ldv + (int64_t)kv * p.f.D, p.f.ldv, wave, lane, p.f.D)(key0, k.count, v_tile);
+    const AttnLane<DP> in(lane);
+    const uint32_t v_rows = attn_lds(v_tile) + kb * 32 * DP * 2 + in.rows;
+    Place here = place(stream);
+    if (rounds)
+#pragma unroll
+        for (int i = 0; i <= 2 * PARTS; ++i) load(here, 0, i);
+    attn_arrived(kf);
+    if constexpr (!VLDS) attn_arrived(vf);
+    // Half of the streams are half a round behind the others, and there is one of each on every SIMD: the products of S and dP of one run beside the
+    // exponentials of the other.  A barrier each half keeps them so.
+    const bool behind = stream >= NS / 2;
+    if (behind) attn_barrier();
     for (int i = 0; i < rounds; ++i) {
         attn_wait();
         attn_barrier();
-        step(next);
-        if (i + 1 < rounds) load(next, (i + 1) & 1);
         unsigned char *at = smem + ((i & 1) * NS + stream) * STAGE;
-        const Place now = x;
-        x = next;
-        const bool mine = now.tile < tiles && (ahead_of_keys(now.tile) || ragged(now.tile));
-        // where any stream has a masked tile all wait while it is cleaned: theirs are tiles lead.tile to (NS - 1) / group + 1 further
-        if (ahead_of_keys(lead.tile) || ragged(lead.tile + (NS - 1) / group + 1)) {
-            if (mine) {
-                for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, lane);
-                attn_reads_done();
-            }
-            attn_barrier();
-        }
-        step(lead);
-        if (DP == 128) asm volatile("" : "+v"(lane));      // the addresses of the LDS reads are formed again each round: 16 registers that the kernel has not
+        const Place now = here;
+        step(here);
+        const bool mine = ahead_of_keys(now.tile) || ragged(now.tile);     // a place behind the last is masked altogether
         const int row0 = now.tile * ROWS;
-        if (now.tile >= tiles || (p.f.causal && row0 + ROWS - 1 + ahead < key0 + kb * 32)) continue;
-        f32x16 sc = {}, dp = {};
-#pragma unroll
-        for (int u = 0; u < DP / 16; ++u) sc = attn_mfma(attn_rows<DP>(at, 0, u, lane), kf[u], sc);
-#pragma unroll
-        for (int u = 0; u < DP / 16; ++u) dp = attn_mfma(attn_rows<DP>(at + TILE, 0, u, lane), vf[u], dp);
+        const uint32_t rows = attn_lds(at) + in.rows, cols = attn_lds(at) + in.cols;      // of Q; dO's tile is behind it
         const float *stats = reinterpret_cast<const float *>(at + 2 * TILE);
+        const auto issue = [&](int product) {              // a load behind every second product of S and dP
+            if (product % 2 == 0 && product / 2 <= 2 * PARTS) load(here, (i + 1) & 1, product / 2);
+            if (product == DP / 8 - 1) load(here, (i + 1) & 1, 2 * PARTS);
+        };
+        static_assert(2 * PARTS <= DP / 16, "a place for every load");
+        // S, and dO V^T - delta: those accumulators begin with -delta
+        f32x16 sc = {}, dp;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const f32x4 l2 = *reinterpret_cast<const f32x4 *>(stats + 8 * g + 4 * h), delta = *reinterpret_cast<const f32x4 *>(stats + 32 + 8 * g + 4 * h);
+            const f32x4 delta = *reinterpret_cast<const f32x4 *>(stats + 32 + 8 * g + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dp[4 * g + e] = delta[e];
+        }
+        constexpr int B = VLDS ? 2 : 4;                    // batches; two operands a product where V is in LDS
+        if constexpr (VLDS) {
+            bf16x8 v[2][B];
+            const auto read_v = [&](int n) {
+#pragma unroll
+                for (int j = 0; j < B; ++j) v[n & 1][j] = attn_rows<DP>(v_rows, 0, n * B + j);
+            };
+            read_v(0);
+            attn_products<DP / 16, B>([&](int i) { return attn_rows<DP>(rows, 0, i); }, [&](int u, bf16x8 a) {
+                sc = attn_mfma(a, kf[u], sc);
+                issue(u);
+            });
+            attn_products<DP / 16, B>(
+                [&](int i) {
+                    if (i % B == 0 && i) read_v(i / B);
+                    return attn_rows<DP>(rows, ROWS, i);
+                },
+                [&](int u, bf16x8 a) {
+                    dp = attn_mfma(a, v[u / B & 1][u % B], dp);
+                    issue(DP / 16 + u);
+                });
+        } else {
+            attn_products<DP / 16, B>([&](int i) { return attn_rows<DP>(rows, 0, i); }, [&](int u, bf16x8 a) {
+                sc = attn_mfma(a, kf[u], sc);
+                issue(u);
+            });
+            attn_products<DP / 16, B>([&](int i) { return attn_rows<DP>(rows, ROWS, i); }, [&](int u, bf16x8 a) {
+                dp = attn_mfma(a, vf[VLDS ? 0 : u], dp);
+                issue(DP / 16 + u);
+            });
+        }
+        if (mine)                                          // for the products with the rows' columns; S and dP are masked by selection
+            for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, lane);
+        attn_reads_done();
+        attn_barrier();
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 l2 = *reinterpret_cast<const f32x4 *>(stats + 8 * g + 4 * h);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = 4 * g + e;
                 sc[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, -l2[e]));
-                dp[r] = sc[r] * (dp[r] - delta[e]);
             }
-            if (mine) {
-                // a row of dO that is not finite was cleaned above; delta - delta hands what it was on
-                const int lim = p.f.causal ? key - ahead - row0 : 0;
+        }
+        if (mine) {
+            const int lim = p.f.causal ? key - ahead - row0 : 0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * g + e, row = attn_acc_row(r, h);
-                    const bool sees = bool((int)(row >= lim) & (int)(row0 + row < q.count));
-                    sc[r] = sees ? sc[r] + (delta[e] - delta[e]) : 0.0f;
-                    dp[r] = sees ? dp[r] : 0.0f;
-                }
+            for (int r = 0; r < 16; ++r) {
+                const int row = attn_acc_row(r, h);
+                const bool sees = bool((int)(row >= lim) & (int)(row0 + row < q.count));
+                sc[r] = sees ? sc[r] + (dp[r] - dp[r]) : 0.0f;                       // a row of dO that is not finite was cleaned above, but delta has it: 0, or NaN there
+                dp[r] = sees ? dp[r] : 0.0f;
             }
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const bf16x8 w = attn_operand(sc, u);
-#pragma unroll
-            for (int b = 0; b < DP / 32; ++b) dv[b] = attn_mfma(attn_cols<DP>(at + TILE, u, b, lane), w, dv[b]);
-        }
+        for (int r = 0; r < 16; ++r) dp[r] *= sc[r];
+        bf16x8 w[2], x[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const bf16x8 w = attn_operand(dp, u);
-#pragma unroll
-            for (int b = 0; b < DP / 32; ++b) dk[b] = attn_mfma(attn_cols<DP>(at, u, b, lane), w, dk[b]);
+            w[u] = attn_operand(sc, u);
+            x[u] = attn_operand(dp, u);
         }
+        attn_values<DP, 1, 4>(cols + TILE, w, dv);
+        attn_values<DP, 1, 4>(cols, x, dk);
     }
+    if (!behind) attn_barrier();
     // The streams' parts are added up in their order: all of dK, then all of dV through LDS, and a stream finishes every NS-th 32 columns
     const int64_t row = (int64_t)k.begin + key;
     const bool there = key < k.count;
@@ -266,27 +290,56 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
             of[i] = !PAD || d < p.f.D ? *reinterpret_cast<const bf16x8 *>(dO + d) : bf16x8{};
         }
     }
-    const float *stats = p.stats + (int64_t)head * p.f.Tq + q.begin + last;
-    const float l2 = stats[0], delta = stats[(int64_t)p.f.heads * p.f.Tq];
+    // The row's statistics, for this kernel and the next: lse * log2(e), and -delta, which the accumulators of dO V^T begin with
+    float l2 = p.f.lse[(int64_t)head * p.f.Tq + q.begin + last] * LOG2E, delta = 0.0f;
+    {
+        const uint16_t *O = p.O + ((int64_t)q.begin + last) * p.ldo + (int64_t)head * p.f.D;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const int d = 16 * i + 8 * h;
+            const bf16x8 o = !PAD || d < p.f.D ? *reinterpret_cast<const bf16x8 *>(O + d) : bf16x8{};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta -= (float)o[e] * (float)of[i][e];
+        }
+        const f32x2 both = attn_halves(delta);
+        delta = both[0] + both[1];
+        if (h == 0 && row < q.count) {
+            float *stats = p.stats + (int64_t)head * p.f.Tq + q.begin + row;
+            stats[0] = l2;
+            stats[(int64_t)p.f.heads * p.f.Tq] = delta;
+        }
+    }
     const auto sees = [&](int r) { return p.f.causal ? min(max(r + ahead + 1, 0), k.count) : k.count; };
     const int mine = sees(last), low = sees(min(row0 + wave * 32, q.count - 1)), high = row0 + wave * 32 < q.count ? sees(min(row0 + wave * 32 + 31, q.count - 1)) : 0;
     const int keys = sees(min(row0 + ROWS - 1, q.count - 1)), whole = sees(row0);
+    const AttnLane<DP> in(lane);
     f32x16 dq[DP / 32];
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
     if (PAD) attn_zero(smem, sizeof(smem), 256);
     const int n = (keys + KEYS - 1) / KEYS;
-    const AttnLoad<DP, PAD, KEYS, BWD_WAVES> load_k(K, p.f.ldk, wave, lane, p.f.D), load_v(V, p.f.ldv, wave, lane, p.f.D);
-    const auto load = [&](int j) {
+    AttnLoad<DP, PAD, KEYS, BWD_WAVES> load_k(K, p.f.ldk, wave, lane, p.f.D), load_v(V, p.f.ldv, wave, lane, p.f.D);
+    constexpr int PARTS = 2 * load_k.LOADS;
+    const auto load = [&](int j, int part) {               // as in the forward kernel
         unsigned char *at = smem + (j & 1) * 2 * TILE;
-        load_k(j * KEYS, k.count, at, lane);
-        load_v(j * KEYS, k.count, at + TILE, lane);
+        if (part == 0) {
+            load_k.begin(j * KEYS, k.count, attn_lds(at));
+            load_v.begin(j * KEYS, k.count, attn_lds(at + TILE));
+        }
+        if (part < PARTS / 2) load_k.next(part);
+        else load_v.next(part - PARTS / 2);
     };
-    if (n > 0) load(0);
+    const auto load_all = [&](int j) {
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) load(j, i);
+    };
+    if (n > 0) load_all(0);
+    attn_arrived(qf);
+    attn_arrived(of);
+    asm volatile("" : "+v"(l2), "+v"(delta));
     for (int j = 0; j < n; ++j) {
         attn_wait();
         attn_barrier();
-        if (j + 1 < n) load(j + 1);
         const int k0 = j * KEYS;
         unsigned char *at = smem + (j & 1) * 2 * TILE;
         if (k0 + KEYS > whole) {
@@ -294,29 +347,37 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
             attn_reads_done();
             attn_barrier();
         }
-        if (k0 >= high) continue;
+        if (k0 >= high) {
+            load_all(j + 1);
+            continue;
+        }
         const int lim = mine - k0;
         const bool masked = k0 + KEYS > low;
+        const uint32_t rows = attn_lds(at) + in.rows;      // of K; V's tile is behind it
+        static_assert(DP / 8 == 2 * PARTS, "a place for every load");
 #pragma unroll
         for (int b = 0; b < KEYS / 32; ++b) {
-            f32x16 sc = {}, dp = {};
+            f32x16 sc = {}, dp;                            // dP - delta: the accumulators begin with -delta
 #pragma unroll
-            for (int u = 0; u < DP / 16; ++u) {
-                sc = attn_mfma(attn_rows<DP>(at, b * 32, u, lane), qf[u], sc);
-                dp = attn_mfma(attn_rows<DP>(at + TILE, b * 32, u, lane), of[u], dp);
-            }
+            for (int r = 0; r < 16; ++r) dp[r] = delta;
+            attn_products<DP / 16, 4>([&](int i) { return attn_rows<DP>(rows, b * 32, i); },
+                                      [&](int i, bf16x8 a) {
+                                          sc = attn_mfma(a, qf[i], sc);
+                                          if (b == 0 && i % 2 == 0) load(j + 1, i / 2);
+                                      });
+            attn_products<DP / 16, 4>([&](int i) { return attn_rows<DP>(rows, KEYS + b * 32, i); },
+                                      [&](int i, bf16x8 a) {
+                                          dp = attn_mfma(a, of[i], dp);
+                                          if (b == 0 && i % 2 == 0) load(j + 1, PARTS / 2 + i / 2);
+                                      });
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, -l2)) * (dp[r] - delta);
+            for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, -l2)) * dp[r];
             if (masked) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = b * 32 + attn_acc_row(r, h) < lim ? dp[r] : 0.0f;
             }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const bf16x8 w = attn_operand(dp, u);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) dq[d] = attn_mfma(attn_cols<DP>(at, 2 * b + u, d, lane), w, dq[d]);
-            }
+            const bf16x8 w[2] = {attn_operand(dp, 0), attn_operand(dp, 1)};
+            attn_values<DP, 1, 4>(attn_lds(at) + in.cols + b * 32 * DP * 2, w, dq);
         }
     }
     const int64_t at = (int64_t)q.begin + row;
@@ -326,14 +387,13 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
     for (int b = 0; b < DP / 32; ++b) bwd_store<PAD>(dq[b], b, p.f.scale, p, p.cos, angle, p.dQ + at * p.lddq + (int64_t)head * p.f.D, there, h);
 }
 
-static int64_t delta_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tq * p.f.heads * (p.f.D > 64 ? 16 : 8) + 255) / 256; }
 static int64_t dkv_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tk / 64 + p.f.n_seqs) * p.f.kv_heads; }
 static int64_t dq_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tq / 128 + p.f.n_seqs) * p.f.heads; }
 
 int64_t bwd_workgroups(const BwdParams &p)
 {
-    const int64_t a = delta_workgroups(p), b = dkv_workgroups(p), d = dq_workgroups(p);
-    return a > b ? (a > d ? a : d) : b > d ? b : d;
+    const int64_t a = 2 * dkv_workgroups(p), b = dq_workgroups(p);       // of 256
+    return a > b ? a : b;
 }
 size_t bwd_bytes(int64_t Tq, int heads) { return (size_t)Tq * heads * 8; }
 
@@ -343,15 +403,11 @@ static hipError_t launch_bwd(const BwdParams &p, hipStream_t s)
     const float c = p.f.scale * LOG2E;
     hipError_t e = hipSuccess;
     if (p.f.Tq > 0) {
-        hipLaunchKernelGGL((attention_delta_kernel<DP>), dim3((unsigned)delta_workgroups(p)), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((attention_dq_kernel<DP, PAD>), dim3((unsigned)dq_workgroups(p)), dim3(256), 0, s, p, c);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.f.Tk > 0) {
-        hipLaunchKernelGGL((attention_dkv_kernel<DP, PAD, 2, DKV_NS>), dim3((unsigned)dkv_workgroups(p)), dim3(128 * DKV_NS), 0, s, p, c);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    if (p.f.Tq > 0) {
-        hipLaunchKernelGGL((attention_dq_kernel<DP, PAD>), dim3((unsigned)dq_workgroups(p)), dim3(256), 0, s, p, c);
+        hipLaunchKernelGGL((attention_dkv_kernel<DP, PAD, 2, 4>), dim3((unsigned)dkv_workgroups(p)), dim3(512), 0, s, p, c);
         e = hipGetLastError();
     }
     return e;

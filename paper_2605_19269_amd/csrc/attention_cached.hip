@@ -93,6 +93,8 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
     const int member = wave % C::GROUP, kg = wave / C::GROUP;
     const int kv = blockIdx.x % p.kv_heads, range = blockIdx.x / p.kv_heads;
 
+    const AttnLane<DP> in(lane);
+
     // This workgroup's range, and the sequence that it begins in
     const auto cost_of = [](const CachedSeq &q) { return (int64_t)q.tiles * (q.steps + C::RESTART); };
     int64_t mine = 0, before;
@@ -222,8 +224,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
             fetch_ids(j0);
             fetch_ids(j0 + 1);
             attn_wait();
-#pragma unroll
-            for (int i = 0; i < DP / 16; ++i) asm volatile("" : "+v"(qf[i]));      // the compiler waits for Q here, and not behind the loads of K and V
+            attn_arrived(qf);
             asm volatile("" : : "v"(bits0), "v"(bits1));
             find_rows(j0);
             fetch(K, j0, 0);
@@ -250,7 +251,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                     attn_barrier();
                     if (j + 1 < j1) fetch(V, j + 1, 1);
                     if (here) {
-                        attn_scores<DP, NB, 4>(slot(j, 0), qf, sc, lane);
+                        attn_scores<DP, NB, 4>(attn_lds(slot(j, 0)) + in.rows, qf, sc, [](int) {});
                         attn_weights<DP, NB>(sc, w, acc, c, lane, masked, see);
                     }
                     if (j + 1 < j1) attn_wait_but<2 * L + 1>();                    // K, pages, V are to come
@@ -268,11 +269,11 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                         attn_reads_done();
                         attn_barrier();
                     }
-                    if (here) attn_values<DP, NB, 4>(slot(j, 1), w, acc, lane);
+                    if (here) attn_values<DP, NB, 4>(attn_lds(slot(j, 1)) + in.cols, w, acc.o);
                 } else {
                     if (j + 1 < j1) attn_wait_but<3 * L + 1>();                    // K and the pages of step j + 2 are there; V, K, pages, V are to come
                     else attn_wait_but<L>();
-                    attn_scores<DP, NB, 4>(slot(j, 0), qf, sc, lane);
+                    attn_scores<DP, NB, 4>(attn_lds(slot(j, 0)) + in.rows, qf, sc, [](int) {});
                     attn_reads_done();
                     if (j + 2 < j1) {
                         find_rows(j + 2);
@@ -288,7 +289,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                             if (attn_clean(slot(j, 1), C::TILE, lane)) bad = true;
                             attn_reads_done();
                         }
-                        attn_values<DP, NB, 4>(slot(j, 1), w, acc, lane);
+                        attn_values<DP, NB, 4>(attn_lds(slot(j, 1)) + in.cols, w, acc.o);
                     }
                     attn_reads_done();
                     if (j + 2 < j1) fetch(V, j + 2, 1);
@@ -308,7 +309,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                     load(V, own);
                     attn_wait();
                     if (MANY) attn_barrier();
-                    attn_add_marks<DP, C::WAVE_KEYS / 16>(own, acc.o, lane, [&](int k) { return sees(k0 + k); });
+                    attn_add_marks<DP, C::WAVE_KEYS / 16>(attn_lds(own) + in.cols, acc.o, lane, [&](int k) { return sees(k0 + k); });
                     attn_reads_done();
                     if (MANY) attn_barrier();
                 }

@@ -41,17 +41,31 @@ __device__ __forceinline__ void attn_load16(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
-// The same from a uniform address and a lane's offset
-__device__ __forceinline__ void attn_load16(const void *uniform, uint32_t off, uint32_t lds)
+// The same from a uniform address and a lane's offset, by the lanes of `mask` alone, which need be none; what the others' 16 bytes of LDS hold stays.  No branch: the
+// callers issue these among their products, and a branch would part those.
+__device__ __forceinline__ uint64_t attn_uniform(uint64_t a)
 {
-    const uint64_t a = reinterpret_cast<uint64_t>(uniform);
-    const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds) : "memory", "m0");
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a);
 }
+__device__ __forceinline__ void attn_load16(const void *base, uint32_t off, uint32_t lds, uint64_t mask)
+{
+    uint64_t all;
+    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %4\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, %0"
+                 : "=&s"(all) : "v"(off), "s"(attn_uniform(reinterpret_cast<uint64_t>(base))), "s"(lds), "s"(attn_uniform(mask)) : "memory", "m0");
+}
+// Four bytes a lane
 __device__ __forceinline__ void attn_load4(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
+__device__ __forceinline__ void attn_load4(const void *base, uint32_t off, uint32_t lds, uint64_t mask)
+{
+    uint64_t all;
+    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %4\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, %0"
+                 : "=&s"(all) : "v"(off), "s"(attn_uniform(reinterpret_cast<uint64_t>(base))), "s"(lds), "s"(attn_uniform(mask)) : "memory", "m0");
+}
+// The first n of 64 lanes, n from 0 on
+__device__ __forceinline__ uint64_t attn_first_lanes(int n) { return n >= 64 ? ~0ull : (1ull << n) - 1; }
 // All loads of this wave have arrived, all its LDS reads are done
 __device__ __forceinline__ void attn_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 // All but the last N of them
@@ -67,45 +81,62 @@ __device__ __forceinline__ void attn_barrier()
     asm volatile("" ::: "memory");
 }
 
-// Tiles of ROWS rows of one head, loaded by NW waves together.  PAD: D < DP, the chunks behind D are left as attn_zero() made them.
+// Tiles of ROWS rows of one head, loaded by NW waves together, 1 KB a load.  PAD: D < DP, the chunks behind D are left as attn_zero() made them.
 template <int DP, bool PAD, int ROWS, int NW>
 struct AttnLoad {
     static constexpr int CH = DP / 8, RPL = 64 / CH, LOADS = ROWS / (NW * RPL);
     static_assert(ROWS % (NW * RPL) == 0, "whole wave-loads");
     const uint16_t *base;              // element (0, 0) of the head's rows
     int64_t ld;
-    int wave, D;
-    uint32_t off;                      // of the lane's chunk within its wave's loads
+    int wave;
+    uint32_t row_off, chunk_off;       // bytes from a load's first row to the lane's, and of its chunk in the first load
+    uint64_t chunks[PAD ? LOADS : 1];  // lanes with a chunk below D
+    // A tile on its way: the next load's first row, how many rows there are from it on, where it goes
+    const uint16_t *from;
+    int left;
+    uint32_t to;
 
     static __device__ __forceinline__ int chunk(int i, int wave, int lane) { return (lane % CH) ^ attn_swizzle<DP>((i * NW + wave) * RPL + lane / CH); }
     __device__ __forceinline__ AttnLoad(const uint16_t *base, int64_t ld, int wave, int lane, int D)
-        : base(base), ld(ld), wave(wave), D(D), off((uint32_t)((lane / CH) * (int)ld + chunk(0, wave, lane) * 8) * 2)
+        : base(base), ld(ld), wave(wave), row_off((uint32_t)((lane / CH) * (int)ld) * 2), chunk_off((uint32_t)chunk(0, wave, lane) * 16)
     {
+        if (PAD)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) chunks[PAD ? i : 0] = __ballot(chunk(i, wave, lane) * 8 < D);
     }
-    // Rows row0 .. of n (those from n on: row n - 1 again).  Whole tiles take uniform addresses, one addition for a lane's 1 KB; a load's chunks are
-    // those of the first one but where four rows times the waves are fewer than the swizzle's 16: there two chunks to the side every other time.
-    __device__ __forceinline__ void operator()(int row0, int n, unsigned char *tile, int lane) const
+    // Rows row0 .. ; rows from n on are not read
+    __device__ __forceinline__ void begin(int row0, int n, uint32_t tile)
     {
-        const uint32_t lds = __builtin_amdgcn_readfirstlane(attn_lds(tile) + wave * 1024);
-        if (row0 + ROWS <= n) {
-            const uint16_t *from = base + (int64_t)(row0 + wave * RPL) * ld;
+        from = base + (int64_t)(row0 + wave * RPL) * ld;
+        left = n - row0 - wave * RPL;
+        to = tile + wave * 1024;
+    }
+    // Load i of them, in order.  Its chunk differs from that of the first in two bits that i gives, none with four waves.
+    __device__ __forceinline__ void next(int i)
+    {
+        constexpr int STEP = DP == 128 ? NW : 2 * NW;
+        attn_load16(from, row_off + (chunk_off ^ (i * STEP % 4 * 16)), __builtin_amdgcn_readfirstlane(to),
+                    attn_first_lanes(max(0, min(left, RPL)) * CH) & (PAD ? chunks[PAD ? i : 0] : ~0ull));
+        from += (int64_t)(NW * RPL) * ld;
+        left -= NW * RPL;
+        to += NW * 1024;
+    }
+    __device__ __forceinline__ void operator()(int row0, int n, const unsigned char *tile)
+    {
+        begin(row0, n, attn_lds(tile));
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                uint32_t o = off;
-                if (RPL * NW < 16 && (i & 1)) o += chunk(0, wave, lane) & 2 ? -32 : 32;
-                static_assert(RPL * NW >= 16 || (DP == 128 && NW == 2), "chunks of later loads");
-                if (!PAD || chunk(i, wave, lane) * 8 < D) attn_load16(from, o, lds + i * NW * 1024);
-                from += (int64_t)(NW * RPL) * ld;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int c = chunk(i, wave, lane), row = min(row0 + (i * NW + wave) * RPL + lane / CH, n - 1);
-                if (!PAD || c * 8 < D) attn_load16(base + row * ld + c * 8, lds + i * NW * 1024);
-            }
-        }
+        for (int i = 0; i < LOADS; ++i) next(i);
     }
 };
+
+// Operands loaded ahead of a loop: the compiler waits for them here.  Otherwise it waits where the loop first uses them, in every round, and with its
+// count of its own loads that wait is for the tiles on their way too.
+template <int N>
+__device__ __forceinline__ void attn_arrived(bf16x8 (&f)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
+}
 
 // Clears `bytes` (a multiple of 16) of LDS for PAD kernels, before their first tile
 __device__ __forceinline__ void attn_zero(unsigned char *p, int bytes, int threads)
@@ -114,25 +145,34 @@ __device__ __forceinline__ void attn_zero(unsigned char *p, int bytes, int threa
     __syncthreads();
 }
 
-// Operand of 32 tile rows x 16 columns: row row_base + lane % 32, columns 16 t + 8 (lane / 32) ..
+// The two ways in which operands are read from a tile, as byte offsets of a lane.  Steps along the columns change single bits of the chunk's position, which lie
+// above the lane's own, so an operand's address is one exclusive or away from that of the first, and rows further on are a constant of the instruction: forming the addresses
+// of 64 reads from rows and columns took dK's kernel 150 of its 350 vector instructions a round, and these, not the products, were its time.
 template <int DP>
-__device__ __forceinline__ bf16x8 attn_rows(const unsigned char *tile, int row_base, int t, int lane)
+struct AttnLane {
+    uint32_t rows, cols;
+    __device__ __forceinline__ explicit AttnLane(int lane)
+    {
+        const int h = lane >> 5, i = lane & 15, r = 4 * h + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+        rows = (lane & 31) * (DP * 2) + ((h ^ attn_swizzle<DP>(lane & 31)) << 4);
+        cols = r * (DP * 2) + ((c ^ attn_swizzle<DP>(r)) << 4) + (i & 1) * 8;
+    }
+};
+// Operand of 32 tile rows x 16 columns: row row_base + lane % 32, columns 16 t + 8 (lane / 32) ..  tile_rows: the tile's LDS address (a multiple of 256) + AttnLane::rows
+template <int DP>
+__device__ __forceinline__ bf16x8 attn_rows(uint32_t tile_rows, int row_base, int t)
 {
-    const int r = row_base + (lane & 31), c = 2 * t + (lane >> 5);
-    return *reinterpret_cast<const bf16x8 *>(tile + r * (DP * 2) + ((c ^ attn_swizzle<DP>(lane & 31)) << 4));
+    return *(const __attribute__((address_space(3))) bf16x8 *)((tile_rows ^ (t << 5)) + row_base * (DP * 2));
 }
-
 // Operand of the transposed tile, 32 columns x 16 rows: column 32 db + lane % 32, rows 16 t + 4 (lane / 32) + {0 1 2 3, 8 9 10 11}.  Within 16
 // lanes, lane i of a transposing read supplies the address of row i / 4, columns 4 (i % 4) .. and receives column i of the four rows.
 template <int DP>
-__device__ __forceinline__ bf16x8 attn_cols(const unsigned char *tile, int t, int db, int lane)
+__device__ __forceinline__ bf16x8 attn_cols(uint32_t tile_cols, int t, int db)
 {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int i = lane & 15, c = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    const int r = 4 * (lane >> 5) + (i >> 2);
-    const unsigned char *p = tile + t * 16 * DP * 2 + (i & 1) * 8;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + r * (DP * 2) + ((c ^ attn_swizzle<DP>(r)) << 4)));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + (r + 8) * (DP * 2) + ((c ^ attn_swizzle<DP>(r + 8)) << 4)));
+    const uint32_t p = tile_cols ^ (db << 6);              // eight rows further the swizzle differs in one bit
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + t * 16 * DP * 2));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((p ^ 32) + (t * 16 + 8) * DP * 2));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
@@ -218,7 +258,7 @@ __device__ __forceinline__ float attn_marked(float o, float marks)
 }
 // What the elements of an uncleaned tile of NT x 16 rows that are not finite come to in acc; vis(k): the lane's row sees row k of the tile
 template <int DP, int NT, class Vis>
-__device__ __forceinline__ void attn_add_marks(const unsigned char *tile, f32x16 (&acc)[DP / 32], int lane, Vis vis)
+__device__ __forceinline__ void attn_add_marks(uint32_t tile_cols, f32x16 (&acc)[DP / 32], int lane, Vis vis)
 {
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) {
@@ -228,7 +268,7 @@ __device__ __forceinline__ void attn_add_marks(const unsigned char *tile, f32x16
             s16x8 see;
 #pragma unroll
             for (int e = 0; e < 8; ++e) see[e] = vis(16 * t + (e & 3) + 8 * (e >> 2) + 4 * (lane >> 5)) ? 0x3f80 : 0;
-            marks = attn_mfma(attn_marks(attn_cols<DP>(tile, t, b, lane)), __builtin_bit_cast(bf16x8, see), marks);
+            marks = attn_mfma(attn_marks(attn_cols<DP>(tile_cols, t, b)), __builtin_bit_cast(bf16x8, see), marks);
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[b][r] = attn_marked(acc[b][r], marks[r]);
@@ -250,29 +290,52 @@ struct AttnRows {
     }
 };
 
-// S^T of NB x 32 keys and 32 rows.  The operands are read a batch of BATCH ahead of their products: left to itself the compiler reads each one where it
-// is used and waits for it there.
-template <int DP, int NB, int BATCH>
-__device__ __forceinline__ void attn_scores(const unsigned char *kt, const bf16x8 (&q)[DP / 16], f32x16 (&s)[NB], int lane)
+// Products 0 .. N - 1 with their LDS operands read a batch of BATCH ahead: left to itself the compiler reads each one where it is used and waits for it there,
+// or, where registers seem to be free, all of them at once.  read(i) returns the operand of product i, multiply(i, operand) takes it; the first batch is
+// read by the caller, and tail() is called ahead of the last products, to read what comes after them.
+template <int BATCH, class Read>
+__device__ __forceinline__ void attn_read(bf16x8 (&a)[BATCH], Read read)
 {
-    constexpr int T = DP / 16, N = T * NB / BATCH;         // batches; product i is step i / NB of block i % NB
-    static_assert(T * NB % BATCH == 0, "whole batches");
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) a[i] = read(i);
+}
+template <int N, int BATCH, class Read, class Multiply, class Tail>
+__device__ __forceinline__ void attn_products(const bf16x8 (&first)[BATCH], Read read, Multiply multiply, Tail tail)
+{
+    static_assert(N % BATCH == 0, "whole batches");
     bf16x8 a[2][BATCH];
-    const auto read = [&](int n) {
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) a[n & 1][i] = attn_rows<DP>(kt, (n * BATCH + i) % NB * 32, (n * BATCH + i) / NB, lane);
-    };
-    read(0);
+    for (int i = 0; i < BATCH; ++i) a[0][i] = first[i];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+    for (int n = 0; n < N / BATCH; ++n) {
+        if (n + 1 < N / BATCH) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        if (n + 1 < N) read(n + 1);
+            for (int i = 0; i < BATCH; ++i) a[(n + 1) & 1][i] = read((n + 1) * BATCH + i);
+        } else tail();
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) s[(n * BATCH + i) % NB] = attn_mfma(a[n & 1][i], q[(n * BATCH + i) / NB], s[(n * BATCH + i) % NB]);
+        for (int i = 0; i < BATCH; ++i) multiply(n * BATCH + i, a[n & 1][i]);
         __builtin_amdgcn_sched_barrier(0);
     }
+}
+template <int N, int BATCH, class Read, class Multiply>
+__device__ __forceinline__ void attn_products(Read read, Multiply multiply)
+{
+    bf16x8 first[BATCH];
+    attn_read<BATCH>(first, read);
+    attn_products<N, BATCH>(first, read, multiply, [] {});
+}
+// S^T of NB x 32 keys and 32 rows; between(i) is called behind product i
+template <int DP, int NB, int BATCH, class Between>
+__device__ __forceinline__ void attn_scores(uint32_t k_rows, const bf16x8 (&q)[DP / 16], f32x16 (&s)[NB], Between between)
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+    attn_products<DP / 16 * NB, BATCH>([&](int i) { return attn_rows<DP>(k_rows, i % NB * 32, i / NB); },
+                                       [&](int i, bf16x8 a) {
+                                           s[i % NB] = attn_mfma(a, q[i / NB], s[i % NB]);
+                                           between(i);
+                                       });
 }
 // The softmax step: scores to weights, rounded, and the rows' maxima and sums.  c = scale * log2(e) > 0.  `masked`: some position is not visible;
 // vis(k) says whether key k of the tile is, for the lane's row.  The maximum that the weights are taken relative to is renewed only when some row's
@@ -317,37 +380,23 @@ __device__ __forceinline__ void attn_weights(f32x16 (&s)[NB], bf16x8 (&p)[2 * NB
 #pragma unroll
     for (int t = 0; t < 2 * NB; ++t) p[t] = attn_operand(s[t >> 1], t & 1);
 }
-// O^T += V^T P^T, operands a batch ahead too
+// O^T += V^T P^T
 template <int DP, int NB, int BATCH>
-__device__ __forceinline__ void attn_values(const unsigned char *vt, const bf16x8 (&p)[2 * NB], AttnRows<DP> &rows, int lane)
+__device__ __forceinline__ void attn_values(uint32_t v_cols, const bf16x8 (&p)[2 * NB], f32x16 (&o)[DP / 32])
 {
-    constexpr int D = DP / 32, N = 2 * NB * D / BATCH;     // product i is step i / D of block i % D
-    static_assert(2 * NB * D % BATCH == 0, "whole batches");
-    bf16x8 a[2][BATCH];
-    const auto read = [&](int n) {
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) a[n & 1][i] = attn_cols<DP>(vt, (n * BATCH + i) / D, (n * BATCH + i) % D, lane);
-    };
-    read(0);
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-        if (n + 1 < N) read(n + 1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) rows.o[(n * BATCH + i) % D] = attn_mfma(a[n & 1][i], p[(n * BATCH + i) / D], rows.o[(n * BATCH + i) % D]);
-        __builtin_amdgcn_sched_barrier(0);
-    }
+    constexpr int D = DP / 32;
+    attn_products<2 * NB * D, BATCH>([&](int i) { return attn_cols<DP>(v_cols, i / D, i % D); }, [&](int i, bf16x8 a) { o[i % D] = attn_mfma(a, p[i / D], o[i % D]); });
 }
 // Keys of a tile (NB x 32 of them) for 32 rows
-template <int DP, int NB, class Vis>
-__device__ __forceinline__ void attn_step(const unsigned char *kt, const unsigned char *vt, const bf16x8 (&q)[DP / 16], AttnRows<DP> &rows, float c, int lane,
-                                          bool masked, Vis vis)
+template <int DP, int NB, class Vis, class Between>
+__device__ __forceinline__ void attn_step(uint32_t k_rows, uint32_t v_cols, const bf16x8 (&q)[DP / 16], AttnRows<DP> &rows, float c, int lane, bool masked, Vis vis,
+                                          Between between)
 {
     f32x16 s[NB];
     bf16x8 p[2 * NB];
-    attn_scores<DP, NB, 4>(kt, q, s, lane);
+    attn_scores<DP, NB, 4>(k_rows, q, s, between);
     attn_weights<DP, NB>(s, p, rows, c, lane, masked, vis);
-    attn_values<DP, NB, 4>(vt, p, rows, lane);
+    attn_values<DP, NB, 4>(v_cols, p, rows.o);
 }
 
 // ---------------------------------------------------------------- packed sequences
