@@ -144,7 +144,7 @@ _blib.coda_calib_mfma_loop16.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp]
 from . import _binding  # noqa: E402  (links libcoda.so)
 
 _NATIVE = ("coda_gemm", "coda_row_finalize", "coda_row_sumsq", "coda_col_finalize", "coda_lse_finalize", "coda_quantize", "coda_dequantize",
-           "coda_gemm_scaled", "coda_grad_scaled")
+           "coda_gemm_scaled", "coda_grad_scaled", "coda_attention", "coda_attention_bwd", "coda_cache_store", "coda_attention_cached")
 _binding.ctypes_calls(*(getattr(_lib, _n) for _n in _NATIVE))
 for _n in _NATIVE:
     setattr(_lib, _n, getattr(_binding, _n))
@@ -430,78 +430,47 @@ def coda_grad_scaled_workspace_bytes(M, N, K):
 
 
 # --- attention: Q, K, V and their gradients are bf16 [tokens x heads * dim] (column blocks of a QKV matrix too), seq_q, seq_k int32 [sequences + 1] ---
-def _ints(t, shape, what):
-    """The address of an int32 tensor, dense, of `shape`."""
-    if t is None:
-        return None
-    assert t.dtype == _torch.int32 and t.shape == shape and t.is_contiguous(), "%s: a dense int32 tensor of shape %s expected" % (what, tuple(shape))
-    return t.data_ptr()
-
-
 def _sequences(seq_q, seq_k):
     n = seq_q.shape[0] - 1
     assert n >= 0, "seq_q: sequences + 1 offsets expected"
-    return _ints(seq_q, (n + 1,), "seq_q"), _ints(seq_k, (n + 1,), "seq_k"), n
-
-
-def _output(t, shape, what):
-    """The address and the pitch of a bf16 output."""
-    assert t.dtype == _torch.bfloat16 and t.shape == shape and (t.shape[1] <= 1 or t.stride(1) == 1), "%s: a row-major bf16 tensor of shape %s expected" % (what, tuple(shape))
-    return t.data_ptr(), t.stride(0)
-
-
-def _row_stats(t, heads, rows, what):
-    if t is None:
-        return None
-    assert t.dtype == _torch.float32 and t.shape == (heads, rows) and t.is_contiguous(), "%s: a dense f32 tensor [heads x rows] expected" % what
-    return t.data_ptr()
+    return _binding.vec(seq_q, _torch.int32, n + 1, None, "seq_q"), _binding.vec(seq_k, _torch.int32, n + 1, None, "seq_k"), n
 
 
 def coda_attention(Q, K, V, seq_q, out, heads, kv_heads, scale, lse=None, seq_k=None, causal=True, stream=None):
     """out: bf16 [Tq x heads * dim]; lse: f32 [heads x Tq] or None; seq_k: None where K and V are packed as Q is."""
-    _torch or _import_torch()
-    at_q, at_k, n = _sequences(seq_q, seq_k)
-    o, ldo = _output(out, Q.shape, "out")
-    _check(_lib.coda_attention(_stream(stream), _binding.mat(Q, False, _DTYPES), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES), at_q, at_k, n,
-                               heads, kv_heads, scale, 1 if causal else 0, o, ldo, _row_stats(lse, heads, Q.shape[0], "lse")))
+    torch = _torch or _import_torch()
+    q, k, v = (_binding.mat(x, False, _DTYPES) for x in (Q, K, V))
+    _check(_lib.coda_attention(_stream(stream), q, k, v, *_sequences(seq_q, seq_k), heads, kv_heads, float(scale), 1 if causal else 0,
+                               *_binding.rows(out, Q, torch.bfloat16, "out"), _binding.vec(lse, torch.float32, heads, Q.shape[0], "lse")))
 
 
 def coda_attention_bwd(Q, K, V, out, dout, lse, seq_q, dQ, dK, dV, heads, kv_heads, scale, workspace, seq_k=None, causal=True, rope=None, stream=None):
     """out, lse: what coda_attention left; dout: the gradient of out.  rope: (cos, sin, pos_q, pos_k) to turn dQ and dK back, pos_k None for pos_q;
     cos / sin: f32 [rows x dim / 2] dense tables, pos_q: int32 [Tq], pos_k: int32 [Tk].  workspace: coda_attention_bwd_workspace_bytes(...) bytes."""
     torch = _torch or _import_torch()
-    at_q, at_k, n = _sequences(seq_q, seq_k)
-    grads = _output(dQ, Q.shape, "dQ") + _output(dK, K.shape, "dK") + _output(dV, V.shape, "dV")
+    mats = [_binding.mat(x, False, _DTYPES) for x in (Q, K, V, out, dout)]
+    bf16, T, Tk = torch.bfloat16, Q.shape[0], K.shape[0]
     turn = None
     if rope is not None:
         cos, sin, pos_q, pos_k = tuple(rope) if len(rope) == 4 else tuple(rope) + (None,)
-        for t in (cos, sin):
-            assert t.dtype == torch.float32 and t.is_contiguous() and t.shape == (cos.shape[0], Q.shape[1] // heads // 2), "dense f32 tables [rows x dim / 2] expected"
-        turn = ctypes.byref(coda_rope(cos.data_ptr(), sin.data_ptr(), _ints(pos_q, (Q.shape[0],), "pos_q"),
-                                      _ints(pos_q if pos_k is None else pos_k, (K.shape[0],), "pos_k"), cos.shape[0]))
-    _check(_lib.coda_attention_bwd(_stream(stream), _binding.mat(Q, False, _DTYPES), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES),
-                                   _binding.mat(out, False, _DTYPES), _binding.mat(dout, False, _DTYPES), _row_stats(lse, heads, Q.shape[0], "lse"), at_q, at_k, n,
-                                   heads, kv_heads, scale, 1 if causal else 0, turn, *grads, *_at(workspace)))
+        n, half = cos.shape[0], Q.shape[1] // max(heads, 1) // 2
+        turn = bytes(coda_rope(_binding.vec(cos, torch.float32, n, half, "cos"), _binding.vec(sin, torch.float32, n, half, "sin"),
+                               _binding.vec(pos_q, torch.int32, T, None, "pos_q"), _binding.vec(pos_q if pos_k is None else pos_k, torch.int32, Tk, None, "pos_k"), n))
+    _check(_lib.coda_attention_bwd(_stream(stream), *mats, _binding.vec(lse, torch.float32, heads, T, "lse"), *_sequences(seq_q, seq_k), heads, kv_heads, float(scale),
+                                   1 if causal else 0, turn, *_binding.rows(dQ, Q, bf16, "dQ"), *_binding.rows(dK, K, bf16, "dK"), *_binding.rows(dV, V, bf16, "dV"),
+                                   *_at(workspace)))
 
 
 def coda_attention_bwd_workspace_bytes(Tq, Tk, n_seqs, heads, kv_heads, head_dim):
     return _lib.coda_attention_bwd_workspace_bytes(Tq, Tk, n_seqs, heads, kv_heads, head_dim)
 
 
-def _cache(k, v):
-    assert k.dtype == v.dtype == _torch.bfloat16 and k.dim() == 4 and k.shape == v.shape and k.is_contiguous() and v.is_contiguous(), \
-        "dense bf16 caches [pages x kv_heads x page x dim] expected"
-    pages, kv_heads, page, dim = k.shape
-    return coda_cache(k.data_ptr(), v.data_ptr(), pages, page, kv_heads, dim)
-
-
 def coda_cache_store(K, V, slots, cache_k, cache_v, stream=None):
     """Rows of K, V: bf16 [T x kv_heads * dim] to slots: int32 [T] (page * places + place, or -1 to leave a row out) of the caches
     [pages x kv_heads x places x dim]."""
-    _torch or _import_torch()
-    cache = _cache(cache_k, cache_v)
-    _check(_lib.coda_cache_store(_stream(stream), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES), _ints(slots, (K.shape[0],), "slots"),
-                                 ctypes.byref(cache)))
+    torch = _torch or _import_torch()
+    _check(_lib.coda_cache_store(_stream(stream), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES),
+                                 _binding.vec(slots, torch.int32, K.shape[0], None, "slots"), _binding.cache(cache_k, cache_v, torch.bfloat16)))
 
 
 def coda_attention_cached(Q, cache_k, cache_v, table, lens, seq_q, out, heads, scale, workspace, tree=None, lse=None, stream=None):
@@ -509,16 +478,16 @@ def coda_attention_cached(Q, cache_k, cache_v, table, lens, seq_q, out, heads, s
     those of the rows; tree: int64 or uint64 [Tq] bits of the sequence's rows that each row sees, None for a chain; workspace:
     coda_attention_cached_workspace_bytes(...) bytes."""
     torch = _torch or _import_torch()
-    cache = _cache(cache_k, cache_v)
     at_q, _, n = _sequences(seq_q, None)
-    assert table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and (table.shape[1] <= 1 or table.stride(1) == 1) and \
-        (n <= 1 or table.stride(0) >= table.shape[1]), \
+    entries, pitch = table.shape[1], table.stride(0)
+    assert table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and (entries <= 1 or table.stride(1) == 1) and (n <= 1 or pitch >= entries), \
         "table: a row-major int32 tensor [sequences x pages] expected"
-    assert tree is None or (tree.dtype in (torch.int64, torch.uint64) and tree.shape == Q.shape[:1] and tree.is_contiguous()), "tree: a 64-bit integer for each row expected"
-    o, ldo = _output(out, Q.shape, "out")
-    _check(_lib.coda_attention_cached(_stream(stream), _binding.mat(Q, False, _DTYPES), ctypes.byref(cache), table.data_ptr(), max(table.stride(0), table.shape[1]),
-                                      table.shape[1], _ints(lens, (n,), "lens"), at_q, n, heads, scale, _ptr(tree), o, ldo,
-                                      _row_stats(lse, heads, Q.shape[0], "lse"), *_at(workspace)))
+    assert tree is None or tree.dtype in (torch.int64, torch.uint64), "tree: a 64-bit integer for each row expected"
+    T = Q.shape[0]
+    _check(_lib.coda_attention_cached(_stream(stream), _binding.mat(Q, False, _DTYPES), _binding.cache(cache_k, cache_v, torch.bfloat16), table.data_ptr(),
+                                      max(pitch, entries), entries, _binding.vec(lens, torch.int32, n, None, "lens"), at_q, n, heads, float(scale),
+                                      None if tree is None else _binding.vec(tree, tree.dtype, T, None, "tree"), *_binding.rows(out, Q, torch.bfloat16, "out"),
+                                      _binding.vec(lse, torch.float32, heads, T, "lse"), *_at(workspace)))
 
 
 def coda_attention_cached_workspace_bytes(Tq, n_seqs, heads, kv_heads, head_dim):

@@ -102,7 +102,6 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
     AttnLoad<DP, PAD, ROWS, KB> load_q(p.f.Q + (int64_t)q.begin * p.f.ldq + (int64_t)kv * group * p.f.D, p.f.ldq, kb, lane, p.f.D),
         load_do(p.dO + (int64_t)q.begin * p.lddo + (int64_t)kv * group * p.f.D, p.lddo, kb, lane, p.f.D);
     const uint16_t *const q_base = load_q.base, *const do_base = load_do.base;
-    const uint32_t stats_off = (lane & 31) * 4;
     static_assert(KB == 2, "a wave for each statistic");
     const float *const stats_base = p.stats + ((int64_t)kb * p.f.heads + (int64_t)kv * group) * p.f.Tq + q.begin;
     // In parts, that a round issues among its products: all waves' at once after the barrier would hold each other up

@@ -162,7 +162,7 @@ struct AttnLane {
 template <int DP>
 __device__ __forceinline__ bf16x8 attn_rows(uint32_t tile_rows, int row_base, int t)
 {
-    return *(const __attribute__((address_space(3))) bf16x8 *)((tile_rows ^ (t << 5)) + row_base * (DP * 2));
+    return *(const __attribute__((address_space(3))) bf16x8 *)(uintptr_t)((tile_rows ^ (t << 5)) + row_base * (DP * 2));
 }
 // Operand of the transposed tile, 32 columns x 16 rows: column 32 db + lane % 32, rows 16 t + 4 (lane / 32) + {0 1 2 3, 8 9 10 11}.  Within 16
 // lanes, lane i of a transposing read supplies the address of row i / 4, columns 4 (i % 4) .. and receives column i of the four rows.
@@ -171,8 +171,8 @@ __device__ __forceinline__ bf16x8 attn_cols(uint32_t tile_cols, int t, int db)
 {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const uint32_t p = tile_cols ^ (db << 6);              // eight rows further the swizzle differs in one bit
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + t * 16 * DP * 2));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)((p ^ 32) + (t * 16 + 8) * DP * 2));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)(p + t * 16 * DP * 2));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(uintptr_t)((p ^ 32) + (t * 16 + 8) * DP * 2));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 

@@ -1,7 +1,7 @@
 // binding.cpp -- the marshalling of coda.py in C: tensors to coda_mat / coda_epi_op, and the calls of the entry points that a
 // program makes for every layer.  A call on a small problem is host work (its kernels take a few microseconds), and most of
 // that was the interpreter and ctypes: a coda_gemm with four ops 10 us before the launch, here 4.2; a 256 x 512 x 256 linear layer of
-// four calls 22.2 -> 18.9 us a pass.  Tensors are asked through their Python methods, so whatever answers to them is accepted as
+// four calls 22.2 -> 18.9 us a pass; storing 64 tokens in a cache 7 -> 5.6, one cached token 10.1 (13.3 a pass with its kernels).  Tensors are asked through their Python methods, so whatever answers to them is accepted as
 // before; arguments of other types than the usual ones go to the ctypes function of the same name.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -227,6 +227,85 @@ PyObject *q8_pitch(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLongLong(pitch);
 }
 
+// Sizes and strides of a tensor of `dims` dimensions and of type `dtype`; false (without an exception) if it is none
+bool tensor(PyObject *t, PyObject *dtype, int dims, int64_t *size, int64_t *stride)
+{
+    PyObject *type = PyObject_GetAttr(t, s_dtype), *shape = type ? PyObject_GetAttr(t, s_shape) : nullptr;
+    PyObject *steps = shape ? PyObject_CallMethodNoArgs(t, s_stride) : nullptr;
+    bool ok = steps != nullptr;
+    if (ok) {
+        const int same = type == dtype ? 1 : PyObject_RichCompareBool(type, dtype, Py_EQ);
+        const Py_ssize_t have = PySequence_Size(shape);
+        ok = same == 1 && have == dims;
+        for (int i = 0; ok && i < dims; ++i) ok = item(shape, i, size + i) && item(steps, i, stride + i);
+    }
+    Py_XDECREF(type);
+    Py_XDECREF(shape);
+    Py_XDECREF(steps);
+    return ok;
+}
+bool dense(int dims, const int64_t *size, const int64_t *stride)
+{
+    int64_t step = 1;
+    for (int i = 0; i < dims; ++i)
+        if (size[i] == 0) return true;
+    for (int i = dims; i-- > 0; step *= size[i])
+        if (size[i] > 1 && stride[i] != step) return false;
+    return true;
+}
+// vec(t, dtype, n, m, what) -> the address of a dense tensor [n], or [n x m] with m not None; None for None
+PyObject *vec(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 5) return PyErr_Format(PyExc_TypeError, "vec takes 5 arguments");
+    if (a[0] == Py_None) Py_RETURN_NONE;
+    const int dims = a[3] == Py_None ? 1 : 2;
+    int64_t size[2], stride[2], want[2] = {PyLong_AsLongLong(a[2]), dims == 2 ? PyLong_AsLongLong(a[3]) : 0};
+    if (PyErr_Occurred()) return nullptr;
+    void *p;
+    if (tensor(a[0], a[1], dims, size, stride) && size[0] == want[0] && (dims == 1 || size[1] == want[1]) && dense(dims, size, stride))
+        return data_ptr(a[0], &p) ? PyLong_FromVoidPtr(p) : nullptr;
+    if (!PyErr_Occurred()) {
+        if (dims == 1) PyErr_Format(PyExc_AssertionError, "%U: a dense tensor of %lld of %S expected", a[4], (long long)want[0], a[1]);
+        else PyErr_Format(PyExc_AssertionError, "%U: a dense tensor of %lld x %lld of %S expected", a[4], (long long)want[0], (long long)want[1], a[1]);
+    }
+    return nullptr;
+}
+// rows(t, like, dtype, what) -> (address, pitch) of a row-major matrix of the shape of `like`
+PyObject *rows(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 4) return PyErr_Format(PyExc_TypeError, "rows takes 4 arguments");
+    int64_t size[2], stride[2], want[2];
+    PyObject *shape = PyObject_GetAttr(a[1], s_shape);
+    if (!shape) return nullptr;
+    const bool ok = PySequence_Size(shape) == 2 && item(shape, 0, want) && item(shape, 1, want + 1);
+    Py_DECREF(shape);
+    if (!ok) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_AssertionError, "row-major 2-D tensor expected");
+    void *p;
+    if (tensor(a[0], a[2], 2, size, stride) && size[0] == want[0] && size[1] == want[1] && (size[1] <= 1 || stride[1] == 1))
+        return data_ptr(a[0], &p) ? Py_BuildValue("NL", PyLong_FromVoidPtr(p), (long long)stride[0]) : nullptr;
+    if (!PyErr_Occurred())
+        PyErr_Format(PyExc_AssertionError, "%U: a row-major tensor of %lld x %lld of %S expected", a[3], (long long)want[0], (long long)want[1], a[2]);
+    return nullptr;
+}
+// cache(k, v, dtype) -> the bytes of a coda_cache
+PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 3) return PyErr_Format(PyExc_TypeError, "cache takes 3 arguments");
+    int64_t k[4], v[4], stride[4];
+    coda_cache c;
+    memset(&c, 0, sizeof c);
+    if (tensor(a[0], a[2], 4, k, stride) && dense(4, k, stride) && tensor(a[1], a[2], 4, v, stride) && dense(4, v, stride) && !memcmp(k, v, sizeof k)) {
+        if (k[1] > INT32_MAX || k[2] > INT32_MAX || k[3] > INT32_MAX) return PyErr_Format(PyExc_AssertionError, "a cache of that size has no layout");
+        c.pages = k[0];
+        c.kv_heads = (int32_t)k[1];
+        c.page = (int32_t)k[2];
+        c.head_dim = (int32_t)k[3];
+        return data_ptr(a[0], &c.k) && data_ptr(a[1], &c.v) ? PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&c), sizeof c) : nullptr;
+    }
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "dense caches [pages x kv_heads x page x dim] of %S expected", a[2]);
+    return nullptr;
+}
+
 // ---- the calls.  Arguments are pointers (an address, None, the bytes of a structure) and numbers; anything else takes the ctypes function.
 struct Args {
     PyObject *const *a;
@@ -252,6 +331,12 @@ struct Args {
         if (over) usual = false;
         return v;
     }
+    int32_t small(int i)
+    {
+        const int64_t v = num(i);
+        if (v < INT32_MIN || v > INT32_MAX) usual = false;
+        return (int32_t)v;
+    }
     float real(int i)
     {
         if (PyFloat_CheckExact(a[i])) return (float)PyFloat_AS_DOUBLE(a[i]);
@@ -260,8 +345,9 @@ struct Args {
     }
 };
 
-enum Call { GEMM, ROW_FINALIZE, ROW_SUMSQ, COL_FINALIZE, LSE_FINALIZE, QUANTIZE, DEQUANTIZE, GEMM_SCALED, GRAD_SCALED, CALLS };
-constexpr int ARITY[CALLS] = {10, 8, 3, 5, 8, 9, 6, 14, 14};
+enum Call { GEMM, ROW_FINALIZE, ROW_SUMSQ, COL_FINALIZE, LSE_FINALIZE, QUANTIZE, DEQUANTIZE, GEMM_SCALED, GRAD_SCALED, ATTENTION, ATTENTION_BWD, CACHE_STORE,
+            ATTENTION_CACHED, CALLS };
+constexpr int ARITY[CALLS] = {10, 8, 3, 5, 8, 9, 6, 14, 14, 14, 23, 5, 17};
 PyObject *g_ctypes[CALLS];           // set once, when coda.py is imported
 
 template <int CALL>
@@ -324,6 +410,44 @@ PyObject *call(PyObject *, PyObject *const *a, Py_ssize_t n)
                 float *G = x.ptr<float>(10);
                 CODA_RUN(coda_grad_scaled(stream, M, N, K, A, sa, lda, B, sb, ldb, G, n8, ws, (size_t)bytes))
             }
+        } else if constexpr (CALL == ATTENTION) {
+            const coda_mat *Q = x.ptr<const coda_mat>(1), *K = x.ptr<const coda_mat>(2), *V = x.ptr<const coda_mat>(3);
+            const int32_t *sq = x.ptr<const int32_t>(4), *sk = x.ptr<const int32_t>(5);
+            const int32_t n_seqs = x.small(6), heads = x.small(7), kv = x.small(8), causal = x.small(10);
+            const float scale = x.real(9);
+            void *out = x.ptr<void>(11);
+            const int64_t ldo = x.num(12);
+            float *lse = x.ptr<float>(13);
+            CODA_RUN(coda_attention(stream, Q, K, V, sq, sk, n_seqs, heads, kv, scale, causal, out, ldo, lse))
+        } else if constexpr (CALL == ATTENTION_BWD) {
+            const coda_mat *m[5];
+            for (int i = 0; i < 5; ++i) m[i] = x.ptr<const coda_mat>(1 + i);
+            const float *lse = x.ptr<const float>(6);
+            const int32_t *sq = x.ptr<const int32_t>(7), *sk = x.ptr<const int32_t>(8);
+            const int32_t n_seqs = x.small(9), heads = x.small(10), kv = x.small(11), causal = x.small(13);
+            const float scale = x.real(12);
+            const coda_rope *rope = x.ptr<const coda_rope>(14);
+            void *dq = x.ptr<void>(15), *dk = x.ptr<void>(17), *dv = x.ptr<void>(19), *ws = x.ptr<void>(21);
+            const int64_t lq = x.num(16), lk = x.num(18), lv = x.num(20), bytes = x.num(22);
+            if (bytes < 0) x.usual = false;
+            CODA_RUN(coda_attention_bwd(stream, m[0], m[1], m[2], m[3], m[4], lse, sq, sk, n_seqs, heads, kv, scale, causal, rope, dq, lq, dk, lk, dv, lv, ws, (size_t)bytes))
+        } else if constexpr (CALL == CACHE_STORE) {
+            const coda_mat *K = x.ptr<const coda_mat>(1), *V = x.ptr<const coda_mat>(2);
+            const int32_t *slots = x.ptr<const int32_t>(3);
+            const coda_cache *c = x.ptr<const coda_cache>(4);
+            CODA_RUN(coda_cache_store(stream, K, V, slots, c))
+        } else if constexpr (CALL == ATTENTION_CACHED) {
+            const coda_mat *Q = x.ptr<const coda_mat>(1);
+            const coda_cache *c = x.ptr<const coda_cache>(2);
+            const int32_t *table = x.ptr<const int32_t>(3), *lens = x.ptr<const int32_t>(6), *sq = x.ptr<const int32_t>(7);
+            const int64_t ldt = x.num(4), cols = x.num(5), ldo = x.num(13), bytes = x.num(16);
+            const int32_t n_seqs = x.small(8), heads = x.small(9);
+            const float scale = x.real(10);
+            const uint64_t *tree = x.ptr<const uint64_t>(11);
+            void *out = x.ptr<void>(12), *ws = x.ptr<void>(15);
+            float *lse = x.ptr<float>(14);
+            if (bytes < 0) x.usual = false;
+            CODA_RUN(coda_attention_cached(stream, Q, c, table, ldt, cols, lens, sq, n_seqs, heads, scale, tree, out, ldo, lse, ws, (size_t)bytes))
         } else {
             const float *pmax = x.ptr<const float>(1), *psum = x.ptr<const float>(2), *ztgt = x.ptr<const float>(5);
             const int64_t M = x.num(3), nblk = x.num(4);
@@ -337,7 +461,7 @@ PyObject *call(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyObject_Vectorcall(g_ctypes[CALL], a, (size_t)n, nullptr);
 }
 
-// ctypes_calls(gemm, row_finalize, row_sumsq, col_finalize, lse_finalize, quantize, dequantize, gemm_scaled, grad_scaled)
+// ctypes_calls(a function for every Call, in their order)
 PyObject *ctypes_calls(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (n != CALLS) return PyErr_Format(PyExc_TypeError, "one function for every call");
@@ -364,6 +488,13 @@ PyMethodDef methods[] = {CODA_FAST("op", op),
                          CODA_FAST("coda_dequantize", call<DEQUANTIZE>),
                          CODA_FAST("coda_gemm_scaled", call<GEMM_SCALED>),
                          CODA_FAST("coda_grad_scaled", call<GRAD_SCALED>),
+                         CODA_FAST("vec", vec),
+                         CODA_FAST("rows", rows),
+                         CODA_FAST("cache", cache),
+                         CODA_FAST("coda_attention", call<ATTENTION>),
+                         CODA_FAST("coda_attention_bwd", call<ATTENTION_BWD>),
+                         CODA_FAST("coda_cache_store", call<CACHE_STORE>),
+                         CODA_FAST("coda_attention_cached", call<ATTENTION_CACHED>),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

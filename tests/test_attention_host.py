@@ -174,6 +174,54 @@ def test_the_binding_asks_for_the_right_tensors(coda):
                                 rope=(torch.zeros(4, 31), torch.zeros(4, 31), ints(8)), stream=0)
 
 
+def test_addresses_of_vectors_matrices_and_caches(coda):
+    b = coda._binding
+    v, m = torch.zeros(6, dtype=torch.int32), torch.zeros(4, 8)
+    assert b.vec(None, torch.int32, 6, None, "v") is None and b.vec(v, torch.int32, 6, None, "v") == v.data_ptr()
+    assert b.vec(v[2:], torch.int32, 4, None, "v") == v.data_ptr() + 8 and b.vec(m, torch.float32, 4, 8, "m") == m.data_ptr()
+    for size in ((0, 8), (4, 0), (0, 0)):                                                   # nothing in it: any strides
+        b.vec(torch.zeros(size), torch.float32, *size, "m")
+        b.vec(torch.zeros(size[::-1]).t(), torch.float32, *size, "m")
+    b.vec(torch.zeros(1, 8)[:, ::8], torch.float32, 1, 1, "m")
+    for bad in (v[::2], v.long()[:3], v[:2], v[:3].view(3, 1), torch.zeros(3), torch.tensor(3, dtype=torch.int32)):
+        with pytest.raises(AssertionError, match="v: a dense tensor of 3 of torch.int32"):
+            b.vec(bad, torch.int32, 3, None, "v")
+    for bad in (m.t(), m[:, :4], m[::2], m.double(), v):
+        with pytest.raises(AssertionError, match="m: a dense tensor of 8 x 4 of torch.float32"):
+            b.vec(bad, torch.float32, 8, 4, "m")
+    for t, pitch in ((m, 8), (torch.zeros(4, 24)[:, 8:16], 24), (torch.zeros(8, 8)[::2], 16)):
+        assert b.rows(t, m, torch.float32, "out") == (t.data_ptr(), pitch)
+    for bad in (m.bfloat16(), m.t(), m[:3], torch.zeros(8, 4).t(), v, None):
+        with pytest.raises((AssertionError, AttributeError)):
+            b.rows(bad, m, torch.float32, "out")
+    k, w = (torch.zeros(3, 2, 16, 8, dtype=torch.bfloat16) for _ in range(2))
+    assert b.cache(k, w, torch.bfloat16) == bytes(coda.coda_cache(k.data_ptr(), w.data_ptr(), 3, 16, 2, 8))
+    for bad in ((k, w.float()), (k[:2], w), (k[:, :1], w[:, :1]), (k.transpose(0, 1), w.transpose(0, 1)), (k[0], w[0])):
+        with pytest.raises(AssertionError, match="dense caches"):
+            b.cache(*bad, torch.bfloat16)
+
+
+def test_calls_take_every_form_of_argument(coda):
+    """Whole numbers for the scale, streams as objects, numbers past 32 bits: as ctypes takes them"""
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32)
+    for stream in (0, ctypes.c_void_p(None), type("S", (), {"cuda_stream": 0})()):
+        coda.coda_attention(bf(0, 128), bf(0, 64), bf(0, 64), ints(2), bf(0, 128), 2, 1, 1, stream=stream)
+        coda.coda_attention_bwd(bf(0, 128), bf(0, 64), bf(0, 64), bf(0, 128), bf(0, 128), torch.zeros(2, 0), ints(2), bf(0, 128), bf(0, 64), bf(0, 64), 2, 1, 1, bf(8),
+                                rope=(torch.zeros(4, 32), torch.zeros(4, 32), ints(0)), stream=stream)
+        coda.coda_cache_store(bf(0, 64), bf(0, 64), ints(0), bf(4, 1, 16, 64), bf(4, 1, 16, 64), stream=stream)
+        coda.coda_attention_cached(bf(0, 128), bf(4, 1, 16, 64), bf(4, 1, 16, 64), ints(1, 4), ints(1), ints(2), bf(0, 128), 2, 1, bf(8), stream=stream)
+    good = (bf(8, 128), bf(8, 64), bf(8, 64), ints(2), bf(8, 128))
+    with pytest.raises(coda.CodaError):
+        coda.coda_attention(*good, 0, 1, 0.1, stream=0)
+    with pytest.raises(coda.CodaError):
+        coda.coda_attention_bwd(*good[:3], bf(8, 128), bf(8, 128), torch.zeros(0, 8), ints(2), bf(8, 128), bf(8, 64), bf(8, 64), 0, 1, 0.1, bf(8),
+                                rope=(torch.zeros(4, 64), torch.zeros(4, 64), ints(8)), stream=0)
+    for bad in (dict(heads=2.0), dict(heads="2"), dict(scale="x")):
+        with pytest.raises((ctypes.ArgumentError, TypeError, ValueError)):
+            coda.coda_attention(*good, **{**dict(heads=2, kv_heads=1, scale=0.1, stream=0), **bad})
+
+
 @pytest.mark.parametrize("rows,keys,causal", [(5, 5, True), (4, 9, True), (6, 4, False), (1, 1, True)])
 def test_the_reference_against_automatic_differentiation(rows, keys, causal):
     g = torch.Generator().manual_seed(rows)
@@ -208,3 +256,24 @@ def test_turning_back_undoes_the_rotation():
     c, s = angle.cos().double()[at], angle.sin().double()[at]
     y = torch.stack((x[:, 0::2] * c - x[:, 1::2] * s, x[:, 0::2] * s + x[:, 1::2] * c), 2).reshape(x.shape)
     assert torch.allclose(R.turn_back(y, angle.cos(), angle.sin(), pos), x, atol=1e-6)
+
+
+def test_registers_and_local_memory_of_the_kernels():
+    """Two waves a SIMD at least, two workgroups of four waves a CU, no spilled registers but the few of one kernel (outside its loop)"""
+    import os
+    import re
+    from paper_2605_19269_amd import build as B
+    if not os.path.exists(B.RESOURCES):
+        B.build(force=True)
+    seen = {}
+    for line in open(B.RESOURCES):
+        name, vgpr, agpr, scratch, spill, lds = line.split()
+        m = re.search(r"attention_(kernel|dq_kernel|dkv_kernel|cached_kernel|join_kernel)I|(cache_store)_kernel", name)
+        if not m:
+            continue
+        kind = m.group(1) or m.group(2)
+        seen[kind] = seen.get(kind, 0) + 1
+        few = kind == "dkv_kernel" and "ILi128E" in name
+        assert int(vgpr) + int(agpr) <= 256 and int(spill) <= (3 if few else 0) and int(scratch) <= (16 if few else 0), line
+        assert int(lds) <= (80 if kind in ("kernel", "dq_kernel") else 160) * 1024, line
+    assert seen == {"kernel": 4, "dq_kernel": 4, "dkv_kernel": 4, "cached_kernel": 8, "join_kernel": 8, "cache_store": 1}
