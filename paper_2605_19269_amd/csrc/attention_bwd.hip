@@ -194,7 +194,7 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
             });
         }
         if (mine)                                          // for the products with the rows' columns; S and dP are masked by selection
-            for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, lane);
+            for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, 0, lane);
         attn_reads_done();
         attn_barrier();
 #pragma unroll
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
         const int k0 = j * KEYS;
         unsigned char *at = smem + (j & 1) * 2 * TILE;
         if (k0 + KEYS > whole) {
-            attn_clean(at + wave * (TILE / BWD_WAVES), TILE / BWD_WAVES, lane);
+            attn_clean(at + wave * (TILE / BWD_WAVES), TILE / BWD_WAVES, 0, lane);
             attn_reads_done();
             attn_barrier();
         }

@@ -265,7 +265,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                     }
                     if (cleaned(j)) {
                         constexpr int PART = C::TILE / C::GROUP;
-                        if (attn_clean(slot(j, 1) + member * PART, PART, lane)) dirty = 1;
+                        if (attn_clean(slot(j, 1) + member * PART, PART, PART, lane)) dirty = 1;
                         attn_reads_done();
                         attn_barrier();
                     }
@@ -286,7 +286,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                     else attn_wait_but<0>();
                     if (here) {
                         if (cleaned(j)) {
-                            if (attn_clean(slot(j, 1), C::TILE, lane)) bad = true;
+                            if (attn_clean(slot(j, 1), C::TILE, C::TILE, lane)) bad = true;
                             attn_reads_done();
                         }
                         attn_values<DP, NB, 4>(attn_lds(slot(j, 1)) + in.cols, w, acc.o);

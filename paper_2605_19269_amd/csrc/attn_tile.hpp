@@ -217,8 +217,8 @@ __device__ __forceinline__ u32x4 attn_store_unit(const float (&lo)[4], const flo
 // NaN 2^20; sums over a tile are exact in fp32) tells for each output whether it met +inf, -inf, both or a NaN.  Whatever order a sum takes
 // these in, the result is the same, so the end is early enough.
 
-// `bytes` of a tile from `tile` on (a multiple of 1024) by one wave; true if something was not finite
-__device__ __forceinline__ bool attn_clean(unsigned char *tile, int bytes, int lane)
+// `bytes` of a tile from `tile` on (a multiple of 1024) by one wave; true if something in the first `there` of them (rows behind were not loaded) was not finite
+__device__ __forceinline__ bool attn_clean(unsigned char *tile, int bytes, int there, int lane)
 {
     bool found = false;
     for (int i = lane * 16; i < bytes; i += 1024) {
@@ -227,7 +227,7 @@ __device__ __forceinline__ bool attn_clean(unsigned char *tile, int bytes, int l
 #pragma unroll
         for (int e = 0; e < 4; ++e) top |= ((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
         if (top) {
-            found = true;
+            found |= i < there;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if ((v[e] & 0x7f80u) == 0x7f80u) v[e] &= 0xffff0000u;

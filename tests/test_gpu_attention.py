@@ -104,6 +104,48 @@ def test_rows_of_no_sequence_and_columns_beside_the_output_stay(coda):
     both(coda, [33, 70], None, 4, 2, 64, True, seed=4, behind=9, pad=24)
 
 
+def behind_empty(D, heads, streams):
+    """How many empty sequences a call takes along for its rows to be shared by `streams` waves: sequences count half a tile each"""
+    room = 288 if D > 64 else 576
+    return {4: 0, 2: 2 * room // heads + 20, 1: 4 * room // heads + 20}[streams]
+
+
+@pytest.mark.parametrize("D", [40, 64, 96, 128])
+@pytest.mark.parametrize("streams", [1, 2, 4])
+@pytest.mark.parametrize("lens,past,causal", [([65], None, True), ([129, 31, 1], None, True), ([257, 0, 64], None, False), ([300], 70, True), ([300, 140], -37, True),
+                                              ([40], 500, False)])
+def test_rows_shared_by_waves(coda, lens, past, causal, streams, D):
+    """However many waves share 32 rows, and whatever tile of keys is a stream's last"""
+    extra = behind_empty(D, 4, streams)
+    if past is not None and past > 0:                                                    # no rows, but keys
+        q_at, k_at = offsets(lens + [0] * extra), offsets([n + past for n in lens] + [0] * extra)
+        Q = qkv(q_at[-1], 4, 2, D, streams)[0]
+        _, K, V = qkv(k_at[-1], 4, 2, D, streams + 10)
+        out, lse = run(coda, Q, K, V, q_at, k_at, 4, 2, D ** -0.5, causal)
+        o, m, b_o, b_m = expected(Q, K, V, q_at, k_at, 4, 2, D, D ** -0.5, causal)
+        R.check(out, o, b_o, "out")
+        R.check(lse, m, b_m, "lse")
+    else:
+        both(coda, lens + [0] * extra, past, 4, 2, D, causal, seed=streams)
+
+
+@pytest.mark.parametrize("streams", [1, 2, 4])
+def test_what_is_masked_has_no_effect_on_shared_rows(coda, streams):
+    D, lens = 64, [300, 90]
+    at = offsets(lens + [0] * behind_empty(D, 2, streams))
+    Q, K, V = qkv(at[-1], 2, 1, D, 21)
+    clean = run(coda, Q, K, V, at, at, 2, 1, D ** -0.5, True)
+    V[140, 3], V[141, 3], V[150, 5], V[260, 7], K[280] = math.inf, -math.inf, math.nan, -math.inf, math.nan
+    out, lse = run(coda, Q, K, V, at, at, 2, 1, D ** -0.5, True)
+    keep = [c for c in range(64) if c not in (3, 5, 7)]
+    for h in range(2):
+        x, y = out[:, h * D: (h + 1) * D], clean[0][:, h * D: (h + 1) * D]
+        assert torch.equal(x[:140], y[:140]) and torch.equal(x[300:], y[300:]) and torch.equal(x[:280, keep], y[:280, keep])
+        assert x[140, 3] == math.inf and torch.isnan(x[141:300, 3]).all() and torch.isnan(x[150:300, 5]).all() and (x[260:280, 7] == -math.inf).all()
+        assert torch.equal(x[:150, 5], y[:150, 5]) and torch.equal(x[:260, 7], y[:260, 7]) and torch.isnan(x[280:300]).all()
+    assert torch.equal(lse[:, :280], clean[1][:, :280]) and torch.isnan(lse[:, 280:300]).all() and torch.equal(lse[:, 300:], clean[1][:, 300:])
+
+
 @pytest.mark.parametrize("scale,size", [(1e-6, 1.0), (3.0, 1.0), (0.125, 30.0)])
 def test_flat_and_steep_weights(coda, scale, size):
     """Scores next to each other, and so far apart that one key has all the weight: hundreds between them"""
