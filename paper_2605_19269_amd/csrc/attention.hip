@@ -186,8 +186,7 @@ static int fwd_split(const AttnParams &p)
 {
     if (p.Tk <= 64) return 1;
     const int64_t room = p.D > 64 ? 288 : 576;
-    const auto tiles = [&](int rows) { return (int64_t)(p.Tq - 1) / rows + 1 + (p.n_seqs - 1) / 2; };
-    return tiles(32) * p.heads <= room ? 4 : tiles(64) * p.heads <= 2 * room ? 2 : 1;
+    return attn_about(p.Tq, p.n_seqs, 32) * p.heads <= room ? 4 : attn_about(p.Tq, p.n_seqs, 64) * p.heads <= 2 * room ? 2 : 1;
 }
 int64_t attn_workgroups(const AttnParams &p) { return ((int64_t)p.Tq * fwd_split(p) / (32 * FWD_WAVES) + p.n_seqs) * p.heads; }
 

@@ -49,11 +49,12 @@ __device__ __forceinline__ int64_t bwd_angle(const BwdParams &p, const int32_t *
     return p.cos && there ? (int64_t)min(max(*pos, 0), p.rope_rows - 1) * (p.f.D / 2) : 0;
 }
 
-// dK and dV.  The four waves are two blocks of 32 keys times two streams: a stream takes every second of the (head of the group, 32 rows) pairs that
-// see the keys, and the two are added up at the end.  S = Q K^T and dP = dO V^T have the lane's key in their columns, so P and dS are
-// operands of dV^T += dO^T P and dK^T += Q^T dS as they stand.
+// dK and dV.  The waves are KB blocks of 32 keys times NS streams: a stream takes every NS-th of the (32 rows, head of the group) pairs that see the keys, and the
+// streams are added up at the end.  S = Q K^T and dP = dO V^T have the lane's key in their columns, so P and dS are operands of dV^T += dO^T P and
+// dK^T += Q^T dS as they stand.  K, and V where D is at most 64, stay in registers; Q and dO are read from LDS twice, by rows and by columns: at D = 128, 40 KB of LDS
+// for 2 MFLOP a wave and round, 2560 of the CU's cycles for its 8 waves against 2048 of products.
 template <int DP, bool PAD, int KB, int NS>
-__global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParams p, float c)
+__global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kernel(BwdParams p, float c)
 {
     constexpr bool VLDS = DP == 128;                       // 32 registers that there are not
     constexpr int ROWS = 32, TILE = ROWS * DP * 2, STAGE = 2 * TILE + 256, KEYS = KB * 32;
@@ -102,7 +103,6 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
     AttnLoad<DP, PAD, ROWS, KB> load_q(p.f.Q + (int64_t)q.begin * p.f.ldq + (int64_t)kv * group * p.f.D, p.f.ldq, kb, lane, p.f.D),
         load_do(p.dO + (int64_t)q.begin * p.lddo + (int64_t)kv * group * p.f.D, p.lddo, kb, lane, p.f.D);
     const uint16_t *const q_base = load_q.base, *const do_base = load_do.base;
-    static_assert(KB == 2, "a wave for each statistic");
     const float *const stats_base = p.stats + ((int64_t)kb * p.f.heads + (int64_t)kv * group) * p.f.Tq + q.begin;
     // In parts, that a round issues among its products: all waves' at once after the barrier would hold each other up
     constexpr int PARTS = ROWS * DP * 2 / 1024 / KB;       // 1 KB loads of Q, and of dO, of a wave
@@ -119,14 +119,16 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
         }
         if (part < PARTS) load_q.next(part);
         else if (part < 2 * PARTS) load_do.next(part - PARTS);
-        else                                               // one wave has lse, the other delta
-            attn_load4(stats_base + (int64_t)x.head * p.f.Tq + row0, lane * 4, __builtin_amdgcn_readfirstlane(at + 2 * TILE + kb * ROWS * 4),
-                       attn_first_lanes(max(0, min(q.count - row0, ROWS))));
+        else                                               // one wave has lse, the other delta, or the only one both
+#pragma unroll
+            for (int i = 0; i < 2 / KB; ++i)
+                attn_load4(stats_base + ((int64_t)i * p.f.heads + x.head) * p.f.Tq + row0, lane * 4, __builtin_amdgcn_readfirstlane(at + 2 * TILE + (kb + i) * ROWS * 4),
+                           attn_first_lanes(max(0, min(q.count - row0, ROWS))));
     };
     // some of the tile's rows do not see all of the workgroup's keys, or are none
     const auto ahead_of_keys = [&](int tile) { return p.f.causal && tile * ROWS + ahead < key0 + KEYS - 1; };
     const auto ragged = [&](int tile) { return tile * ROWS + ROWS > q.count; };
-    if (VLDS) AttnLoad<DP, PAD, KEYS, KB * NS>(p.f.V + (int64_t)k.begin * p.f.ldv + (int64_t)kv * p.f.D, p.f.ldv, wave, lane, p.f.D)(key0, k.count, v_tile);
+    if constexpr (VLDS) AttnLoad<DP, PAD, KEYS, KB * NS>(p.f.V + (int64_t)k.begin * p.f.ldv + (int64_t)kv * p.f.D, p.f.ldv, wave, lane, p.f.D)(key0, k.count, v_tile);
     const AttnLane<DP> in(lane);
     const uint32_t v_rows = attn_lds(v_tile) + kb * 32 * DP * 2 + in.rows;
     Place here = place(stream);
@@ -149,11 +151,11 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
         const int row0 = now.tile * ROWS;
         const uint32_t rows = attn_lds(at) + in.rows, cols = attn_lds(at) + in.cols;      // of Q; dO's tile is behind it
         const float *stats = reinterpret_cast<const float *>(at + 2 * TILE);
-        const auto issue = [&](int product) {              // a load behind every second product of S and dP
-            if (product % 2 == 0 && product / 2 <= 2 * PARTS) load(here, (i + 1) & 1, product / 2);
+        const auto issue = [&](int product) {              // a load behind every product of S and dP, or every second
+            if (product % KB == 0) load(here, (i + 1) & 1, product / KB);
             if (product == DP / 8 - 1) load(here, (i + 1) & 1, 2 * PARTS);
         };
-        static_assert(2 * PARTS <= DP / 16, "a place for every load");
+        static_assert(2 * PARTS * KB == DP / 8, "a place for every load");
         // S, and dO V^T - delta: those accumulators begin with -delta
         f32x16 sc = {}, dp;
 #pragma unroll
@@ -261,13 +263,14 @@ __global__ __launch_bounds__(KB * NS * 64, 2) void attention_dkv_kernel(BwdParam
     }
 }
 
-// dQ, as the forward kernel goes: S^T = K Q^T and dP^T = V dO^T with the lane's row in their columns, dQ^T += K^T dS^T
-template <int DP, bool PAD>
+// dQ, as the forward kernel goes, SPLIT waves for 32 rows with every SPLIT-th tile of KEYS keys each: S^T = K Q^T and dP^T = V dO^T with the lane's row in their columns, dQ^T += K^T dS^T
+template <int DP, bool PAD, int SPLIT, int KEYS>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float c)
 {
-    constexpr int ROWS = 128, KEYS = 64, TILE = KEYS * DP * 2;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * TILE];
+    constexpr int NW = BWD_WAVES / SPLIT, ROWS = NW * 32, TILE = KEYS * DP * 2, ROUND = SPLIT * KEYS;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * SPLIT * TILE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int block = wave % NW, stream = wave / NW;
     const int64_t tiles = (int64_t)gridDim.x / p.f.heads;
     const int64_t t = tiles - 1 - blockIdx.x / p.f.heads;
     int head = blockIdx.x % p.f.heads;
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
     if (first < 0 || first >= q.count) return;
     const int row0 = (int)first, ahead = k.count - q.count, kv = head / (p.f.heads / p.f.kv_heads);
     const uint16_t *K = p.f.K + (int64_t)k.begin * p.f.ldk + (int64_t)kv * p.f.D, *V = p.f.V + (int64_t)k.begin * p.f.ldv + (int64_t)kv * p.f.D;
-    const int row = row0 + wave * 32 + (lane & 31), last = min(row, q.count - 1);
+    const int row = row0 + block * 32 + (lane & 31), last = min(row, q.count - 1);
     bf16x8 qf[DP / 16], of[DP / 16];
     {
         const uint16_t *Q = p.f.Q + ((int64_t)q.begin + last) * p.f.ldq + (int64_t)head * p.f.D, *dO = p.dO + ((int64_t)q.begin + last) * p.lddo + (int64_t)head * p.f.D;
@@ -302,28 +305,29 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
         }
         const f32x2 both = attn_halves(delta);
         delta = both[0] + both[1];
-        if (h == 0 && row < q.count) {
+        if (h == 0 && stream == 0 && row < q.count) {
             float *stats = p.stats + (int64_t)head * p.f.Tq + q.begin + row;
             stats[0] = l2;
             stats[(int64_t)p.f.heads * p.f.Tq] = delta;
         }
     }
     const auto sees = [&](int r) { return p.f.causal ? min(max(r + ahead + 1, 0), k.count) : k.count; };
-    const int mine = sees(last), low = sees(min(row0 + wave * 32, q.count - 1)), high = row0 + wave * 32 < q.count ? sees(min(row0 + wave * 32 + 31, q.count - 1)) : 0;
+    const int mine = sees(last), low = sees(min(row0 + block * 32, q.count - 1)), high = row0 + block * 32 < q.count ? sees(min(row0 + block * 32 + 31, q.count - 1)) : 0;
     const int keys = sees(min(row0 + ROWS - 1, q.count - 1)), whole = sees(row0);
     const AttnLane<DP> in(lane);
     f32x16 dq[DP / 32];
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
     if (PAD) attn_zero(smem, sizeof(smem), 256);
-    const int n = (keys + KEYS - 1) / KEYS;
-    AttnLoad<DP, PAD, KEYS, BWD_WAVES> load_k(K, p.f.ldk, wave, lane, p.f.D), load_v(V, p.f.ldv, wave, lane, p.f.D);
-    constexpr int PARTS = 2 * load_k.LOADS;
+    const int n = (keys + ROUND - 1) / ROUND;
+    AttnLoad<DP, PAD, KEYS, NW> load_k(K, p.f.ldk, block, lane, p.f.D), load_v(V, p.f.ldv, block, lane, p.f.D);
+    constexpr int PARTS = 2 * load_k.LOADS, EVERY = DP / 8 / PARTS;
+    const auto stage = [&](int j) { return smem + ((j & 1) * SPLIT + stream) * 2 * TILE; };
     const auto load = [&](int j, int part) {               // as in the forward kernel
-        unsigned char *at = smem + (j & 1) * 2 * TILE;
+        unsigned char *at = stage(j);
         if (part == 0) {
-            load_k.begin(j * KEYS, k.count, attn_lds(at));
-            load_v.begin(j * KEYS, k.count, attn_lds(at + TILE));
+            load_k.begin(j * ROUND + stream * KEYS, k.count, attn_lds(at));
+            load_v.begin(j * ROUND + stream * KEYS, k.count, attn_lds(at + TILE));
         }
         if (part < PARTS / 2) load_k.next(part);
         else load_v.next(part - PARTS / 2);
@@ -339,10 +343,10 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
     for (int j = 0; j < n; ++j) {
         attn_wait();
         attn_barrier();
-        const int k0 = j * KEYS;
-        unsigned char *at = smem + (j & 1) * 2 * TILE;
-        if (k0 + KEYS > whole) {
-            attn_clean(at + wave * (TILE / BWD_WAVES), TILE / BWD_WAVES, 0, lane);
+        const int k0 = j * ROUND + stream * KEYS;
+        unsigned char *at = stage(j);
+        if ((j + 1) * ROUND > whole) {
+            attn_clean(at + block * (TILE / NW), TILE / NW, 0, lane);
             attn_reads_done();
             attn_barrier();
         }
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
         const int lim = mine - k0;
         const bool masked = k0 + KEYS > low;
         const uint32_t rows = attn_lds(at) + in.rows;      // of K; V's tile is behind it
-        static_assert(DP / 8 == 2 * PARTS, "a place for every load");
+        static_assert(DP / 8 == EVERY * PARTS, "a place for every load");
 #pragma unroll
         for (int b = 0; b < KEYS / 32; ++b) {
             f32x16 sc = {}, dp;                            // dP - delta: the accumulators begin with -delta
@@ -362,12 +366,12 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
             attn_products<DP / 16, 4>([&](int i) { return attn_rows<DP>(rows, b * 32, i); },
                                       [&](int i, bf16x8 a) {
                                           sc = attn_mfma(a, qf[i], sc);
-                                          if (b == 0 && i % 2 == 0) load(j + 1, i / 2);
+                                          if (b == 0 && i % EVERY == 0) load(j + 1, i / EVERY);
                                       });
             attn_products<DP / 16, 4>([&](int i) { return attn_rows<DP>(rows, KEYS + b * 32, i); },
                                       [&](int i, bf16x8 a) {
                                           dp = attn_mfma(a, of[i], dp);
-                                          if (b == 0 && i % 2 == 0) load(j + 1, PARTS / 2 + i / 2);
+                                          if (b == 0 && i % EVERY == 0) load(j + 1, PARTS / 2 + i / EVERY);
                                       });
 #pragma unroll
             for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, -l2)) * dp[r];
@@ -382,12 +386,48 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(BwdParams p, float
     const int64_t at = (int64_t)q.begin + row;
     const bool there = row < q.count;
     const int64_t angle = bwd_angle(p, p.pos_q + at, there);
+    if constexpr (SPLIT > 1) {                             // the streams' parts are added up in their order
+        constexpr int UNITS = DP / 32 * 4;                 // of four registers, 1 KB each
+        static_assert(BWD_WAVES * UNITS * 1024 <= 4 * SPLIT * TILE, "the parts take the place of the tiles");
+        f32x4 *parts = reinterpret_cast<f32x4 *>(smem) + lane;
+        __syncthreads();
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b) bwd_store<PAD>(dq[b], b, p.f.scale, p, p.cos, angle, p.dQ + at * p.lddq + (int64_t)head * p.f.D, there, h);
+        for (int u = 0; u < UNITS; ++u) {
+            const int g = u % 4 * 4;
+            parts[(wave * UNITS + u) * 64] = f32x4{dq[u / 4][g], dq[u / 4][g + 1], dq[u / 4][g + 2], dq[u / 4][g + 3]};
+        }
+        __syncthreads();
+        for (int b = stream; b < DP / 32; b += SPLIT) {
+            f32x16 sum = {};
+#pragma unroll
+            for (int j = 0; j < SPLIT; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 v = parts[((j * NW + block) * UNITS + b * 4 + g) * 64];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[4 * g + e] += v[e];
+                }
+            bwd_store<PAD>(sum, b, p.f.scale, p, p.cos, angle, p.dQ + at * p.lddq + (int64_t)head * p.f.D, there, h);
+        }
+    } else
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b) bwd_store<PAD>(dq[b], b, p.f.scale, p, p.cos, angle, p.dQ + at * p.lddq + (int64_t)head * p.f.D, there, h);
 }
 
-static int64_t dkv_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tk / 64 + p.f.n_seqs) * p.f.kv_heads; }
-static int64_t dq_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tq / 128 + p.f.n_seqs) * p.f.heads; }
+// How many waves share 32 rows, as in the forward kernel, and for the same reason.  us with SPLIT 1 / 2 / 4, 32 heads over 8: D = 64, a sequence of 256: 10 / 8 / 7,
+// 509: 14 / 11 / 10, 1024: 23 / 18 / 23, 2048: 44 / 42 / 57, 4096: 115 / 128 / 182; D = 128, 256: 14 / 12 / 11, 1024: 35 / 28 / 57, 2048: 71 / 72 / 159 (SPLIT 4 gains too
+// little to be there).
+static int dq_split(const BwdParams &p)
+{
+    const int64_t room = p.f.D > 64 ? 288 : 576;
+    return p.f.D <= 64 && attn_about(p.f.Tq, p.f.n_seqs, 32) * p.f.heads <= room ? 4 : attn_about(p.f.Tq, p.f.n_seqs, 64) * p.f.heads <= 2 * room ? 2 : 1;
+}
+// Keys of a workgroup of dK's kernel: 32, with more streams where LDS has room for them, while there are at most one and a half workgroups a CU.  us with 64 / 32, 32
+// heads over 8: D = 64, a sequence of 509: 26 / 18, 1024: 42 / 28, 1500: 59 / 42, 2048: 77 / 61, 4096: 188 / 225, 4 x 512: 27 / 33; D = 128, 256: 25 / 22,
+// 1024: 67 / 62, 2048: 131 / 133, 4 x 512: 44 / 62.
+static int dkv_keys(const BwdParams &p) { return attn_about(p.f.Tk, p.f.n_seqs, 32) * p.f.kv_heads <= 400 ? 32 : 64; }
+static int64_t dkv_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tk / dkv_keys(p) + p.f.n_seqs) * p.f.kv_heads; }
+static int64_t dq_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tq * dq_split(p) / 128 + p.f.n_seqs) * p.f.heads; }
 
 int64_t bwd_workgroups(const BwdParams &p)
 {
@@ -402,11 +442,19 @@ static hipError_t launch_bwd(const BwdParams &p, hipStream_t s)
     const float c = p.f.scale * LOG2E;
     hipError_t e = hipSuccess;
     if (p.f.Tq > 0) {
-        hipLaunchKernelGGL((attention_dq_kernel<DP, PAD>), dim3((unsigned)dq_workgroups(p)), dim3(256), 0, s, p, c);
+        const dim3 grid((unsigned)dq_workgroups(p));
+        const int split = dq_split(p);
+        if constexpr (DP == 64)
+            if (split == 4) hipLaunchKernelGGL((attention_dq_kernel<DP, PAD, 4, 32>), grid, dim3(256), 0, s, p, c);
+        if (split == 2) hipLaunchKernelGGL((attention_dq_kernel<DP, PAD, 2, 32>), grid, dim3(256), 0, s, p, c);
+        if (split == 1) hipLaunchKernelGGL((attention_dq_kernel<DP, PAD, 1, 64>), grid, dim3(256), 0, s, p, c);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.f.Tk > 0) {
-        hipLaunchKernelGGL((attention_dkv_kernel<DP, PAD, 2, 4>), dim3((unsigned)dkv_workgroups(p)), dim3(512), 0, s, p, c);
+        const dim3 grid((unsigned)dkv_workgroups(p));
+        constexpr int NS = DP == 64 ? 8 : 4;               // streams that LDS has room for
+        if (dkv_keys(p) == 32) hipLaunchKernelGGL((attention_dkv_kernel<DP, PAD, 1, NS>), grid, dim3(NS * 64), 0, s, p, c);
+        else hipLaunchKernelGGL((attention_dkv_kernel<DP, PAD, 2, 4>), grid, dim3(512), 0, s, p, c);
         e = hipGetLastError();
     }
     return e;

@@ -17,6 +17,8 @@ struct AttnParams {
     int64_t ldo;
     float *lse;                        // [heads x Tq] or null
 };
+// About how many tiles of `rows` rows n_seqs sequences of T rows come to, where each but one adds half a tile (their lengths are on the device)
+inline int64_t attn_about(int T, int n_seqs, int rows) { return ((int64_t)T - 1) / rows + 1 + (n_seqs - 1) / 2; }
 int64_t attn_workgroups(const AttnParams &p);
 hipError_t launch_attention(const AttnParams &p, hipStream_t s);
 

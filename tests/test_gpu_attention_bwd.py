@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests import attn_ref as R
-from tests.test_gpu_attention import FILL, coda, device, offsets, qkv  # noqa: F401
+from tests.test_gpu_attention import FILL, behind_empty, coda, device, offsets, qkv  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -123,6 +123,27 @@ def test_full(coda, lens):
 @pytest.mark.parametrize("D", [64, 128])
 def test_rope_and_rows_of_no_sequence(coda, D):
     Pass(coda, [33, 70], None, 4, 2, D, True, seed=4, behind=9, rope=True).check()
+
+
+@pytest.mark.parametrize("D", [40, 64, 96, 128])
+@pytest.mark.parametrize("streams", [1, 2, 4])
+@pytest.mark.parametrize("lens,past,causal", [([65], None, True), ([129, 31, 1], None, True), ([257, 0, 64], None, False), ([300, 140], -37, True)])
+def test_rows_shared_by_waves(coda, lens, past, causal, streams, D):
+    """However many waves share 32 rows, and 32 or 64 keys a workgroup (empty sequences stand for their half tile there too)"""
+    p = Pass(coda, lens + [0] * behind_empty(D, 4, streams), past, 4, 2, D, causal, seed=streams, rope=streams == 2)
+    p.check()
+
+
+@pytest.mark.parametrize("streams", [1, 2, 4])
+def test_what_is_masked_has_no_effect_on_shared_rows(coda, streams):
+    p = Pass(coda, [200, 90] + [0] * behind_empty(64, 2, streams), None, 2, 1, 64, True, seed=31)
+    clean = p.run()
+    p.K[150], p.V[160:200] = math.nan, math.inf
+    coda.coda_attention(p.Q, p.K, p.V, p.seq_q, p.out, 2, 1, p.scale, lse=p.lse)           # what is saved is that of these keys and values
+    got = p.run()
+    for x, y in zip(got, clean):
+        assert torch.equal(x[200:], y[200:])
+    assert torch.equal(got[0][:150], clean[0][:150]) and not torch.isfinite(got[0][150:200]).all(1).any()
 
 
 @pytest.mark.parametrize("scale,size", [(1e-6, 1.0), (3.0, 1.0)])
