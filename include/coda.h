@@ -411,7 +411,7 @@ typedef struct coda_rope {
  * dK and dV are summed over the query heads of their group.  rope (host, may be NULL): dQ and dK are turned back, i.e. are the gradients of
  * the QKV projection's outputs before its ROPE epilogue (pairs of columns of all D; D a multiple of 8 as there).
  * dQ, dK, dV: bf16 of the shapes of Q, K, V, overwritten; they may be column blocks of one matrix.  Rows of no sequence are left as they are; a key
- * that no row sees has gradients of zero.  P and dS are rounded to bf16 for their products, sums are fp32; the order of additions depends on the
+ * that no row sees has gradients of zero.  P and dS are rounded to bf16 for their products (dS in two parts for that of dQ), sums are fp32; the order of additions depends on the
  * sizes only (no atomics).  A row of dO that is not finite makes NaN or infinities of what it reaches, and of nothing else.
  * workspace: device memory, 16-byte aligned, coda_attention_bwd_workspace_bytes(...) bytes (CODA_ERR_WORKSPACE below that); it holds nothing
  * between calls, and two calls that share one must not overlap in time.

@@ -190,6 +190,23 @@ __device__ __forceinline__ bf16x8 attn_operand(const f32x16 &x, int half)
     for (int e = 0; e < 4; ++e) v[e] = attn_pack(x[half * 8 + 2 * e], x[half * 8 + 2 * e + 1]);
     return __builtin_bit_cast(bf16x8, v);
 }
+// The whole accumulator as operands of two products that are added up: its upper bits, cut off, and what they leave, to the nearest bf16: off by 2^-16 at most
+__device__ __forceinline__ void attn_two_parts(const f32x16 &x, bf16x8 (&hi)[2], bf16x8 (&lo)[2])
+{
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        u32x4 a, b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float f = x[u * 8 + 2 * e], g = x[u * 8 + 2 * e + 1];                    // a bit cast of an element of the vector takes the first one each time
+            const uint32_t p = __builtin_bit_cast(uint32_t, f), q = __builtin_bit_cast(uint32_t, g);
+            a[e] = __builtin_amdgcn_perm(q, p, 0x07060302u);
+            b[e] = attn_pack(f - __builtin_bit_cast(float, p & 0xffff0000u), g - __builtin_bit_cast(float, q & 0xffff0000u));
+        }
+        hi[u] = __builtin_bit_cast(bf16x8, a);
+        lo[u] = __builtin_bit_cast(bf16x8, b);
+    }
+}
 // Row of the accumulator that register r of a lane of half h holds
 __device__ __forceinline__ int attn_acc_row(int r, int h) { return (r & 3) + 8 * (r >> 2) + 4 * h; }
 

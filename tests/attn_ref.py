@@ -62,7 +62,8 @@ def gradients(q, k, v, o, do, lse, scale, see):
     n = max(s.shape)
     dq, dk, dv = scale * ds @ k, scale * ds.t() @ q, p.t() @ do
     # sums of fp32: as many additions as terms
-    b_dq = scale * (b_ds + n * F32 * ds.abs()) @ k.abs()
+    b_2 = ds.abs() * (2.0 ** -16 + rel) + p * e_dp                                       # in two parts for dQ: 8 bits cut off, the rest of them rounded
+    b_dq = scale * (b_2 + 2 * n * F32 * ds.abs()) @ k.abs()
     b_dk = scale * (b_ds + n * F32 * ds.abs()).t() @ q.abs()
     b_dv = (b_p + n * F32 * p).t() @ do.abs()
     return dq, dk, dv, b_dq, b_dk, b_dv
