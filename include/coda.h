@@ -424,7 +424,7 @@ CODA_API size_t coda_attention_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int32
 
 /*
  * A paged cache of keys and values: k and v are bf16 [pages][kv_heads][page][head_dim], dense, 16-byte aligned.  page, the keys of a page, is a power of
- * two; head_dim as above; pages * page < 2^31.  Slot page * p + i is place i of page p.
+ * two; head_dim as above; pages * page < 2^31, page * kv_heads * head_dim < 2^31.  Slot page * p + i is place i of page p.
  */
 typedef struct coda_cache {
     void *k, *v;                        /* device */
@@ -442,6 +442,7 @@ CODA_API coda_status coda_cache_store(void *stream, const coda_mat *K, const cod
  * sequence), and rows seq_q[s] .. seq_q[s + 1] - 1 of Q.  The last of its keys are those of its rows, in their order (coda_cache_store comes first).
  * Row i sees all keys before those, and key j of them if j <= i, or, with tree (uint64 [Tq], device; NULL for none), where bit j of the row's tree is
  * set; with a tree, rows and bits from 64 on have no key of their own.  Where lens[s] is below the number of rows the keys are those of the last rows.
+ * table_pages * page is at most 2^30, rows of Q times heads / kv_heads below 2^31.
  * lens are taken between 0 and table_pages * page and entries of the table to the nearest page, whatever they hold; entries behind a sequence's keys are
  * not read, nor are places of the last page behind them.
  *

@@ -4,8 +4,10 @@
 //   dV = P^T dO,  dQ = scale dS K,  dK = scale dS^T Q
 //
 // Two kernels, no atomics: dQ, a workgroup for 128 rows, over the keys, which also leaves the row statistics; dK and dV, a workgroup for 64 keys of a key / value
-// head, over all rows of all heads of the group.  S and dO V^T are formed in both (seven products where five would do): the
-// alternative, dQ added up in fp32 across workgroups, is either of no fixed order or a partial of every row for every tile of keys.
+// head, over all rows of all heads of the group.  S and dO V^T are formed in both (eight products, with dS in two parts, where five would do): the
+// alternative, dQ added up in fp32 across workgroups, is either of no fixed order or a partial of every row for every tile of keys.  Bound by the issue of vector instructions and products
+// on one port, dK and dV at 128 columns also by LDS: 4 x 2048 rows, 32 heads over 8 of 64 columns, 159 + 213 us (740 TFLOP/s over the eight products), 8192 rows in six
+// sequences of 128 columns 368 + 460 (860).
 #include "attn_launch.hpp"
 #include "attn_tile.hpp"
 

@@ -110,14 +110,14 @@ def cached(coda, **over):
 
 
 CACHES = [("NULL", dict(cache=None)), ("NULL", dict(cache=dict(k=0))), ("NULL", dict(cache=dict(v=0))), ("SHAPE", dict(cache=dict(pages=-1))),
-          ("SHAPE", dict(cache=dict(page=0))), ("SHAPE", dict(cache=dict(page=-16))), ("SHAPE", dict(cache=dict(page=24))), ("SHAPE", dict(cache=dict(pages=1 << 27))),
+          ("SHAPE", dict(cache=dict(page=0))), ("SHAPE", dict(cache=dict(page=-16))), ("SHAPE", dict(cache=dict(page=24))), ("SHAPE", dict(cache=dict(pages=1 << 27))), ("SHAPE", dict(cache=dict(pages=2, page=1 << 24))),
           ("SHAPE", dict(cache=dict(head_dim=136))), ("SHAPE", dict(cache=dict(head_dim=20))), ("SHAPE", dict(cache=dict(kv_heads=0))), ("ALIGN", dict(cache=dict(k=P + 8)))]
 
 
 @pytest.mark.parametrize("want,over", CACHES + [
     ("NULL", dict(Q=None)), ("NULL", dict(Q=dict(ptr=0))), ("NULL", dict(table=0)), ("NULL", dict(lens=0)), ("NULL", dict(seq_q=0)), ("NULL", dict(out=0)), ("NULL", dict(ws=0)),
     ("DTYPE", dict(Q=dict(dtype=2))), ("SHAPE", dict(Q=dict(trans=1))), ("SHAPE", dict(heads=3)), ("SHAPE", dict(heads=0)), ("SHAPE", dict(n=-1)), ("SHAPE", dict(scale=0.0)),
-    ("SHAPE", dict(ld=4)), ("SHAPE", dict(cols=-1)), ("SHAPE", dict(cols=(1 << 26) + 1, ld=1 << 27)), ("SHAPE", dict(T=1 << 31)), ("SHAPE", dict(ldo=128)),
+    ("SHAPE", dict(ld=4)), ("SHAPE", dict(cols=-1)), ("SHAPE", dict(cols=(1 << 26) + 1, ld=1 << 27)), ("SHAPE", dict(T=1 << 30)), ("SHAPE", dict(T=1 << 31)), ("SHAPE", dict(ldo=128)),
     ("ALIGN", dict(table=P + 2)), ("ALIGN", dict(lens=P + 1)), ("ALIGN", dict(tree=P + 4)), ("ALIGN", dict(out=P + 8)), ("ALIGN", dict(lse=P + 2)), ("ALIGN", dict(ws=P + 4)),
     ("WORKSPACE", dict(nbytes=1000))])
 def test_cached_refuses(coda, want, over):
