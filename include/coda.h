@@ -389,7 +389,8 @@ CODA_API size_t coda_grad_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K
  *
  * over the keys j of row i's sequence, with causal != 0 those up to j = i + keys - rows (both counted from the sequence's start: the last row
  * sees all keys).  A row that sees no key is zeros with lse = -inf.  What a row does not see has no effect on it, infinities and NaN included.
- * lse (natural logarithm): f32 [heads x Tq], may be NULL.  scale is positive and finite (CODA_ERR_SHAPE).
+ * lse (natural logarithm): f32 [heads x Tq], may be NULL.  scale is positive and below 2^127, and neither
+ * Tk nor Tq times heads / kv_heads is above 2^31 - 512 (CODA_ERR_SHAPE).
  *
  * Products are exact, sums, maxima and lse in fp32; the weights exp(S - max) are rounded to bf16 for their product with V (error of an output: about that of one
  * rounding to bf16 again), their sum is taken before.  The order of additions depends on the sizes only.
@@ -442,7 +443,7 @@ CODA_API coda_status coda_cache_store(void *stream, const coda_mat *K, const cod
  * sequence), and rows seq_q[s] .. seq_q[s + 1] - 1 of Q.  The last of its keys are those of its rows, in their order (coda_cache_store comes first).
  * Row i sees all keys before those, and key j of them if j <= i, or, with tree (uint64 [Tq], device; NULL for none), where bit j of the row's tree is
  * set; with a tree, rows and bits from 64 on have no key of their own.  Where lens[s] is below the number of rows the keys are those of the last rows.
- * table_pages * page is at most 2^30, rows of Q times heads / kv_heads below 2^31.
+ * table_pages * page is at most 2^30, rows of Q times heads / kv_heads at most 2^31 - 512.
  * lens are taken between 0 and table_pages * page and entries of the table to the nearest page, whatever they hold; entries behind a sequence's keys are
  * not read, nor are places of the last page behind them.
  *

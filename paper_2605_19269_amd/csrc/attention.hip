@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, DP == 128 && SPLIT == 4 ? 1 : 2) void attentio
         unsigned char *at = stage(j);
         if ((j + 1) * ROUND > whole) {
             constexpr int PART = TILE / NW;
-            if (attn_clean(at + TILE + block * PART, PART, (k.count - k0) * (DP * 2) - block * PART, lane)) dirty = 1;
+            if (attn_clean(at + TILE + block * PART, PART, min(k.count - k0, KEYS) * (DP * 2) - block * PART, lane)) dirty = 1;
             attn_reads_done();
             attn_barrier();
         }

@@ -460,19 +460,21 @@ hipError_t static_scratch(void **out)
 }
 
 // ---- attention ----------------------------------------------------------------------------------------------------------
+constexpr int64_t MAX_ROWS = INT32_MAX - 511;              // rows of the tile behind the last are numbered in 32 bits too
+
 // bf16 [r x c], one row a token
 coda_status check_rows(const coda_mat *X, int64_t r, int64_t c)
 {
     if (!X) return CODA_ERR_NULL;
     if (X->dtype != CODA_BF16) return CODA_ERR_DTYPE;
-    if (X->trans || X->rows < 0 || X->rows > INT32_MAX) return CODA_ERR_SHAPE;
+    if (X->trans || X->rows < 0 || X->rows > MAX_ROWS) return CODA_ERR_SHAPE;
     return check_operand(X, r, c);
 }
 bool heads_fit(int32_t heads, int32_t kv_heads, int64_t head_dim)
 {
     return kv_heads > 0 && heads > 0 && heads % kv_heads == 0 && head_dim >= 8 && head_dim <= 128 && head_dim % 8 == 0 && heads * head_dim <= MAX_LD;
 }
-bool scale_fits(float scale) { return scale > 0.0f && scale < __builtin_inff(); }
+bool scale_fits(float scale) { return scale > 0.0f && scale < 0x1p127f; }        // times log2(e) it is finite
 
 coda_status check_heads(const coda_mat *Q, const coda_mat *K, const coda_mat *V, const int32_t *seq_q, const int32_t *seq_k, int32_t n_seqs, int32_t heads,
                         int32_t kv_heads, float scale, coda::AttnParams &p)
@@ -484,7 +486,7 @@ coda_status check_heads(const coda_mat *Q, const coda_mat *K, const coda_mat *V,
     if ((st = check_rows(Q, Q->rows, heads * D)) != CODA_OK) return st;
     if ((st = check_rows(K, K->rows, kv_heads * D)) != CODA_OK) return st;
     if ((st = check_rows(V, K->rows, kv_heads * D)) != CODA_OK) return st;
-    if ((!seq_k && K->rows != Q->rows) || Q->rows * (heads / kv_heads) > INT32_MAX) return CODA_ERR_SHAPE;
+    if ((!seq_k && K->rows != Q->rows) || Q->rows * (heads / kv_heads) > MAX_ROWS) return CODA_ERR_SHAPE;
     if (n_seqs > 0 && (Q->rows > 0 || K->rows > 0)) {
         if ((st = check_vec(seq_q)) != CODA_OK) return st;
         if (seq_k && !aligned4(seq_k)) return CODA_ERR_ALIGN;
@@ -787,7 +789,7 @@ coda_status coda_attention(void *stream, const coda_mat *Q, const coda_mat *K, c
 
 size_t coda_attention_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int32_t n_seqs, int32_t heads, int32_t kv_heads, int32_t head_dim)
 {
-    if (Tq <= 0 || Tq > INT32_MAX || Tk < 0 || n_seqs <= 0 || !heads_fit(heads, kv_heads, head_dim)) return 0;
+    if (Tq <= 0 || Tq > MAX_ROWS || Tk < 0 || n_seqs <= 0 || !heads_fit(heads, kv_heads, head_dim)) return 0;
     return coda::bwd_bytes(Tq, heads);
 }
 
@@ -861,7 +863,7 @@ coda_status coda_cache_store(void *stream, const coda_mat *K, const coda_mat *V,
 
 size_t coda_attention_cached_workspace_bytes(int64_t Tq, int32_t n_seqs, int32_t heads, int32_t kv_heads, int32_t head_dim)
 {
-    if (Tq <= 0 || Tq > INT32_MAX || n_seqs <= 0 || !heads_fit(heads, kv_heads, head_dim)) return 0;
+    if (Tq <= 0 || Tq > MAX_ROWS || n_seqs <= 0 || !heads_fit(heads, kv_heads, head_dim)) return 0;
     return coda::cached_bytes(Tq, n_seqs, heads, kv_heads, head_dim);
 }
 
@@ -875,7 +877,7 @@ coda_status coda_attention_cached(void *stream, const coda_mat *Q, const coda_ca
     if (!heads_fit(heads, cache->kv_heads, cache->head_dim) || n_seqs < 0 || !scale_fits(scale)) return CODA_ERR_SHAPE;
     if ((st = check_rows(Q, Q->rows, (int64_t)heads * cache->head_dim)) != CODA_OK) return st;
     const int group = heads / cache->kv_heads;
-    if (Q->rows * group > INT32_MAX || table_pages < 0 || ld_table < table_pages || table_pages > (int64_t(1) << 30) / cache->page) return CODA_ERR_SHAPE;
+    if (Q->rows * group > MAX_ROWS || table_pages < 0 || ld_table < table_pages || table_pages > (int64_t(1) << 30) / cache->page) return CODA_ERR_SHAPE;
     if (Q->rows == 0 || n_seqs == 0) return CODA_OK;
     if ((st = check_vec(lens)) != CODA_OK || (st = check_vec(seq_q)) != CODA_OK) return st;
     const int64_t capacity = cache->pages ? table_pages * cache->page : 0;

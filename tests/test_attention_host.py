@@ -47,6 +47,8 @@ OPERANDS = [
     ("SHAPE", dict(Q=dict(cols=260))), ("SHAPE", dict(D=136)), ("SHAPE", dict(D=60)), ("SHAPE", dict(D=4)), ("SHAPE", dict(K=dict(cols=120, ld=128))),
     ("SHAPE", dict(V=dict(rows=63))), ("SHAPE", dict(Tk=65)), ("SHAPE", dict(Q=dict(ld=248))), ("SHAPE", dict(K=dict(ld=(1 << 22) + 8))), ("SHAPE", dict(Q=dict(rows=-1))),
     ("SHAPE", dict(n=-1)), ("SHAPE", dict(scale=0.0)), ("SHAPE", dict(scale=-1.0)), ("SHAPE", dict(scale=math.inf)), ("SHAPE", dict(scale=math.nan)),
+    ("SHAPE", dict(scale=2.0 ** 127)), ("SHAPE", dict(T=(1 << 31) - 511, heads=1, kv=1, D=8)), ("SHAPE", dict(T=8, Tk=(1 << 31) - 511, seq_k=P)),
+    ("SHAPE", dict(T=(1 << 30) - 255, Tk=8, seq_k=P)),
     ("SHAPE", dict(T=1 << 31, seq_k=P, Tk=8)), ("SHAPE", dict(T=1 << 30, heads=8, kv=1, seq_k=P, Tk=8)),
     ("ALIGN", dict(Q=dict(ptr=P + 8))), ("ALIGN", dict(V=dict(ptr=P + 2))), ("ALIGN", dict(K=dict(ld=132))), ("ALIGN", dict(seq_q=P + 2)), ("ALIGN", dict(seq_k=P + 1)),
 ]
@@ -117,7 +119,7 @@ CACHES = [("NULL", dict(cache=None)), ("NULL", dict(cache=dict(k=0))), ("NULL", 
 @pytest.mark.parametrize("want,over", CACHES + [
     ("NULL", dict(Q=None)), ("NULL", dict(Q=dict(ptr=0))), ("NULL", dict(table=0)), ("NULL", dict(lens=0)), ("NULL", dict(seq_q=0)), ("NULL", dict(out=0)), ("NULL", dict(ws=0)),
     ("DTYPE", dict(Q=dict(dtype=2))), ("SHAPE", dict(Q=dict(trans=1))), ("SHAPE", dict(heads=3)), ("SHAPE", dict(heads=0)), ("SHAPE", dict(n=-1)), ("SHAPE", dict(scale=0.0)),
-    ("SHAPE", dict(ld=4)), ("SHAPE", dict(cols=-1)), ("SHAPE", dict(cols=(1 << 26) + 1, ld=1 << 27)), ("SHAPE", dict(T=1 << 30)), ("SHAPE", dict(T=1 << 31)), ("SHAPE", dict(ldo=128)),
+    ("SHAPE", dict(ld=4)), ("SHAPE", dict(cols=-1)), ("SHAPE", dict(cols=(1 << 26) + 1, ld=1 << 27)), ("SHAPE", dict(T=1 << 30)), ("SHAPE", dict(T=(1 << 30) - 255)), ("SHAPE", dict(scale=2.0 ** 127)), ("SHAPE", dict(T=1 << 31)), ("SHAPE", dict(ldo=128)),
     ("ALIGN", dict(table=P + 2)), ("ALIGN", dict(lens=P + 1)), ("ALIGN", dict(tree=P + 4)), ("ALIGN", dict(out=P + 8)), ("ALIGN", dict(lse=P + 2)), ("ALIGN", dict(ws=P + 4)),
     ("WORKSPACE", dict(nbytes=1000))])
 def test_cached_refuses(coda, want, over):
