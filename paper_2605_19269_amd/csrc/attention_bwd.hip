@@ -67,7 +67,7 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
     const int64_t t = blockIdx.x / p.f.kv_heads;
     const int kv = blockIdx.x % p.f.kv_heads;
     const int s = attn_find(p.f.seq_k, p.f.n_seqs, 1, KEYS, t, lane);
-    const AttnSpan q = attn_span(p.f.seq_q, s, p.f.Tq), k = attn_span(p.f.seq_k, s, p.f.Tk);
+    const AttnSpan q = attn_span_of_wave(p.f.seq_q, s, p.f.Tq), k = attn_span_of_wave(p.f.seq_k, s, p.f.Tk);
     const int64_t first = (t - (max(p.f.seq_k[s], 0) / KEYS + s)) * KEYS;
     if (first < 0 || first >= k.count) return;
     const int key0 = (int)first, ahead = k.count - q.count, group = p.f.heads / p.f.kv_heads;
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
     int head = blockIdx.x % p.f.heads;
     if (p.f.heads % 8 == 0) head = head % 8 * (p.f.heads / 8) + head / 8;
     const int s = attn_find(p.f.seq_q, p.f.n_seqs, 1, ROWS, t, lane);
-    const AttnSpan q = attn_span(p.f.seq_q, s, p.f.Tq), k = attn_span(p.f.seq_k, s, p.f.Tk);
+    const AttnSpan q = attn_span_of_wave(p.f.seq_q, s, p.f.Tq), k = attn_span_of_wave(p.f.seq_k, s, p.f.Tk);
     const int64_t first = (t - (max(p.f.seq_q[s], 0) / ROWS + s)) * ROWS;
     if (first < 0 || first >= q.count) return;
     const int row0 = (int)first, ahead = k.count - q.count, kv = head / (p.f.heads / p.f.kv_heads);

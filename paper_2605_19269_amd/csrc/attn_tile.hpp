@@ -81,45 +81,43 @@ __device__ __forceinline__ void attn_barrier()
     asm volatile("" ::: "memory");
 }
 
-// Tiles of ROWS rows of one head, loaded by NW waves together, 1 KB a load.  PAD: D < DP, the chunks behind D are left as attn_zero() made them.
+// Tiles of ROWS rows of one head, loaded by NW waves together, 1 KB a load.  Loads go through a buffer descriptor that ends with the last row of the tile that there is, so rows behind it need no
+// mask: the card drops lanes past the end, and with them, in PAD kernels, those whose chunk is not below D (attn_zero() has cleared those).  A load is two instructions;
+// masks and 64-bit addresses took 18, a quarter of all that the forward kernel's loop issued.
 template <int DP, bool PAD, int ROWS, int NW>
 struct AttnLoad {
     static constexpr int CH = DP / 8, RPL = 64 / CH, LOADS = ROWS / (NW * RPL);
     static_assert(ROWS % (NW * RPL) == 0, "whole wave-loads");
-    const uint16_t *base;              // element (0, 0) of the head's rows
+    const uint16_t *base;              // element (0, 0) of the head's rows; uniform
     int64_t ld;
     int wave;
-    uint32_t row_off, chunk_off;       // bytes from a load's first row to the lane's, and of its chunk in the first load
-    uint64_t chunks[PAD ? LOADS : 1];  // lanes with a chunk below D
-    // A tile on its way: the next load's first row, how many rows there are from it on, where it goes
-    const uint16_t *from;
-    int left;
+    uint32_t off[LOADS];               // bytes from the tile's first row, at most 64 rows of 2^22 elements
+    // A tile on its way
+    u32x4 buffer;
     uint32_t to;
 
-    static __device__ __forceinline__ int chunk(int i, int wave, int lane) { return (lane % CH) ^ attn_swizzle<DP>((i * NW + wave) * RPL + lane / CH); }
     __device__ __forceinline__ AttnLoad(const uint16_t *base, int64_t ld, int wave, int lane, int D)
-        : base(base), ld(ld), wave(wave), row_off((uint32_t)((lane / CH) * (int)ld) * 2), chunk_off((uint32_t)chunk(0, wave, lane) * 16)
+        : base(reinterpret_cast<const uint16_t *>(attn_uniform(reinterpret_cast<uint64_t>(base)))), ld(ld), wave(wave)
     {
-        if (PAD)
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) chunks[PAD ? i : 0] = __ballot(chunk(i, wave, lane) * 8 < D);
+        for (int i = 0; i < LOADS; ++i) {
+            const int row = (i * NW + wave) * RPL + lane / CH, chunk = (lane % CH) ^ attn_swizzle<DP>(row);
+            off[i] = PAD && chunk * 8 >= D ? 0xfffffff0u : (uint32_t)row * (uint32_t)ld * 2 + chunk * 16;
+        }
     }
     // Rows row0 .. ; rows from n on are not read
     __device__ __forceinline__ void begin(int row0, int n, uint32_t tile)
     {
-        from = base + (int64_t)(row0 + wave * RPL) * ld;
-        left = n - row0 - wave * RPL;
-        to = tile + wave * 1024;
+        const uint64_t at = reinterpret_cast<uint64_t>(base) + (uint64_t)((int64_t)row0 * ld * 2);
+        const uint32_t bytes = (uint32_t)max(0, min(n - row0, ROWS)) * (uint32_t)ld * 2;
+        buffer = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu),
+                       (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x20000u};         // no stride, 32-bit elements
+        to = __builtin_amdgcn_readfirstlane(tile + wave * 1024);
     }
-    // Load i of them, in order.  Its chunk differs from that of the first in two bits that i gives, none with four waves.
+    // Load i of them, in order
     __device__ __forceinline__ void next(int i)
     {
-        constexpr int STEP = DP == 128 ? NW : 2 * NW;
-        attn_load16(from, row_off + (chunk_off ^ (i * STEP % 4 * 16)), __builtin_amdgcn_readfirstlane(to),
-                    attn_first_lanes(max(0, min(left, RPL)) * CH) & (PAD ? chunks[PAD ? i : 0] : ~0ull));
-        from += (int64_t)(NW * RPL) * ld;
-        left -= NW * RPL;
-        to += NW * 1024;
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" : : "v"(off[i]), "s"(buffer), "s"(to + i * NW * 1024) : "memory", "m0");
     }
     __device__ __forceinline__ void operator()(int row0, int n, const unsigned char *tile)
     {
@@ -425,6 +423,12 @@ __device__ __forceinline__ AttnSpan attn_span(const int32_t *at, int s, int tota
 {
     const int a = min(max(at[s], 0), total), b = min(max(at[s + 1], a), total);
     return {a, b - a};
+}
+// Of one sequence for the whole wave
+__device__ __forceinline__ AttnSpan attn_span_of_wave(const int32_t *at, int s, int total)
+{
+    const AttnSpan x = attn_span(at, s, total);
+    return {__builtin_amdgcn_readfirstlane(x.begin), __builtin_amdgcn_readfirstlane(x.count)};
 }
 // Tiles of `rows` rows are numbered from begin / rows + s in sequence s, so that the number of a tile gives its sequence without anyone having
 // counted the tiles: the next sequence's first number is never below this one's last plus one.  Numbers that no sequence uses do nothing.
