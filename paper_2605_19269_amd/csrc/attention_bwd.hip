@@ -201,6 +201,11 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
             for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, 0, lane);
         attn_reads_done();
         attn_barrier();
+        bf16x8 first[VLDS ? 1 : 4];                        // of dO's columns, to arrive behind the exponentials
+        if constexpr (!VLDS) {
+            attn_read<4>(first, [&](int i) { return attn_cols<DP>(cols + TILE, i / (DP / 32), i % (DP / 32)); });
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 l2 = *reinterpret_cast<const f32x4 *>(stats + 8 * g + 4 * h);
@@ -220,15 +225,20 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
                 dp[r] = sees ? dp[r] : 0.0f;
             }
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= sc[r];
         bf16x8 w[2], x[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            w[u] = attn_operand(sc, u);
-            x[u] = attn_operand(dp, u);
-        }
-        attn_values<DP, 1, 4>(cols + TILE, w, dv);
+        for (int u = 0; u < 2; ++u) w[u] = attn_operand(sc, u);
+        constexpr int B32 = DP / 32, N = 2 * B32;          // products of dV; dS is formed among them
+        const auto add_dv = [&](int i, bf16x8 a) {
+            dv[i % B32] = attn_mfma(a, w[i / B32], dv[i % B32]);
+#pragma unroll
+            for (int r = i * 16 / N; r < (i + 1) * 16 / N; ++r) dp[r] *= sc[r];
+        };
+        const auto read_do = [&](int i) { return attn_cols<DP>(cols + TILE, i / B32, i % B32); };
+        if constexpr (VLDS) attn_products<N, 4>(read_do, add_dv);
+        else attn_products<N, 4>(first, read_do, add_dv, [] {});
+#pragma unroll
+        for (int u = 0; u < 2; ++u) x[u] = attn_operand(dp, u);
         attn_values<DP, 1, 4>(cols, x, dk);
     }
     if (!behind) attn_barrier();

@@ -67,7 +67,12 @@ __device__ __forceinline__ void attn_load4(const void *base, uint32_t off, uint3
 // The first n of 64 lanes, n from 0 on
 __device__ __forceinline__ uint64_t attn_first_lanes(int n) { return n >= 64 ? ~0ull : (1ull << n) - 1; }
 // All loads of this wave have arrived, all its LDS reads are done
-__device__ __forceinline__ void attn_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void attn_wait()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);                    // lgkmcnt(0) that the compiler sees: else it waits for a step's first operand as if scalar loads from ahead of the loop were on their way
+    asm volatile("" ::: "memory");
+}
 // All but the last N of them
 template <int N>
 __device__ __forceinline__ void attn_wait_but()
@@ -109,7 +114,8 @@ struct AttnLoad {
     __device__ __forceinline__ void begin(int row0, int n, uint32_t tile)
     {
         const uint64_t at = reinterpret_cast<uint64_t>(base) + (uint64_t)((int64_t)row0 * ld * 2);
-        const uint32_t bytes = (uint32_t)max(0, min(n - row0, ROWS)) * (uint32_t)ld * 2;
+        const int left = __builtin_amdgcn_readfirstlane(min(n - row0, ROWS));              // keeps the clamp and the product scalar
+        const uint32_t bytes = (uint32_t)max(0, left) * (uint32_t)ld * 2;
         buffer = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffffu),
                        (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x20000u};         // no stride, 32-bit elements
         to = __builtin_amdgcn_readfirstlane(tile + wave * 1024);
@@ -407,11 +413,15 @@ template <int DP, int NB, class Vis, class Between>
 __device__ __forceinline__ void attn_step(uint32_t k_rows, uint32_t v_cols, const bf16x8 (&q)[DP / 16], AttnRows<DP> &rows, float c, int lane, bool masked, Vis vis,
                                           Between between)
 {
+    constexpr int D = DP / 32;
     f32x16 s[NB];
-    bf16x8 p[2 * NB];
+    bf16x8 p[2 * NB], first[4];
     attn_scores<DP, NB, 4>(k_rows, q, s, between);
+    const auto read = [&](int i) { return attn_cols<DP>(v_cols, i / D, i % D); };
+    attn_read<4>(first, read);                             // arrive behind the exponentials
+    __builtin_amdgcn_sched_barrier(0);
     attn_weights<DP, NB>(s, p, rows, c, lane, masked, vis);
-    attn_values<DP, NB, 4>(v_cols, p, rows.o);
+    attn_products<2 * NB * D, 4>(first, read, [&](int i, bf16x8 a) { rows.o[i % D] = attn_mfma(a, p[i / D], rows.o[i % D]); }, [] {});
 }
 
 // ---------------------------------------------------------------- packed sequences
