@@ -262,7 +262,7 @@ def test_turning_back_undoes_the_rotation():
 
 def test_registers_and_local_memory_of_the_kernels():
     """Two waves a SIMD at least (one where LDS has no room for more), two workgroups of four waves a CU, no spilled registers but the few of one kernel (outside
-    its loop)"""
+    its loop, and where it masks a tile)"""
     import os
     import re
     from paper_2605_19269_amd import build as B
@@ -277,7 +277,7 @@ def test_registers_and_local_memory_of_the_kernels():
         kind = m.group(1) or m.group(2)
         seen[kind] = seen.get(kind, 0) + 1
         few, alone = kind == "dkv_kernel" and re.search("ILi128ELb[01]ELi2E", name), kind == "dkv_kernel" and re.search("ILi128ELb[01]ELi1E", name)
-        assert int(vgpr) + int(agpr) <= (512 if alone else 256) and int(spill) <= (3 if few else 0) and int(scratch) <= (16 if few else 0), line
+        assert int(vgpr) + int(agpr) <= (512 if alone else 256) and int(spill) <= (4 if few else 0) and int(scratch) <= (20 if few else 0), line
         wide = "ILi128E" in name and "ELi4ELi32E" in name                                 # four streams of 128 columns: one workgroup a CU
         assert int(lds) <= (80 if kind in ("kernel", "dq_kernel") and not wide else 160) * 1024, line
     assert seen == {"kernel": 12, "dq_kernel": 10, "dkv_kernel": 8, "cached_kernel": 8, "join_kernel": 8, "cache_store": 1}
