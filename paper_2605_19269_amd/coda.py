@@ -144,7 +144,7 @@ _blib.coda_calib_mfma_loop16.argtypes = [_vp, _vp, _vp, _i64, _i64, _vp]
 from . import _binding  # noqa: E402  (links libcoda.so)
 
 _NATIVE = ("coda_gemm", "coda_row_finalize", "coda_row_sumsq", "coda_col_finalize", "coda_lse_finalize", "coda_quantize", "coda_dequantize",
-           "coda_gemm_scaled", "coda_grad_scaled", "coda_attention", "coda_attention_bwd", "coda_cache_store", "coda_attention_cached")
+           "coda_gemm_scaled", "coda_grad_scaled", "coda_attention_bwd")
 _binding.ctypes_calls(*(getattr(_lib, _n) for _n in _NATIVE))
 for _n in _NATIVE:
     setattr(_lib, _n, getattr(_binding, _n))
@@ -168,10 +168,11 @@ _torch = None
 
 
 def _import_torch():
-    global _torch, _DTYPES
+    global _torch, _DTYPES, _TYPES
     import torch
     # raw OCP E4M3 bytes come as either 8-bit type
     _DTYPES = {torch.bfloat16: CODA_BF16, torch.uint8: CODA_F8E4M3, torch.float8_e4m3fn: CODA_F8E4M3}
+    _TYPES = (_DTYPES, torch.bfloat16, torch.float32, torch.int32)
     _torch = torch
     return torch
 
@@ -438,10 +439,8 @@ def _sequences(seq_q, seq_k):
 
 def coda_attention(Q, K, V, seq_q, out, heads, kv_heads, scale, lse=None, seq_k=None, causal=True, stream=None):
     """out: bf16 [Tq x heads * dim]; lse: f32 [heads x Tq] or None; seq_k: None where K and V are packed as Q is."""
-    torch = _torch or _import_torch()
-    q, k, v = (_binding.mat(x, False, _DTYPES) for x in (Q, K, V))
-    _check(_lib.coda_attention(_stream(stream), q, k, v, *_sequences(seq_q, seq_k), heads, kv_heads, float(scale), 1 if causal else 0,
-                               *_binding.rows(out, Q, torch.bfloat16, "out"), _binding.vec(lse, torch.float32, heads, Q.shape[0], "lse")))
+    _torch or _import_torch()
+    _check(_binding.attention(_TYPES, _stream(stream), Q, K, V, seq_q, seq_k, out, lse, heads, kv_heads, scale, causal))
 
 
 def coda_attention_bwd(Q, K, V, out, dout, lse, seq_q, dQ, dK, dV, heads, kv_heads, scale, workspace, seq_k=None, causal=True, rope=None, stream=None):
@@ -468,9 +467,8 @@ def coda_attention_bwd_workspace_bytes(Tq, Tk, n_seqs, heads, kv_heads, head_dim
 def coda_cache_store(K, V, slots, cache_k, cache_v, stream=None):
     """Rows of K, V: bf16 [T x kv_heads * dim] to slots: int32 [T] (page * places + place, or -1 to leave a row out) of the caches
     [pages x kv_heads x places x dim]."""
-    torch = _torch or _import_torch()
-    _check(_lib.coda_cache_store(_stream(stream), _binding.mat(K, False, _DTYPES), _binding.mat(V, False, _DTYPES),
-                                 _binding.vec(slots, torch.int32, K.shape[0], None, "slots"), _binding.cache(cache_k, cache_v, torch.bfloat16)))
+    _torch or _import_torch()
+    _check(_binding.cache_store(_TYPES, _stream(stream), K, V, slots, cache_k, cache_v))
 
 
 def coda_attention_cached(Q, cache_k, cache_v, table, lens, seq_q, out, heads, scale, workspace, tree=None, lse=None, stream=None):
@@ -478,16 +476,9 @@ def coda_attention_cached(Q, cache_k, cache_v, table, lens, seq_q, out, heads, s
     those of the rows; tree: int64 or uint64 [Tq] bits of the sequence's rows that each row sees, None for a chain; workspace:
     coda_attention_cached_workspace_bytes(...) bytes."""
     torch = _torch or _import_torch()
-    at_q, _, n = _sequences(seq_q, None)
-    entries, pitch = table.shape[1], table.stride(0)
-    assert table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == n and (entries <= 1 or table.stride(1) == 1) and (n <= 1 or pitch >= entries), \
-        "table: a row-major int32 tensor [sequences x pages] expected"
-    assert tree is None or tree.dtype in (torch.int64, torch.uint64), "tree: a 64-bit integer for each row expected"
-    T = Q.shape[0]
-    _check(_lib.coda_attention_cached(_stream(stream), _binding.mat(Q, False, _DTYPES), _binding.cache(cache_k, cache_v, torch.bfloat16), table.data_ptr(),
-                                      max(pitch, entries), entries, _binding.vec(lens, torch.int32, n, None, "lens"), at_q, n, heads, float(scale),
-                                      None if tree is None else _binding.vec(tree, tree.dtype, T, None, "tree"), *_binding.rows(out, Q, torch.bfloat16, "out"),
-                                      _binding.vec(lse, torch.float32, heads, T, "lse"), *_at(workspace)))
+    kind = None if tree is None else tree.dtype
+    assert kind in (None, torch.int64, torch.uint64), "tree: a 64-bit integer for each row expected"
+    _check(_binding.attention_cached(_TYPES, _stream(stream), Q, cache_k, cache_v, table, lens, seq_q, out, lse, heads, scale, tree, kind, workspace))
 
 
 def coda_attention_cached_workspace_bytes(Tq, n_seqs, heads, kv_heads, head_dim):

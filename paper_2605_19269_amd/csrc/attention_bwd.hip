@@ -6,8 +6,8 @@
 // Two kernels, no atomics: dQ, a workgroup for 128 rows, over the keys, which also leaves the row statistics; dK and dV, a workgroup for 64 keys of a key / value
 // head, over all rows of all heads of the group.  S and dO V^T are formed in both (eight products, with dS in two parts, where five would do): the
 // alternative, dQ added up in fp32 across workgroups, is either of no fixed order or a partial of every row for every tile of keys.  Bound by the issue of vector instructions and products
-// on one port, dK and dV at 128 columns also by LDS: 4 x 2048 rows, 32 heads over 8 of 64 columns, 159 + 213 us (740 TFLOP/s over the eight products), 8192 rows in six
-// sequences of 128 columns 368 + 460 (860).
+// on one port, dK and dV at 128 columns also by LDS: 4 x 2048 rows, 32 heads over 8 of 64 columns, 154 + 193 us (790 TFLOP/s over the eight products), 8192 rows in six
+// sequences of 128 columns 352 + 422 (930).
 #include "attn_launch.hpp"
 #include "attn_tile.hpp"
 
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
             }
             // dS in two parts: the key channels that a row's weights go by weigh its errors most, and rounded once they came to as much as one and a half roundings of dQ
             // (0.0025 of its norm, against 0.0017 for the rounding of the output alone).  The second product and its operand take a sixth of this kernel's
-            // time: 130 -> 159 us for 4 sequences of 2048, 32 heads over 8 of 64 columns, 308 -> 368 for 8192 rows of 128.
+            // time (with the loads as they were then 130 and 159 us for 4 sequences of 2048, 32 heads over 8 of 64 columns, 308 and 368 for 8192 rows of 128).
             bf16x8 upper[2], lower[2];
             attn_two_parts(dp, upper, lower);
             const uint32_t cols = attn_lds(at) + in.cols + b * 32 * DP * 2;

@@ -1,7 +1,7 @@
 // binding.cpp -- the marshalling of coda.py in C: tensors to coda_mat / coda_epi_op, and the calls of the entry points that a
 // program makes for every layer.  A call on a small problem is host work (its kernels take a few microseconds), and most of
 // that was the interpreter and ctypes: a coda_gemm with four ops 10 us before the launch, here 4.2; a 256 x 512 x 256 linear layer of
-// four calls 22.2 -> 18.9 us a pass; storing 64 tokens in a cache 7 -> 5.6, one cached token 10.1 (13.3 a pass with its kernels).  Tensors are asked through their Python methods, so whatever answers to them is accepted as
+// four calls 22.2 -> 18.9 us a pass.  Tensors are asked through their Python methods, so whatever answers to them is accepted as
 // before; arguments of other types than the usual ones go to the ctypes function of the same name.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -253,57 +253,199 @@ bool dense(int dims, const int64_t *size, const int64_t *stride)
         if (size[i] > 1 && stride[i] != step) return false;
     return true;
 }
+// The address of a dense tensor of `dims` dimensions of the given sizes; null for None
+bool vec_ptr(PyObject *t, PyObject *dtype, int dims, int64_t n, int64_t m, const char *what, void **p)
+{
+    *p = nullptr;
+    if (t == Py_None) return true;
+    int64_t size[2], stride[2];
+    if (tensor(t, dtype, dims, size, stride) && size[0] == n && (dims == 1 || size[1] == m) && dense(dims, size, stride)) return data_ptr(t, p);
+    if (!PyErr_Occurred()) {
+        if (dims == 1) PyErr_Format(PyExc_AssertionError, "%s: a dense tensor of %lld of %S expected", what, (long long)n, dtype);
+        else PyErr_Format(PyExc_AssertionError, "%s: a dense tensor of %lld x %lld of %S expected", what, (long long)n, (long long)m, dtype);
+    }
+    return false;
+}
+// The address and the pitch of a row-major matrix
+bool rows_ptr(PyObject *t, PyObject *dtype, int64_t n, int64_t m, const char *what, void **p, int64_t *ld)
+{
+    int64_t size[2], stride[2];
+    if (tensor(t, dtype, 2, size, stride) && size[0] == n && size[1] == m && (m <= 1 || stride[1] == 1)) {
+        *ld = stride[0];
+        return data_ptr(t, p);
+    }
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "%s: a row-major tensor of %lld x %lld of %S expected", what, (long long)n, (long long)m, dtype);
+    return false;
+}
+bool fill_cache(PyObject *kt, PyObject *vt, PyObject *dtype, coda_cache *c)
+{
+    int64_t k[4], v[4], stride[4];
+    memset(c, 0, sizeof *c);
+    if (tensor(kt, dtype, 4, k, stride) && dense(4, k, stride) && tensor(vt, dtype, 4, v, stride) && dense(4, v, stride) && !memcmp(k, v, sizeof k)) {
+        if (k[1] > INT32_MAX || k[2] > INT32_MAX || k[3] > INT32_MAX) {
+            PyErr_SetString(PyExc_AssertionError, "a cache of that size has no layout");
+            return false;
+        }
+        c->pages = k[0];
+        c->kv_heads = (int32_t)k[1];
+        c->page = (int32_t)k[2];
+        c->head_dim = (int32_t)k[3];
+        return data_ptr(kt, &c->k) && data_ptr(vt, &c->v);
+    }
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "dense caches [pages x kv_heads x page x dim] of %S expected", dtype);
+    return false;
+}
 // vec(t, dtype, n, m, what) -> the address of a dense tensor [n], or [n x m] with m not None; None for None
 PyObject *vec(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (n != 5) return PyErr_Format(PyExc_TypeError, "vec takes 5 arguments");
     if (a[0] == Py_None) Py_RETURN_NONE;
     const int dims = a[3] == Py_None ? 1 : 2;
-    int64_t size[2], stride[2], want[2] = {PyLong_AsLongLong(a[2]), dims == 2 ? PyLong_AsLongLong(a[3]) : 0};
-    if (PyErr_Occurred()) return nullptr;
+    const int64_t rows = PyLong_AsLongLong(a[2]), cols = dims == 2 ? PyLong_AsLongLong(a[3]) : 0;
+    const char *what = PyErr_Occurred() ? nullptr : PyUnicode_AsUTF8(a[4]);
     void *p;
-    if (tensor(a[0], a[1], dims, size, stride) && size[0] == want[0] && (dims == 1 || size[1] == want[1]) && dense(dims, size, stride))
-        return data_ptr(a[0], &p) ? PyLong_FromVoidPtr(p) : nullptr;
-    if (!PyErr_Occurred()) {
-        if (dims == 1) PyErr_Format(PyExc_AssertionError, "%U: a dense tensor of %lld of %S expected", a[4], (long long)want[0], a[1]);
-        else PyErr_Format(PyExc_AssertionError, "%U: a dense tensor of %lld x %lld of %S expected", a[4], (long long)want[0], (long long)want[1], a[1]);
-    }
-    return nullptr;
+    return what && vec_ptr(a[0], a[1], dims, rows, cols, what, &p) ? PyLong_FromVoidPtr(p) : nullptr;
 }
 // rows(t, like, dtype, what) -> (address, pitch) of a row-major matrix of the shape of `like`
 PyObject *rows(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     if (n != 4) return PyErr_Format(PyExc_TypeError, "rows takes 4 arguments");
-    int64_t size[2], stride[2], want[2];
+    int64_t want[2], ld;
     PyObject *shape = PyObject_GetAttr(a[1], s_shape);
     if (!shape) return nullptr;
     const bool ok = PySequence_Size(shape) == 2 && item(shape, 0, want) && item(shape, 1, want + 1);
     Py_DECREF(shape);
     if (!ok) return PyErr_Occurred() ? nullptr : PyErr_Format(PyExc_AssertionError, "row-major 2-D tensor expected");
+    const char *what = PyUnicode_AsUTF8(a[3]);
     void *p;
-    if (tensor(a[0], a[2], 2, size, stride) && size[0] == want[0] && size[1] == want[1] && (size[1] <= 1 || stride[1] == 1))
-        return data_ptr(a[0], &p) ? Py_BuildValue("NL", PyLong_FromVoidPtr(p), (long long)stride[0]) : nullptr;
-    if (!PyErr_Occurred())
-        PyErr_Format(PyExc_AssertionError, "%U: a row-major tensor of %lld x %lld of %S expected", a[3], (long long)want[0], (long long)want[1], a[2]);
-    return nullptr;
+    return what && rows_ptr(a[0], a[2], want[0], want[1], what, &p, &ld) ? Py_BuildValue("NL", PyLong_FromVoidPtr(p), (long long)ld) : nullptr;
 }
-// cache(k, v, dtype) -> the bytes of a coda_cache
-PyObject *cache(PyObject *, PyObject *const *a, Py_ssize_t n)
+
+// ---- attention, without and with a cache, and storing: calls that small problems make for every layer and token, marshalled here from one end to the other (host
+// time by ctypes structures and by this: a prompt of 509 rows 7.2 and 5.8 us, a token with 4097 keys in the cache 10.1 and 9.3, storing 64 tokens 7 and 5.5; a launch is 3.2 of it)
+bool stream_ptr(PyObject *o, void **s)
 {
-    if (n != 3) return PyErr_Format(PyExc_TypeError, "cache takes 3 arguments");
-    int64_t k[4], v[4], stride[4];
-    coda_cache c;
-    memset(&c, 0, sizeof c);
-    if (tensor(a[0], a[2], 4, k, stride) && dense(4, k, stride) && tensor(a[1], a[2], 4, v, stride) && dense(4, v, stride) && !memcmp(k, v, sizeof k)) {
-        if (k[1] > INT32_MAX || k[2] > INT32_MAX || k[3] > INT32_MAX) return PyErr_Format(PyExc_AssertionError, "a cache of that size has no layout");
-        c.pages = k[0];
-        c.kv_heads = (int32_t)k[1];
-        c.page = (int32_t)k[2];
-        c.head_dim = (int32_t)k[3];
-        return data_ptr(a[0], &c.k) && data_ptr(a[1], &c.v) ? PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&c), sizeof c) : nullptr;
+    *s = nullptr;
+    if (o == Py_None) return true;
+    PyObject *v = PyLong_Check(o) ? Py_NewRef(o) : PyObject_GetAttrString(o, "value");     // a ctypes pointer
+    if (!v) return false;
+    if (v != Py_None) *s = PyLong_AsVoidPtr(v);
+    Py_DECREF(v);
+    return !PyErr_Occurred();
+}
+bool int_of(PyObject *o, int32_t *v)
+{
+    const long long x = PyLong_AsLongLong(o);
+    if (x == -1 && PyErr_Occurred()) return false;
+    *v = x < INT32_MIN || x > INT32_MAX ? 0 : (int32_t)x;                                  // 0 heads: refused
+    return true;
+}
+bool real_of(PyObject *o, float *v)
+{
+    const double x = PyFloat_AsDouble(o);
+    *v = (float)x;
+    return !(x == -1.0 && PyErr_Occurred());
+}
+// Offsets of sequences [n + 1], and their number
+bool offsets_ptr(PyObject *t, PyObject *i32, int32_t *n, void **p)
+{
+    int64_t size, stride;
+    if (!tensor(t, i32, 1, &size, &stride) || size < 1 || size > INT32_MAX || (size > 1 && stride != 1)) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_AssertionError, "seq_q: sequences + 1 offsets of torch.int32 expected, dense");
+        return false;
     }
-    if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "dense caches [pages x kv_heads x page x dim] of %S expected", a[2]);
-    return nullptr;
+    *n = (int32_t)(size - 1);
+    return data_ptr(t, p);
+}
+bool bytes_of(PyObject *t, void **p, size_t *bytes)
+{
+    *p = nullptr;
+    *bytes = 0;
+    if (t == Py_None) return true;
+    PyObject *n = PyObject_CallMethod(t, "numel", nullptr), *e = n ? PyObject_CallMethodNoArgs(t, s_element_size) : nullptr;
+    const long long count = n ? PyLong_AsLongLong(n) : -1, each = e ? PyLong_AsLongLong(e) : -1;
+    Py_XDECREF(n);
+    Py_XDECREF(e);
+    if (PyErr_Occurred()) return false;
+    *bytes = count > 0 && each > 0 ? (size_t)count * (size_t)each : 0;
+    return data_ptr(t, p);
+}
+#define CODA_STATUS(...)           \
+    coda_status st;                \
+    Py_BEGIN_ALLOW_THREADS         \
+    st = __VA_ARGS__;              \
+    Py_END_ALLOW_THREADS           \
+    return PyLong_FromLong(st);
+// types: (the dict of operand types, bfloat16, float32, int32)
+struct Types {
+    PyObject *operands, *bf16, *f32, *i32;
+    bool read(PyObject *t)
+    {
+        if (PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 4) {
+            operands = PyTuple_GET_ITEM(t, 0);
+            bf16 = PyTuple_GET_ITEM(t, 1);
+            f32 = PyTuple_GET_ITEM(t, 2);
+            i32 = PyTuple_GET_ITEM(t, 3);
+            return true;
+        }
+        PyErr_SetString(PyExc_TypeError, "types expected");
+        return false;
+    }
+};
+// attention(types, stream, Q, K, V, seq_q, seq_k, out, lse, heads, kv_heads, scale, causal) -> status
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 13) return PyErr_Format(PyExc_TypeError, "attention takes 13 arguments");
+    Types ty;
+    coda_mat Q, K, V;
+    void *s, *sq, *sk, *out, *lse;
+    int32_t seqs, heads, kv;
+    int64_t ldo;
+    float scale;
+    const int causal = PyObject_IsTrue(a[12]);
+    if (causal < 0 || !ty.read(a[0]) || !stream_ptr(a[1], &s) || !fill_mat(a[2], false, ty.operands, &Q) || !fill_mat(a[3], false, ty.operands, &K) ||
+        !fill_mat(a[4], false, ty.operands, &V) || !offsets_ptr(a[5], ty.i32, &seqs, &sq) || !vec_ptr(a[6], ty.i32, 1, (int64_t)seqs + 1, 0, "seq_k", &sk) ||
+        !rows_ptr(a[7], ty.bf16, Q.rows, Q.cols, "out", &out, &ldo) || !int_of(a[9], &heads) || !vec_ptr(a[8], ty.f32, 2, heads, Q.rows, "lse", &lse) ||
+        !int_of(a[10], &kv) || !real_of(a[11], &scale))
+        return nullptr;
+    CODA_STATUS(coda_attention(s, &Q, &K, &V, static_cast<const int32_t *>(sq), static_cast<const int32_t *>(sk), seqs, heads, kv, scale, causal, out, ldo, static_cast<float *>(lse)))
+}
+// cache_store(types, stream, K, V, slots, cache_k, cache_v) -> status
+PyObject *cache_store(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 7) return PyErr_Format(PyExc_TypeError, "cache_store takes 7 arguments");
+    Types ty;
+    coda_mat K, V;
+    coda_cache c;
+    void *s, *slots;
+    if (!ty.read(a[0]) || !stream_ptr(a[1], &s) || !fill_mat(a[2], false, ty.operands, &K) || !fill_mat(a[3], false, ty.operands, &V) ||
+        !vec_ptr(a[4], ty.i32, 1, K.rows, 0, "slots", &slots) || !fill_cache(a[5], a[6], ty.bf16, &c))
+        return nullptr;
+    CODA_STATUS(coda_cache_store(s, &K, &V, static_cast<const int32_t *>(slots), &c))
+}
+// attention_cached(types, stream, Q, cache_k, cache_v, table, lens, seq_q, out, lse, heads, scale, tree, type of the tree, workspace) -> status
+PyObject *attention_cached(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 15) return PyErr_Format(PyExc_TypeError, "attention_cached takes 15 arguments");
+    Types ty;
+    coda_mat Q;
+    coda_cache c;
+    void *s, *sq, *lens, *out, *lse, *tree, *ws, *table;
+    int32_t seqs, heads;
+    int64_t ldo, size[2], stride[2];
+    size_t bytes;
+    float scale;
+    if (!ty.read(a[0]) || !stream_ptr(a[1], &s) || !fill_mat(a[2], false, ty.operands, &Q) || !fill_cache(a[3], a[4], ty.bf16, &c) || !offsets_ptr(a[7], ty.i32, &seqs, &sq))
+        return nullptr;
+    if (!tensor(a[5], ty.i32, 2, size, stride) || size[0] != seqs || (size[1] > 1 && stride[1] != 1) || (seqs > 1 && stride[0] < size[1])) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_AssertionError, "table: a row-major int32 tensor [sequences x pages] expected");
+        return nullptr;
+    }
+    if (!data_ptr(a[5], &table) || !vec_ptr(a[6], ty.i32, 1, seqs, 0, "lens", &lens) || !rows_ptr(a[8], ty.bf16, Q.rows, Q.cols, "out", &out, &ldo) || !int_of(a[10], &heads) ||
+        !vec_ptr(a[9], ty.f32, 2, heads, Q.rows, "lse", &lse) || !real_of(a[11], &scale) || !vec_ptr(a[12], a[13], 1, Q.rows, 0, "tree", &tree) || !bytes_of(a[14], &ws, &bytes))
+        return nullptr;
+    CODA_STATUS(coda_attention_cached(s, &Q, &c, static_cast<const int32_t *>(table), stride[0] > size[1] ? stride[0] : size[1], size[1], static_cast<const int32_t *>(lens),
+                                      static_cast<const int32_t *>(sq), seqs, heads, scale, static_cast<const uint64_t *>(tree), out, ldo, static_cast<float *>(lse), ws, bytes))
 }
 
 // ---- the calls.  Arguments are pointers (an address, None, the bytes of a structure) and numbers; anything else takes the ctypes function.
@@ -345,9 +487,8 @@ struct Args {
     }
 };
 
-enum Call { GEMM, ROW_FINALIZE, ROW_SUMSQ, COL_FINALIZE, LSE_FINALIZE, QUANTIZE, DEQUANTIZE, GEMM_SCALED, GRAD_SCALED, ATTENTION, ATTENTION_BWD, CACHE_STORE,
-            ATTENTION_CACHED, CALLS };
-constexpr int ARITY[CALLS] = {10, 8, 3, 5, 8, 9, 6, 14, 14, 14, 23, 5, 17};
+enum Call { GEMM, ROW_FINALIZE, ROW_SUMSQ, COL_FINALIZE, LSE_FINALIZE, QUANTIZE, DEQUANTIZE, GEMM_SCALED, GRAD_SCALED, ATTENTION_BWD, CALLS };
+constexpr int ARITY[CALLS] = {10, 8, 3, 5, 8, 9, 6, 14, 14, 23};
 PyObject *g_ctypes[CALLS];           // set once, when coda.py is imported
 
 template <int CALL>
@@ -410,15 +551,6 @@ PyObject *call(PyObject *, PyObject *const *a, Py_ssize_t n)
                 float *G = x.ptr<float>(10);
                 CODA_RUN(coda_grad_scaled(stream, M, N, K, A, sa, lda, B, sb, ldb, G, n8, ws, (size_t)bytes))
             }
-        } else if constexpr (CALL == ATTENTION) {
-            const coda_mat *Q = x.ptr<const coda_mat>(1), *K = x.ptr<const coda_mat>(2), *V = x.ptr<const coda_mat>(3);
-            const int32_t *sq = x.ptr<const int32_t>(4), *sk = x.ptr<const int32_t>(5);
-            const int32_t n_seqs = x.small(6), heads = x.small(7), kv = x.small(8), causal = x.small(10);
-            const float scale = x.real(9);
-            void *out = x.ptr<void>(11);
-            const int64_t ldo = x.num(12);
-            float *lse = x.ptr<float>(13);
-            CODA_RUN(coda_attention(stream, Q, K, V, sq, sk, n_seqs, heads, kv, scale, causal, out, ldo, lse))
         } else if constexpr (CALL == ATTENTION_BWD) {
             const coda_mat *m[5];
             for (int i = 0; i < 5; ++i) m[i] = x.ptr<const coda_mat>(1 + i);
@@ -431,23 +563,6 @@ PyObject *call(PyObject *, PyObject *const *a, Py_ssize_t n)
             const int64_t lq = x.num(16), lk = x.num(18), lv = x.num(20), bytes = x.num(22);
             if (bytes < 0) x.usual = false;
             CODA_RUN(coda_attention_bwd(stream, m[0], m[1], m[2], m[3], m[4], lse, sq, sk, n_seqs, heads, kv, scale, causal, rope, dq, lq, dk, lk, dv, lv, ws, (size_t)bytes))
-        } else if constexpr (CALL == CACHE_STORE) {
-            const coda_mat *K = x.ptr<const coda_mat>(1), *V = x.ptr<const coda_mat>(2);
-            const int32_t *slots = x.ptr<const int32_t>(3);
-            const coda_cache *c = x.ptr<const coda_cache>(4);
-            CODA_RUN(coda_cache_store(stream, K, V, slots, c))
-        } else if constexpr (CALL == ATTENTION_CACHED) {
-            const coda_mat *Q = x.ptr<const coda_mat>(1);
-            const coda_cache *c = x.ptr<const coda_cache>(2);
-            const int32_t *table = x.ptr<const int32_t>(3), *lens = x.ptr<const int32_t>(6), *sq = x.ptr<const int32_t>(7);
-            const int64_t ldt = x.num(4), cols = x.num(5), ldo = x.num(13), bytes = x.num(16);
-            const int32_t n_seqs = x.small(8), heads = x.small(9);
-            const float scale = x.real(10);
-            const uint64_t *tree = x.ptr<const uint64_t>(11);
-            void *out = x.ptr<void>(12), *ws = x.ptr<void>(15);
-            float *lse = x.ptr<float>(14);
-            if (bytes < 0) x.usual = false;
-            CODA_RUN(coda_attention_cached(stream, Q, c, table, ldt, cols, lens, sq, n_seqs, heads, scale, tree, out, ldo, lse, ws, (size_t)bytes))
         } else {
             const float *pmax = x.ptr<const float>(1), *psum = x.ptr<const float>(2), *ztgt = x.ptr<const float>(5);
             const int64_t M = x.num(3), nblk = x.num(4);
@@ -490,11 +605,10 @@ PyMethodDef methods[] = {CODA_FAST("op", op),
                          CODA_FAST("coda_grad_scaled", call<GRAD_SCALED>),
                          CODA_FAST("vec", vec),
                          CODA_FAST("rows", rows),
-                         CODA_FAST("cache", cache),
-                         CODA_FAST("coda_attention", call<ATTENTION>),
+                         CODA_FAST("attention", attention),
+                         CODA_FAST("attention_cached", attention_cached),
+                         CODA_FAST("cache_store", cache_store),
                          CODA_FAST("coda_attention_bwd", call<ATTENTION_BWD>),
-                         CODA_FAST("coda_cache_store", call<CACHE_STORE>),
-                         CODA_FAST("coda_attention_cached", call<ATTENTION_CACHED>),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -197,10 +197,13 @@ def test_addresses_of_vectors_matrices_and_caches(coda):
         with pytest.raises((AssertionError, AttributeError)):
             b.rows(bad, m, torch.float32, "out")
     k, w = (torch.zeros(3, 2, 16, 8, dtype=torch.bfloat16) for _ in range(2))
-    assert b.cache(k, w, torch.bfloat16) == bytes(coda.coda_cache(k.data_ptr(), w.data_ptr(), 3, 16, 2, 8))
+    rows, slots = torch.zeros(0, 16, dtype=torch.bfloat16), torch.zeros(0, dtype=torch.int32)
+    coda.coda_cache_store(rows, rows, slots, k, w, stream=0)
+    with pytest.raises(coda.CodaError):                                                     # heads and columns of the cache, not of K
+        coda.coda_cache_store(rows[:, :8], rows[:, :8], slots, k, w, stream=0)
     for bad in ((k, w.float()), (k[:2], w), (k[:, :1], w[:, :1]), (k.transpose(0, 1), w.transpose(0, 1)), (k[0], w[0])):
         with pytest.raises(AssertionError, match="dense caches"):
-            b.cache(*bad, torch.bfloat16)
+            coda.coda_cache_store(rows, rows, slots, *bad, stream=0)
 
 
 def test_calls_take_every_form_of_argument(coda):
@@ -219,8 +222,11 @@ def test_calls_take_every_form_of_argument(coda):
     with pytest.raises(coda.CodaError):
         coda.coda_attention_bwd(*good[:3], bf(8, 128), bf(8, 128), torch.zeros(0, 8), ints(2), bf(8, 128), bf(8, 64), bf(8, 64), 0, 1, 0.1, bf(8),
                                 rope=(torch.zeros(4, 64), torch.zeros(4, 64), ints(8)), stream=0)
-    for bad in (dict(heads=2.0), dict(heads="2"), dict(scale="x")):
-        with pytest.raises((ctypes.ArgumentError, TypeError, ValueError)):
+    for bad in (dict(heads=2 ** 40), dict(heads=-2 ** 70), dict(kv_heads=2 ** 32 + 1), dict(scale=1e300)):
+        with pytest.raises((coda.CodaError, OverflowError)):
+            coda.coda_attention(*good, **{**dict(heads=2, kv_heads=1, scale=0.1, stream=0), **bad})
+    for bad in (dict(heads=2.0), dict(heads="2"), dict(scale="x"), dict(stream="s")):
+        with pytest.raises((ctypes.ArgumentError, TypeError, ValueError, AttributeError)):
             coda.coda_attention(*good, **{**dict(heads=2, kv_heads=1, scale=0.1, stream=0), **bad})
 
 
