@@ -54,6 +54,10 @@ __device__ __forceinline__ int64_t cached_uniform(int64_t x)
 {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
+__device__ __forceinline__ int64_t cached_of_lane(int64_t x, int lane)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
+}
 // Sum over the workgroup's threads of each one's value, and of those before it
 template <int WAVES>
 __device__ __forceinline__ int64_t cached_scan(int64_t v, int64_t *part, int64_t &before)
@@ -97,9 +101,12 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
 
     // This workgroup's range, and the sequence that it begins in
     const auto cost_of = [](const CachedSeq &q) { return (int64_t)q.tiles * (q.steps + C::RESTART); };
-    int64_t mine = 0, before;
     const int each = (p.n_seqs + THREADS - 1) / THREADS, s0 = min((int)threadIdx.x * each, p.n_seqs), s1 = min(s0 + each, p.n_seqs);
-    for (int s = s0; s < s1; ++s) {
+    // Up to 64 sequences a wave looks at by itself (all leave the same in LDS): without barriers, which with the exchange through LDS take 0.5 us of a lone token's 10
+    const bool alone = p.n_seqs <= 64;
+    const int t0 = alone ? min(lane, p.n_seqs) : s0, t1 = alone ? min(lane + 1, p.n_seqs) : s1;
+    int64_t mine = 0, before, total;
+    for (int s = t0; s < t1; ++s) {
         const CachedSeq q = cached_seq(p, s, C::ROWS, C::KEYS);
         mine += cost_of(q);
         if (s < CACHED_SEQS) {
@@ -108,7 +115,16 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
             seqs[s][2] = q.len;
         }
     }
-    const int64_t total = cached_uniform(cached_scan<C::WAVES>(mine, part, before));
+    if (alone) {
+        int64_t run = mine;
+        for (int off = 1; off < p.n_seqs; off <<= 1) {
+            const int64_t o = __shfl_up(run, off, 64);
+            if (lane >= off) run += o;
+        }
+        before = run - mine;
+        total = cached_of_lane(run, p.n_seqs - 1);
+    } else
+        total = cached_uniform(cached_scan<C::WAVES>(mine, part, before));
     const int64_t ranges = min((int64_t)p.ranges, total);
     if (blockIdx.x == 0) {                                 // numbers that no tile of rows has
         const int64_t items = cached_items(p.Tq, p.n_seqs, p.group, MANY);
@@ -128,19 +144,27 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
         return cached_seq_of(p, __builtin_amdgcn_readfirstlane(seqs[s][0]), __builtin_amdgcn_readfirstlane(seqs[s][1]), __builtin_amdgcn_readfirstlane(seqs[s][2]),
                              C::ROWS, C::KEYS);
     };
-    if (before <= at && at < before + mine) {
-        int s = s0;
-        for (;; ++s) {
-            const int64_t cost = cost_of(cached_seq(p, s, C::ROWS, C::KEYS));
-            if (at < before + cost) break;
-            before += cost;
+    int s;
+    int64_t base;
+    const bool here = before <= at && at < before + mine;
+    if (alone) {
+        s = __builtin_ctzll(__ballot(here));
+        base = cached_of_lane(before, s);
+    } else {
+        if (here) {
+            s = s0;
+            for (;; ++s) {
+                const int64_t cost = cost_of(cached_seq(p, s, C::ROWS, C::KEYS));
+                if (at < before + cost) break;
+                before += cost;
+            }
+            found[0] = s;
+            found[1] = before;
         }
-        found[0] = s;
-        found[1] = before;
+        __syncthreads();
+        s = __builtin_amdgcn_readfirstlane((int)found[0]);
+        base = cached_uniform(found[1]);
     }
-    __syncthreads();
-    int s = __builtin_amdgcn_readfirstlane((int)found[0]);
-    int64_t base = cached_uniform(found[1]);
 
     while (at < end) {
         const CachedSeq seq = sequence(s);
