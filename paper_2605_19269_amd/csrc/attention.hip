@@ -72,17 +72,21 @@ __global__ __launch_bounds__(256, DP == 128 && SPLIT == 4 ? 1 : 2) void attentio
         for (int i = 0; i < PARTS; ++i) load(j, i);
     };
     if (n > 0) load_all(0);
+    if (NW == 1) {                                         // `dirty` is cleared before anyone sets it
+        attn_reads_done();
+        attn_barrier();
+    }
     attn_arrived(qf);
     for (int j = 0; j < n; ++j) {
         attn_wait();
-        attn_barrier();                                    // the tiles of round j are there, and nobody reads those of j - 1 any more
+        if (NW > 1) attn_barrier();                        // the tiles of round j are there, and nobody reads those of j - 1 any more; a lone wave's are its own
         const int k0 = j * ROUND + stream * KEYS;
         unsigned char *at = stage(j);
         if ((j + 1) * ROUND > whole) {
             constexpr int PART = TILE / NW;
             if (attn_clean(at + TILE + block * PART, PART, min(k.count - k0, KEYS) * (DP * 2) - block * PART, lane)) dirty = 1;
             attn_reads_done();
-            attn_barrier();
+            if (NW > 1) attn_barrier();
         }
         if (k0 < high) {
             const int lim = mine - k0;
@@ -144,6 +148,7 @@ __global__ __launch_bounds__(256, DP == 128 && SPLIT == 4 ? 1 : 2) void attentio
         }
     }
     if (n * ROUND > whole) {
+        attn_wait();                                       // the last round's loads for the next
         __syncthreads();
         if (dirty)
             for (int j = whole / ROUND * SPLIT; j < n * SPLIT; ++j) {

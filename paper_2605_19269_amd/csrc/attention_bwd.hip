@@ -140,12 +140,17 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
     attn_arrived(kf);
     if constexpr (!VLDS) attn_arrived(vf);
     // Half of the streams are half a round behind the others, and there is one of each on every SIMD: the products of S and dP of one run beside the
-    // exponentials of the other.  A barrier each half keeps them so.
+    // exponentials of the other.  A barrier each half keeps them so.  With KB = 1 nobody shares a tile, and waves that go their own way take a tenth to a fifth less (1024 rows,
+    // 32 heads over 8 of 64 columns 26 -> 24 us, of 128 columns 58 -> 48).
     const bool behind = stream >= NS / 2;
-    if (behind) attn_barrier();
-    for (int i = 0; i < rounds; ++i) {
+    if (KB == 1 && VLDS) {                                 // V's tile is everybody's
         attn_wait();
         attn_barrier();
+    }
+    if (KB > 1 && behind) attn_barrier();
+    for (int i = 0; i < rounds; ++i) {
+        attn_wait();
+        if (KB > 1) attn_barrier();
         unsigned char *at = smem + ((i & 1) * NS + stream) * STAGE;
         const Place now = here;
         step(here);
@@ -200,7 +205,7 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
         if (mine)                                          // for the products with the rows' columns; S and dP are masked by selection
             for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, 0, lane);
         attn_reads_done();
-        attn_barrier();
+        if (KB > 1) attn_barrier();
         bf16x8 first[VLDS ? 1 : 4];                        // of dO's columns, to arrive behind the exponentials
         if constexpr (!VLDS) {
             attn_read<4>(first, [&](int i) { return attn_cols<DP>(cols + TILE, i / (DP / 32), i % (DP / 32)); });
@@ -241,7 +246,8 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
         for (int u = 0; u < 2; ++u) x[u] = attn_operand(dp, u);
         attn_values<DP, 1, 4>(cols, x, dk);
     }
-    if (!behind) attn_barrier();
+    attn_wait();                                           // the last round's loads for the next, of rows that there are none of: where the parts come they may still leave zeros
+    if (KB > 1 && !behind) attn_barrier();
     // The streams' parts are added up in their order: all of dK, then all of dV through LDS, and a stream finishes every NS-th 32 columns
     const int64_t row = (int64_t)k.begin + key;
     const bool there = key < k.count;
@@ -354,13 +360,13 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
     asm volatile("" : "+v"(l2), "+v"(delta));
     for (int j = 0; j < n; ++j) {
         attn_wait();
-        attn_barrier();
+        if (NW > 1) attn_barrier();                        // else a wave's tiles are its own
         const int k0 = j * ROUND + stream * KEYS;
         unsigned char *at = stage(j);
         if ((j + 1) * ROUND > whole) {
             attn_clean(at + block * (TILE / NW), TILE / NW, 0, lane);
             attn_reads_done();
-            attn_barrier();
+            if (NW > 1) attn_barrier();
         }
         if (k0 >= high) {
             load_all(j + 1);
@@ -412,6 +418,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
         constexpr int UNITS = DP / 32 * 4;                 // of four registers, 1 KB each
         static_assert(BWD_WAVES * UNITS * 1024 <= 4 * SPLIT * TILE, "the parts take the place of the tiles");
         f32x4 *parts = reinterpret_cast<f32x4 *>(smem) + lane;
+        attn_wait();                                       // the last round's loads for the next, which go where the parts come
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
@@ -444,10 +451,10 @@ static int dq_split(const BwdParams &p)
     const int64_t room = p.f.D > 64 ? 288 : 576;
     return p.f.D <= 64 && attn_about(p.f.Tq, p.f.n_seqs, 32) * p.f.heads <= room ? 4 : attn_about(p.f.Tq, p.f.n_seqs, 64) * p.f.heads <= 2 * room ? 2 : 1;
 }
-// Keys of a workgroup of dK's kernel: 32, with more streams where LDS has room for them, while there are at most one and a half workgroups a CU.  us with 64 / 32, 32
-// heads over 8: D = 64, a sequence of 509: 26 / 18, 1024: 42 / 28, 1500: 59 / 42, 2048: 77 / 61, 4096: 188 / 225, 4 x 512: 27 / 33; D = 128, 256: 25 / 22,
-// 1024: 67 / 62, 2048: 131 / 133, 4 x 512: 44 / 62.
-static int dkv_keys(const BwdParams &p) { return attn_about(p.f.Tk, p.f.n_seqs, 32) * p.f.kv_heads <= 400 ? 32 : 64; }
+// Keys of a workgroup of dK's kernel: 32, whose waves each have tiles of their own and no barrier, while there are at most two workgroups a CU, or 64, whose pairs of waves share their
+// tiles.  us with 64 / 32, 32 heads over 8: D = 64, a sequence of 509: 26 / 15, 1024: 42 / 24, 2048: 70 / 54, 4096: 176 / 192, 4 x 512: 25 / 29; D = 128, 256: 25 / 17,
+// 1024: 67 / 48, 2048: 114 / 104, 4096: 293 / 403, 4 x 512: 39 / 49.
+static int dkv_keys(const BwdParams &p) { return attn_about(p.f.Tk, p.f.n_seqs, 32) * p.f.kv_heads <= 512 ? 32 : 64; }
 static int64_t dkv_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tk / dkv_keys(p) + p.f.n_seqs) * p.f.kv_heads; }
 static int64_t dq_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tq * dq_split(p) / 128 + p.f.n_seqs) * p.f.heads; }
 
