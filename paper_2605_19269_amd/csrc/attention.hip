@@ -186,9 +186,9 @@ __global__ __launch_bounds__(256, DP == 128 && SPLIT == 4 ? 1 : 2) void attentio
 // How many waves share 32 rows.  A wave's time is that of its steps one after the other (0.9 us for 64 keys where nothing else runs on its SIMD), so while the
 // card has room for all workgroups at once (by their registers and LDS: SPLIT 4 one a CU, SPLIT 2 two, D <= 64 twice as many), splitting rows' keys cuts the longest
 // one's steps; past that, shared tiles count.  Tiles are estimated, half a tile a sequence on average, and an eighth more than fits at once is still
-// worth it.  Measured, us with SPLIT 1 / 2 / 4, 32 heads over 8: D = 64, a sequence of 128: 6.2 / 5.2 / 5.2, 509: 11.9 / 9.3 / 8.4, 1024: 19.9 / 15.6 / 18.8,
-// 2048: 35.2 / 30.9 / 47, 4096: 90 / 96 / 148; 4 x 512: 17.0 / 17.2 / 28.  D = 128: 128: 8.3 / 7.1 / 7.0, 509: 16.4 / 12.8 / 17, 1024: 27.2 / 22.3 / 42, 2048: 52.5 / 56.5 / 120.
-// 8 heads over 2: D = 64, 1024: 18.9 / 13.9 / 10.4, 4096: 63 / 45 / 44.  33 keys, one tile: 4.5 / 4.5 / 5.1.
+// worth it.  Measured, us with SPLIT 1 / 2 / 4, 32 heads over 8: D = 64, a sequence of 128: 6.0 / 5.1 / 5.0, 509: 11.5 / 8.7 / 7.5, 1024: 18.9 / 13.7 / 16.1,
+// 2048: 33.3 / 28.9 / 39, 4096: 88 / 91 / 122; 4 x 512: 16.0 / 15.9 / 24.6.  D = 128: 128: 8.0 / 6.8 / 6.6, 509: 15.1 / 11.5 / 15.1, 1024: 24.3 / 19.9 / 34.5, 2048: 48.9 / 51.6 / 90.
+// 8 heads over 2: D = 64, 1024: 18.2 / 12.8 / 8.6, 4096: 61 / 39 / 36; D = 128, 1024: 23.2 / 17.0 / 12.1.  33 keys, one tile: 4.3 / 4.3 / 4.9.
 static int fwd_split(const AttnParams &p)
 {
     if (p.Tk <= 64) return 1;

@@ -444,7 +444,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
 }
 
 // How many waves share 32 rows, as in the forward kernel, and for the same reason.  us with SPLIT 1 / 2 / 4, 32 heads over 8: D = 64, a sequence of 256: 10 / 8 / 7,
-// 509: 14 / 11 / 10, 1024: 23 / 18 / 23, 2048: 44 / 42 / 57, 4096: 115 / 128 / 182; D = 128, 256: 14 / 12 / 11, 1024: 35 / 28 / 57, 2048: 71 / 72 / 159 (SPLIT 4 gains too
+// 509: 15 / 11 / 10, 1024: 25 / 19 / 22, 2048: 51 / 46 / 56, 4096: 141 / 141 / 181; D = 128, 256: 15 / 11, 1024: 38 / 30, 2048: 81 / 79, 4 x 512: 33 / 37 (SPLIT 4 gains too
 // little to be there).
 static int dq_split(const BwdParams &p)
 {
@@ -452,8 +452,8 @@ static int dq_split(const BwdParams &p)
     return p.f.D <= 64 && attn_about(p.f.Tq, p.f.n_seqs, 32) * p.f.heads <= room ? 4 : attn_about(p.f.Tq, p.f.n_seqs, 64) * p.f.heads <= 2 * room ? 2 : 1;
 }
 // Keys of a workgroup of dK's kernel: 32, whose waves each have tiles of their own and no barrier, while there are at most two workgroups a CU, or 64, whose pairs of waves share their
-// tiles.  us with 64 / 32, 32 heads over 8: D = 64, a sequence of 509: 26 / 15, 1024: 42 / 24, 2048: 70 / 54, 4096: 176 / 192, 4 x 512: 25 / 29; D = 128, 256: 25 / 17,
-// 1024: 67 / 48, 2048: 114 / 104, 4096: 293 / 403, 4 x 512: 39 / 49.
+// tiles.  us with 64 / 32, 32 heads over 8: D = 64, a sequence of 509: 23 / 15, 1024: 37 / 24, 2048: 69 / 53, 4096: 179 / 192, 4 x 512: 24 / 28; D = 128, 256: 22 / 18,
+// 1024: 58 / 49, 2048: 111 / 109, 4096: 297 / 415, 4 x 512: 38 / 50.
 static int dkv_keys(const BwdParams &p) { return attn_about(p.f.Tk, p.f.n_seqs, 32) * p.f.kv_heads <= 512 ? 32 : 64; }
 static int64_t dkv_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tk / dkv_keys(p) + p.f.n_seqs) * p.f.kv_heads; }
 static int64_t dq_workgroups(const BwdParams &p) { return ((int64_t)p.f.Tq * dq_split(p) / 128 + p.f.n_seqs) * p.f.heads; }
