@@ -1,12 +1,13 @@
 // attention_cached.hip -- attention of new tokens over a paged cache, and storing into it.
 //
 // The rows of one key / value head are the tokens of a sequence times the query heads of the group, so that every key is read once for all of
-// them.  Bound by HBM for few rows: 4 D bytes a key and key / value head, and 4 D operations a key and row.
+// them.  Bound by HBM for few rows: 4 D bytes a key and key / value head, and 4 D operations a key and row.  32 heads over 8 of 128 columns: 64 sequences of 200000 keys in all 140 us (5.8 TB/s); a
+// lone one of 4097 keys 9.3, of which 6 are launch, code and three trips to memory.
 //
 //  * Rows are cut into tiles of 32 or 128.  With 32 (a few tokens) the workgroup's four waves take a quarter of the keys of a tile each, from LDS of their
 //    own without a barrier: four slots of K or V a wave, three of them on their way (24 KB a wave, 96 KB a CU) while one is read.  With 128 (trees) four
-//    waves have 32 rows each and share the keys, and the workgroup's two such groups take the halves of a tile of 128 keys.  At the end the waves of a row
-//    are joined in LDS.
+//    waves have 32 rows each and share the keys, and the workgroup's two such groups take the halves of a tile of 128 keys, a barrier a step (with two, V's loads behind K's products,
+//    36.4 us where 33.7 are for eight sequences of 31000 keys in all and 32 drafts each).  At the end the waves of a row are joined in LDS.
 //  * The tiles of keys of all tiles of rows, laid end to end, are cut into equal ranges, a workgroup each: lengths may differ as they like and
 //    the host needs to know none of them; a tile of rows counts for two or three steps more than it has, which is what a range loses between two (64 sequences' last workgroups
 //    ended 12 us behind the first without).  A range that covers a tile of rows whole writes its outputs; otherwise fp32 partials go to slot
@@ -225,11 +226,13 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
             rows_at[wave][lane] = pg * p.page_bytes + ((uint32_t)clamped(first_key(j) + lane) & p.page_mask) * (uint32_t)(p.D * 2);
             __builtin_amdgcn_wave_barrier();               // a wave's LDS operations stay in order
         };
+        const auto load_part = [&](const unsigned char *cache, unsigned char *to, int i) {
+            if (!PAD || lane_chunk(i) * 8 < p.D)
+                attn_load16(cache + lane_chunk(i) * 16 + rows_at[wave][tile_row(i)], __builtin_amdgcn_readfirstlane(attn_lds(to) + (i * C::GROUP + member) * 1024));
+        };
         const auto load = [&](const unsigned char *cache, unsigned char *to) {
 #pragma unroll
-            for (int i = 0; i < C::LOADS; ++i)
-                if (!PAD || lane_chunk(i) * 8 < p.D)
-                    attn_load16(cache + lane_chunk(i) * 16 + rows_at[wave][tile_row(i)], __builtin_amdgcn_readfirstlane(attn_lds(to) + (i * C::GROUP + member) * 1024));
+            for (int i = 0; i < C::LOADS; ++i) load_part(cache, to, i);
         };
         // V's tiles that are cleaned: masked ones, and where groups wait for each other also what lies beside one
         const auto cleaned = [&](int j) { return (MANY ? j * C::KEYS + C::KEYS : first_key(j) + C::WAVE_KEYS) > whole; };
@@ -252,49 +255,46 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
             asm volatile("" : : "v"(bits0), "v"(bits1));
             find_rows(j0);
             fetch(K, j0, 0);
-            fetch_ids(j0 + 2);
+            if (!MANY) fetch_ids(j0 + 2);
             fetch(V, j0, 1);
-            if (j0 + 1 < j1) {
+            if (MANY) fetch_ids(j0 + 2);
+            if (!MANY && j0 + 1 < j1) {
                 find_rows(j0 + 1);
                 fetch(K, j0 + 1, 0);
                 fetch_ids(j0 + 3);
-                if (!MANY) fetch(V, j0 + 1, 1);
+                fetch(V, j0 + 1, 1);
             }
             for (int j = j0; j < j1; ++j) {
                 const int k0 = first_key(j);
                 const bool here = k0 < seq.len && row0 < nrows;                    // the last step's keys may leave nothing for this wave
                 const bool masked = k0 + C::WAVE_KEYS > whole;
-                f32x16 sc[NB];
-                bf16x8 w[2 * NB];
                 const auto see = [&](int k) { return sees(k0 + k); };
                 if constexpr (MANY) {
-                    // Two barriers a step: K of j is there and V of j - 1 read, V of j + 1 may come; V of j is there and K of j read, K of j + 2 may come
-                    if (j + 1 < j1) attn_wait_but<2 * L + 2>();                    // pages, V, K, pages are to come
-                    else attn_wait_but<L + 1>();
+                    attn_wait_but<1>();                    // K and V of j and the pages of j + 1 are there; pages are to come
                     attn_reads_done();
-                    attn_barrier();
-                    if (j + 1 < j1) fetch(V, j + 1, 1);
-                    if (here) {
-                        attn_scores<DP, NB, 4>(attn_lds(slot(j, 0)) + in.rows, qf, sc, [](int) {});
-                        attn_weights<DP, NB>(sc, w, acc, c, lane, masked, see);
-                    }
-                    if (j + 1 < j1) attn_wait_but<2 * L + 1>();                    // K, pages, V are to come
-                    else attn_wait_but<0>();
-                    attn_reads_done();
-                    attn_barrier();
-                    if (j + 2 < j1) {
-                        find_rows(j + 2);
-                        fetch(K, j + 2, 0);
-                        fetch_ids(j + 4);
-                    }
+                    attn_barrier();                        // for all waves, and K and V of j - 1 are read
                     if (cleaned(j)) {
                         constexpr int PART = C::TILE / C::GROUP;
                         if (attn_clean(slot(j, 1) + member * PART, PART, PART, lane)) dirty = 1;
                         attn_reads_done();
                         attn_barrier();
                     }
-                    if (here) attn_values<DP, NB, 4>(attn_lds(slot(j, 1)) + in.cols, w, acc.o);
+                    const bool more = j + 1 < j1;
+                    if (more) find_rows(j + 1);
+                    const auto issue = [&](int i) {
+                        if (more) load_part(i < L ? K : V, slot(j + 1, i >= L), i % L);
+                    };
+                    if (here)
+                        attn_step<DP, NB>(attn_lds(slot(j, 0)) + in.rows, attn_lds(slot(j, 1)) + in.cols, qf, acc, c, lane, masked, see, [&](int i) {
+                            if (i % 2 == 0) issue(i / 2);
+                        });
+                    else
+#pragma unroll
+                        for (int i = 0; i < 2 * L; ++i) issue(i);
+                    if (more) fetch_ids(j + 3);
                 } else {
+                    f32x16 sc[NB];
+                    bf16x8 w[2 * NB];
                     if (j + 1 < j1) attn_wait_but<3 * L + 1>();                    // K and the pages of step j + 2 are there; V, K, pages, V are to come
                     else attn_wait_but<L>();
                     attn_scores<DP, NB, 4>(attn_lds(slot(j, 0)) + in.rows, qf, sc, [](int) {});
