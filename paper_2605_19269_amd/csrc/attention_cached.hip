@@ -6,8 +6,9 @@
 //
 //  * Rows are cut into tiles of 32 or 128.  With 32 (a few tokens) the workgroup's four waves take a quarter of the keys of a tile each, from LDS of their
 //    own without a barrier: four slots of K or V a wave, three of them on their way (24 KB a wave, 96 KB a CU) while one is read.  With 128 (trees) four
-//    waves have 32 rows each and share the keys, and the workgroup's two such groups take the halves of a tile of 128 keys, a barrier a step (with two, V's loads behind K's products,
-//    36.4 us where 33.7 are for eight sequences of 31000 keys in all and 32 drafts each).  At the end the waves of a row are joined in LDS.
+//    waves have 32 rows each and share the keys, and the workgroup's two such groups take the halves of a tile of 128 keys, a barrier a step.  Two a step, with V's
+//    loads behind K's products and more of them on their way, take 36.4 us where 33.1 are for eight sequences of 31000 keys in all and 32 drafts each (47.5 and 48.0 with the join where nothing of
+//    them is cached), and 29.0 where 27.6 are for one of 16411 keys and 61 drafts.  At the end the waves of a row are joined in LDS.
 //  * The tiles of keys of all tiles of rows, laid end to end, are cut into equal ranges, a workgroup each: lengths may differ as they like and
 //    the host needs to know none of them; a tile of rows counts for two or three steps more than it has, which is what a range loses between two (64 sequences' last workgroups
 //    ended 12 us behind the first without).  A range that covers a tile of rows whole writes its outputs; otherwise fp32 partials go to slot
@@ -226,13 +227,11 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
             rows_at[wave][lane] = pg * p.page_bytes + ((uint32_t)clamped(first_key(j) + lane) & p.page_mask) * (uint32_t)(p.D * 2);
             __builtin_amdgcn_wave_barrier();               // a wave's LDS operations stay in order
         };
-        const auto load_part = [&](const unsigned char *cache, unsigned char *to, int i) {
-            if (!PAD || lane_chunk(i) * 8 < p.D)
-                attn_load16(cache + lane_chunk(i) * 16 + rows_at[wave][tile_row(i)], __builtin_amdgcn_readfirstlane(attn_lds(to) + (i * C::GROUP + member) * 1024));
-        };
         const auto load = [&](const unsigned char *cache, unsigned char *to) {
 #pragma unroll
-            for (int i = 0; i < C::LOADS; ++i) load_part(cache, to, i);
+            for (int i = 0; i < C::LOADS; ++i)
+                if (!PAD || lane_chunk(i) * 8 < p.D)
+                    attn_load16(cache + lane_chunk(i) * 16 + rows_at[wave][tile_row(i)], __builtin_amdgcn_readfirstlane(attn_lds(to) + (i * C::GROUP + member) * 1024));
         };
         // V's tiles that are cleaned: masked ones, and where groups wait for each other also what lies beside one
         const auto cleaned = [&](int j) { return (MANY ? j * C::KEYS + C::KEYS : first_key(j) + C::WAVE_KEYS) > whole; };
@@ -280,17 +279,13 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                         attn_barrier();
                     }
                     const bool more = j + 1 < j1;
-                    if (more) find_rows(j + 1);
-                    const auto issue = [&](int i) {
-                        if (more) load_part(i < L ? K : V, slot(j + 1, i >= L), i % L);
-                    };
+                    if (more) {
+                        find_rows(j + 1);
+                        fetch(K, j + 1, 0);
+                        fetch(V, j + 1, 1);
+                    }
                     if (here)
-                        attn_step<DP, NB>(attn_lds(slot(j, 0)) + in.rows, attn_lds(slot(j, 1)) + in.cols, qf, acc, c, lane, masked, see, [&](int i) {
-                            if (i % 2 == 0) issue(i / 2);
-                        });
-                    else
-#pragma unroll
-                        for (int i = 0; i < 2 * L; ++i) issue(i);
+                        attn_step<DP, NB>(attn_lds(slot(j, 0)) + in.rows, attn_lds(slot(j, 1)) + in.cols, qf, acc, c, lane, masked, see, [](int) {});
                     if (more) fetch_ids(j + 3);
                 } else {
                     f32x16 sc[NB];

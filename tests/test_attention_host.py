@@ -268,7 +268,7 @@ def test_turning_back_undoes_the_rotation():
 
 def test_registers_and_local_memory_of_the_kernels():
     """Two waves a SIMD at least (one where LDS has no room for more), two workgroups of four waves a CU, no spilled registers but the few of one kernel (outside
-    its loop, and where it masks a tile) and one of another (ahead of its loop)"""
+    its loop, and where it masks a tile)"""
     import os
     import re
     from paper_2605_19269_amd import build as B
@@ -282,9 +282,8 @@ def test_registers_and_local_memory_of_the_kernels():
             continue
         kind = m.group(1) or m.group(2)
         seen[kind] = seen.get(kind, 0) + 1
-        one = int("attention_cached_kernelILi128ELb0ELb1E" in name)
         few, alone = kind == "dkv_kernel" and re.search("ILi128ELb[01]ELi2E", name), re.search("dkv_kernelILi128ELb[01]ELi1E|cached_kernelILi[0-9]+ELb[01]ELb0E", name)
-        assert int(vgpr) + int(agpr) <= (512 if alone else 256) and int(spill) <= (4 if few else one) and int(scratch) <= (20 if few else 8 * one), line
+        assert int(vgpr) + int(agpr) <= (512 if alone else 256) and int(spill) <= (4 if few else 0) and int(scratch) <= (20 if few else 0), line
         wide = "ILi128E" in name and "ELi4ELi32E" in name                                 # four streams of 128 columns: one workgroup a CU
         assert int(lds) <= (80 if kind in ("kernel", "dq_kernel") and not wide else 160) * 1024, line
     assert seen == {"kernel": 12, "dq_kernel": 10, "dkv_kernel": 8, "cached_kernel": 8, "join_kernel": 8, "cache_store": 1}
