@@ -143,11 +143,10 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
     // exponentials of the other.  A barrier each half keeps them so.  With KB = 1 nobody shares a tile, and waves that go their own way take a tenth to a fifth less (1024 rows,
     // 32 heads over 8 of 64 columns 26 -> 24 us, of 128 columns 58 -> 48).
     const bool behind = stream >= NS / 2;
-    if (KB == 1 && VLDS) {                                 // V's tile is everybody's
-        attn_wait();
+    if (KB == 1 ? VLDS : behind) {                         // the first barrier of every wave comes behind its part of V's tile, which all read from then on: here, or in the first round
+        if (VLDS) attn_wait();
         attn_barrier();
     }
-    if (KB > 1 && behind) attn_barrier();
     for (int i = 0; i < rounds; ++i) {
         attn_wait();
         if (KB > 1) attn_barrier();
