@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256, DP == 128 && SPLIT == 4 ? 1 : 2) void attentio
                 attn_wait();
                 attn_barrier();
                 const int lim = mine - j * KEYS;
-                attn_add_marks<DP, KEYS / 16>(attn_lds(smem) + in.cols, acc.o, lane, [&](int key) { return key < lim; });
+                attn_add_marks<DP, KEYS / 16>(attn_lds(smem) + in.cols, acc.o, lane, [&](int key) { return key < lim; }, attn_marked);
                 __syncthreads();
             }
     }

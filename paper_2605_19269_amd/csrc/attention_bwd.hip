@@ -286,6 +286,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
 {
     constexpr int NW = BWD_WAVES / SPLIT, ROWS = NW * 32, TILE = KEYS * DP * 2, ROUND = SPLIT * KEYS;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[4 * SPLIT * TILE];
+    __shared__ int dirty;                                  // a masked tile of K held something that is not finite
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int block = wave % NW, stream = wave / NW;
     const int64_t tiles = (int64_t)gridDim.x / p.f.heads;
@@ -335,6 +336,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
     f32x16 dq[DP / 32];
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) dq[b] = f32x16{};
+    if (threadIdx.x == 0) dirty = 0;
     if (PAD) attn_zero(smem, sizeof(smem), 256);
     const int n = (keys + ROUND - 1) / ROUND;
     AttnLoad<DP, PAD, KEYS, NW> load_k(K, p.f.ldk, block, lane, p.f.D), load_v(V, p.f.ldv, block, lane, p.f.D);
@@ -354,21 +356,41 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
         for (int i = 0; i < PARTS; ++i) load(j, i);
     };
     if (n > 0) load_all(0);
+    if (NW == 1) {                                         // `dirty` is cleared before anyone sets it
+        attn_reads_done();
+        attn_barrier();
+    }
     attn_arrived(qf);
     attn_arrived(of);
     asm volatile("" : "+v"(l2), "+v"(delta));
+    // A weight of zero times an infinity of K is NaN, so K is cleaned where rows do not see all of it, but for the product with dS alone: S takes K as it is (a weight of zero may come
+    // of an infinity).  Nearly always there is nothing to clean, so the tile is only looked at ahead of S, and cleaned behind S, with barriers, where something was found.
+    bool slow = false;
     for (int j = 0; j < n; ++j) {
         attn_wait();
         if (NW > 1) attn_barrier();                        // else a wave's tiles are its own
         const int k0 = j * ROUND + stream * KEYS;
         unsigned char *at = stage(j);
         if ((j + 1) * ROUND > whole) {
-            attn_clean(at + block * (TILE / NW), TILE / NW, 0, lane);
+            constexpr int PART = TILE / NW;
+            if (attn_check(at + block * PART, PART, min(k.count - k0, KEYS) * (DP * 2) - block * PART, lane)) dirty = 1;
             attn_reads_done();
             if (NW > 1) attn_barrier();
+            slow = __builtin_amdgcn_readfirstlane(dirty) != 0;
         }
+        const auto clean = [&](int b) {                    // the keys of block b, by all waves that share them
+            constexpr int PART = 32 * DP * 2 / NW;
+            int own = lane;
+            asm volatile("" : "+v"(own));                  // no addresses of this are kept in registers all the way
+            if (NW > 1) attn_barrier();
+            attn_clean(at + b * 32 * DP * 2 + block * PART, PART, 0, own);
+            attn_reads_done();
+            if (NW > 1) attn_barrier();
+        };
         if (k0 >= high) {
             load_all(j + 1);
+            if (slow)
+                for (int b = 0; b < KEYS / 32; ++b) clean(b);
             continue;
         }
         const int lim = mine - k0;
@@ -390,6 +412,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
                                           dp = attn_mfma(a, of[i], dp);
                                           if (b == 0 && i % EVERY == 0) load(j + 1, PARTS / 2 + i / EVERY);
                                       });
+            if (slow) clean(b);
 #pragma unroll
             for (int r = 0; r < 16; ++r) dp[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, -l2)) * dp[r];
             if (masked) {
@@ -410,6 +433,24 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
                                       });
         }
     }
+    if (SPLIT > 1) {
+        attn_wait();                                       // the last round's loads for the next, which go where the parts come
+        __syncthreads();
+        slow = __builtin_amdgcn_readfirstlane(dirty) != 0;
+    }
+    if (slow) {                                            // what was cleaned, for the rows that see it: whatever their weight, an infinity or a NaN times dS makes NaN of their sum
+        attn_wait();
+        __syncthreads();
+        for (int j = whole / ROUND * SPLIT; j < n * SPLIT; ++j) {
+            AttnLoad<DP, PAD, KEYS, BWD_WAVES>(K, p.f.ldk, wave, lane, p.f.D)(j * KEYS, k.count, smem);
+            attn_wait();
+            attn_barrier();
+            const int lim = mine - j * KEYS;
+            attn_add_marks<DP, KEYS / 16>(attn_lds(smem) + in.cols, dq, lane, [&](int key) { return key < lim; },
+                                          [](float x, float marks) { return marks == 0.0f ? x : __builtin_nanf(""); });
+            __syncthreads();
+        }
+    }
     const int64_t at = (int64_t)q.begin + row;
     const bool there = row < q.count;
     const int64_t angle = bwd_angle(p, p.pos_q + at, there);
@@ -417,8 +458,6 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
         constexpr int UNITS = DP / 32 * 4;                 // of four registers, 1 KB each
         static_assert(BWD_WAVES * UNITS * 1024 <= 4 * SPLIT * TILE, "the parts take the place of the tiles");
         f32x4 *parts = reinterpret_cast<f32x4 *>(smem) + lane;
-        attn_wait();                                       // the last round's loads for the next, which go where the parts come
-        __syncthreads();
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             const int g = u % 4 * 4;

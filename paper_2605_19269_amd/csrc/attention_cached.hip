@@ -328,7 +328,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
                     load(V, own);
                     attn_wait();
                     if (MANY) attn_barrier();
-                    attn_add_marks<DP, C::WAVE_KEYS / 16>(attn_lds(own) + in.cols, acc.o, lane, [&](int k) { return sees(k0 + k); });
+                    attn_add_marks<DP, C::WAVE_KEYS / 16>(attn_lds(own) + in.cols, acc.o, lane, [&](int k) { return sees(k0 + k); }, attn_marked);
                     attn_reads_done();
                     if (MANY) attn_barrier();
                 }

@@ -259,6 +259,22 @@ __device__ __forceinline__ bool attn_clean(unsigned char *tile, int bytes, int t
     }
     return __ballot(found) != 0;
 }
+// The same without touching what was loaded, for a tile that others still read: rows behind it, which nobody's result depends on, are cleared where they are not finite
+__device__ __forceinline__ bool attn_check(unsigned char *tile, int bytes, int there, int lane)
+{
+    bool found = false;
+    for (int i = lane * 16; i < bytes; i += 1024) {
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + i);
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top |= ((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        if (top) {
+            if (i < there) found = true;
+            else *reinterpret_cast<u32x4 *>(tile + i) = u32x4{0, 0, 0, 0};
+        }
+    }
+    return __ballot(found) != 0;
+}
 __device__ __forceinline__ bf16x8 attn_marks(bf16x8 x)
 {
     s16x8 v = __builtin_bit_cast(s16x8, x);
@@ -277,9 +293,9 @@ __device__ __forceinline__ float attn_marked(float o, float marks)
     if (n >= 1048576 || (plus && minus)) return __builtin_nanf("");
     return o + (plus ? __builtin_inff() : -__builtin_inff());
 }
-// What the elements of an uncleaned tile of NT x 16 rows that are not finite come to in acc; vis(k): the lane's row sees row k of the tile
-template <int DP, int NT, class Vis>
-__device__ __forceinline__ void attn_add_marks(uint32_t tile_cols, f32x16 (&acc)[DP / 32], int lane, Vis vis)
+// What the elements of an uncleaned tile of NT x 16 rows that are not finite come to in acc; vis(k): the lane's row sees row k of the tile; met(x, marks): x with what it met
+template <int DP, int NT, class Vis, class Met>
+__device__ __forceinline__ void attn_add_marks(uint32_t tile_cols, f32x16 (&acc)[DP / 32], int lane, Vis vis, Met met)
 {
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b) {
@@ -292,7 +308,7 @@ __device__ __forceinline__ void attn_add_marks(uint32_t tile_cols, f32x16 (&acc)
             marks = attn_mfma(attn_marks(attn_cols<DP>(tile_cols, t, b)), __builtin_bit_cast(bf16x8, see), marks);
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[b][r] = attn_marked(acc[b][r], marks[r]);
+        for (int r = 0; r < 16; ++r) acc[b][r] = met(acc[b][r], marks[r]);
     }
 }
 

@@ -1,0 +1,43 @@
+"""Infinities in what rows do see: a key with an infinite element whose score is -inf has a weight of zero, and everything else is as if the key were not there; an infinite
+element of an output's gradient reaches its own column of dV.  Wherever the key or the row lies, in a tile that a mask touches or in one that all rows see."""
+import math
+
+import pytest
+import torch
+
+from tests import attn_ref as R
+from tests.test_gpu_attention import behind_empty, coda  # noqa: F401
+from tests.test_gpu_attention_bwd import Pass
+
+pytestmark = pytest.mark.gpu
+
+
+def hidden(key):
+    """R.visible of a first sequence whose rows' weight of `key` is zero; the sequences behind it have no rows"""
+    see = R.visible
+    return lambda rows, keys, causal: see(rows, keys, causal) & (torch.arange(keys) != key)
+
+
+@pytest.mark.parametrize("D", [64, 128, 40, 96])
+@pytest.mark.parametrize("streams", [1, 2, 4])
+@pytest.mark.parametrize("rows,past,causal,key", [(300, None, True, 290), (300, None, True, 130), (300, None, True, 3), (77, 200, True, 210), (77, 200, True, 70),
+                                                  (150, -30, True, 90), (130, None, False, 129), (130, None, False, 9)])
+def test_gradients_with_a_key_of_weight_zero(coda, monkeypatch, rows, past, causal, key, streams, D):
+    """The key's column of dQ is NaN (zero times an infinity) for the rows that see it, no other column and no other row notices, dK and dV of the key are zero"""
+    col = D - 3
+    p = Pass(coda, [rows] + [0] * behind_empty(D, 2, streams), past, 2, 1, D, causal, seed=key + D)
+    for h in range(2):
+        p.Q[:, h * D + col] = p.Q[:, h * D + col].abs() + 0.25
+    p.K[key, col] = -math.inf
+    coda.coda_attention(p.Q, p.K, p.V, p.seq_q, p.out, 2, 1, p.scale, lse=p.lse, seq_k=p.seq_k, causal=causal)
+    got = p.run()
+    sees = R.visible(rows, p.k_at[1], causal)[:, key]
+    assert sees.any() and torch.isfinite(p.out).all()
+    p.K[key, col] = 0.0
+    with monkeypatch.context() as m:
+        m.setattr(R, "visible", hidden(key))
+        want, bound = p.expected()
+    for h in range(2):
+        want[0][sees, h * D + col] = math.nan
+    for x, w, b, name in zip(got, want, bound, ("dQ", "dK", "dV")):
+        R.check(x, w, b, name)
