@@ -61,6 +61,7 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
     constexpr bool VLDS = DP == 128;                       // 32 registers that there are not
     constexpr int ROWS = 32, TILE = ROWS * DP * 2, STAGE = 2 * TILE + 256, KEYS = KB * 32;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * NS * STAGE + (VLDS ? KEYS * DP * 2 : 0)];
+    __shared__ int found[NS][KB];                          // what the waves of a stream found in its masked tile
     unsigned char *const v_tile = smem + 2 * NS * STAGE;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int kb = wave % KB, stream = wave / KB;
@@ -201,13 +202,20 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
                 issue(DP / 16 + u);
             });
         }
-        if (mine)                                          // for the products with the rows' columns; S and dP are masked by selection
-            for (int j = kb; j < 2; j += KB) attn_clean(at + j * TILE, TILE, 0, lane);
+        // S and dP are masked by selection, but for the products with the rows' columns Q and dO have to be finite.  The tiles are only looked at here, where the other wave of a pair may still
+        // read them for S or dP; where something was found, each wave clears all of both behind the barrier, ahead of its own reads: whoever comes second finds what it would have written.
+        int bad = 0;
+        if (mine) {
+            const int bytes = max(0, min(q.count - row0, ROWS)) * (DP * 2);
+            for (int j = kb; j < 2; j += KB) bad |= (int)attn_check(at + j * TILE, TILE, bytes, lane) << j;
+            if (KB > 1) found[stream][kb] = bad;
+        }
         attn_reads_done();
         if (KB > 1) attn_barrier();
         bf16x8 first[VLDS ? 1 : 4];                        // of dO's columns, to arrive behind the exponentials
+        const auto read_do = [&](int i) { return attn_cols<DP>(cols + TILE, i / (DP / 32), i % (DP / 32)); };
         if constexpr (!VLDS) {
-            attn_read<4>(first, [&](int i) { return attn_cols<DP>(cols + TILE, i / (DP / 32), i % (DP / 32)); });
+            attn_read<4>(first, read_do);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
@@ -220,6 +228,14 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
             }
         }
         if (mine) {
+            if (KB > 1) bad = __builtin_amdgcn_readfirstlane(found[stream][0] | found[stream][KB - 1]);
+            if (bad) {
+                int own = lane;
+                asm volatile("" : "+v"(own));              // no addresses of this are kept in registers all the way
+                attn_clean(at, 2 * TILE, 0, own);
+                attn_reads_done();
+                if constexpr (!VLDS) attn_read<4>(first, read_do);
+            }
             const int lim = p.f.causal ? key - ahead - row0 : 0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -238,7 +254,6 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
 #pragma unroll
             for (int r = i * 16 / N; r < (i + 1) * 16 / N; ++r) dp[r] *= sc[r];
         };
-        const auto read_do = [&](int i) { return attn_cols<DP>(cols + TILE, i / B32, i % B32); };
         if constexpr (VLDS) attn_products<N, 4>(read_do, add_dv);
         else attn_products<N, 4>(first, read_do, add_dv, [] {});
 #pragma unroll

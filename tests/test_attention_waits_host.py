@@ -24,3 +24,16 @@ def test_values_in_lds_have_arrived_ahead_of_every_first_barrier():
     for at in before:
         statement = text[:begin + at].rsplit("{", 1)[-1] if "{" in text[begin + at - 80: begin + at] else ""
         assert "attn_wait()" in statement, text[begin + at - 80: begin + at + 20]
+
+
+def test_no_shared_tile_is_changed_while_others_read_it():
+    """The gradients' kernels: rows of a tile are read for S and dP by waves that a barrier has to hold before anyone clears what is not finite in it"""
+    text = kernel("attention_bwd.hip", "attention_dkv_kernel")
+    loop = text[text.index("for (int i = 0; i < rounds"):]
+    products = loop.rindex("attn_rows<DP>(rows, ROWS")                      # the last that reads rows
+    assert products < loop.index("attn_barrier()", products) < loop.index("attn_clean(")
+    text = kernel("attention_bwd.hip", "attention_dq_kernel")
+    assert text.count("attn_clean(") == 1
+    clean = text[text.index("const auto clean"):]
+    clean = clean[: clean.index("};")]
+    assert clean.index("attn_barrier()") < clean.index("attn_clean(") < clean.index("attn_reads_done()") < clean.rindex("attn_barrier()")
