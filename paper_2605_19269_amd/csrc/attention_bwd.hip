@@ -51,6 +51,27 @@ __device__ __forceinline__ int64_t bwd_angle(const BwdParams &p, const int32_t *
     return p.cos && there ? (int64_t)min(max(*pos, 0), p.rope_rows - 1) * (p.f.D / 2) : 0;
 }
 
+// A row of dO (in memory) whose elements that are not finite were cleared for the products: added to the accumulators of dV^T of the lane's key, if it is seen.  Its weight is positive, so that
+// an infinity stays one, and the order of additions does not matter to what comes of it.
+template <int DP, bool PAD>
+__device__ __forceinline__ void bwd_add_infinities(const uint16_t *x, int D, int lane, bool seen, f32x16 (&acc)[DP / 32])
+{
+    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * b + 8 * g + 4 * (lane >> 5);
+            const u32x2 v = !PAD || d < D ? *reinterpret_cast<const u32x2 *>(x + d) : u32x2{};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t w = e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16;
+                if (seen && (w & 0x7f800000u) == 0x7f800000u) acc[b][4 * g + e] += __builtin_bit_cast(float, w);
+            }
+            __builtin_amdgcn_sched_barrier(0);             // one after the other: all at once would not find registers
+        }
+}
+
 // dK and dV.  The waves are KB blocks of 32 keys times NS streams: a stream takes every NS-th of the (32 rows, head of the group) pairs that see the keys, and the
 // streams are added up at the end.  S = Q K^T and dP = dO V^T have the lane's key in their columns, so P and dS are operands of dV^T += dO^T P and
 // dK^T += Q^T dS as they stand.  K, and V where D is at most 64, stay in registers; Q and dO are read from LDS twice, by rows and by columns: at D = 128, 40 KB of LDS
@@ -207,41 +228,50 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
         int bad = 0;
         if (mine) {
             const int bytes = max(0, min(q.count - row0, ROWS)) * (DP * 2);
-            for (int j = kb; j < 2; j += KB) bad |= (int)attn_check(at + j * TILE, TILE, bytes, lane) << j;
+            for (int j = kb; j < 2; j += KB) bad |= (int)attn_check<TILE>(at + j * TILE, bytes, lane) << j;
             if (KB > 1) found[stream][kb] = bad;
         }
         attn_reads_done();
         if (KB > 1) attn_barrier();
         bf16x8 first[VLDS ? 1 : 4];                        // of dO's columns, to arrive behind the exponentials
         const auto read_do = [&](int i) { return attn_cols<DP>(cols + TILE, i / (DP / 32), i % (DP / 32)); };
+        f32x4 l2[4];                                       // of the lane's rows, ahead of the columns: the exponentials wait for them
+        const auto read_l2 = [&](int g) { l2[g] = *reinterpret_cast<const f32x4 *>(stats + 8 * g + 4 * h); };
         if constexpr (!VLDS) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) read_l2(g);
+            __builtin_amdgcn_sched_barrier(0);
             attn_read<4>(first, read_do);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const f32x4 l2 = *reinterpret_cast<const f32x4 *>(stats + 8 * g + 4 * h);
+            if (VLDS) read_l2(g);                          // no registers to do so there
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = 4 * g + e;
-                sc[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, -l2[e]));
+                sc[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[r], c, -l2[g][e]));
             }
         }
         if (mine) {
             if (KB > 1) bad = __builtin_amdgcn_readfirstlane(found[stream][0] | found[stream][KB - 1]);
+            const int lim = p.f.causal ? key - ahead - row0 : 0;
             if (bad) {
                 int own = lane;
                 asm volatile("" : "+v"(own));              // no addresses of this are kept in registers all the way
+                // What is cleared of dO reaches its columns of dV for the keys that the row sees (of Q it needs nothing: lse and dS are not finite then, in all columns)
+                if (bad & 2)
+                    for (int row = 0; row < ROWS && row0 + row < q.count; ++row)
+                        bwd_add_infinities<DP, PAD>(do_base + (int64_t)now.head * p.f.D + (int64_t)(row0 + row) * p.lddo, p.f.D, own, row >= lim, dv);
                 attn_clean(at, 2 * TILE, 0, own);
                 attn_reads_done();
                 if constexpr (!VLDS) attn_read<4>(first, read_do);
             }
-            const int lim = p.f.causal ? key - ahead - row0 : 0;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int row = attn_acc_row(r, h);
                 const bool sees = bool((int)(row >= lim) & (int)(row0 + row < q.count));
-                sc[r] = sees ? sc[r] + (dp[r] - dp[r]) : 0.0f;                       // a row of dO that is not finite was cleaned above, but delta has it: 0, or NaN there
+                sc[r] = sees ? sc[r] : 0.0f;
                 dp[r] = sees ? dp[r] : 0.0f;
             }
         }
@@ -388,7 +418,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
         unsigned char *at = stage(j);
         if ((j + 1) * ROUND > whole) {
             constexpr int PART = TILE / NW;
-            if (attn_check(at + block * PART, PART, min(k.count - k0, KEYS) * (DP * 2) - block * PART, lane)) dirty = 1;
+            if (attn_check<PART>(at + block * PART, min(k.count - k0, KEYS) * (DP * 2) - block * PART, lane)) dirty = 1;
             attn_reads_done();
             if (NW > 1) attn_barrier();
             slow = __builtin_amdgcn_readfirstlane(dirty) != 0;

@@ -238,16 +238,21 @@ __device__ __forceinline__ u32x4 attn_store_unit(const float (&lo)[4], const flo
 // NaN 2^20; sums over a tile are exact in fp32) tells for each output whether it met +inf, -inf, both or a NaN.  Whatever order a sum takes
 // these in, the result is the same, so the end is early enough.
 
+// Not zero if one of eight elements is not finite
+__device__ __forceinline__ uint32_t attn_not_finite(u32x4 v)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top |= ((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    return top;
+}
 // `bytes` of a tile from `tile` on (a multiple of 1024) by one wave; true if something in the first `there` of them (rows behind were not loaded) was not finite
 __device__ __forceinline__ bool attn_clean(unsigned char *tile, int bytes, int there, int lane)
 {
     bool found = false;
     for (int i = lane * 16; i < bytes; i += 1024) {
         u32x4 v = *reinterpret_cast<const u32x4 *>(tile + i);
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top |= ((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-        if (top) {
+        if (attn_not_finite(v)) {
             found |= i < there;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -260,20 +265,20 @@ __device__ __forceinline__ bool attn_clean(unsigned char *tile, int bytes, int t
     return __ballot(found) != 0;
 }
 // The same without touching what was loaded, for a tile that others still read: rows behind it, which nobody's result depends on, are cleared where they are not finite
-__device__ __forceinline__ bool attn_check(unsigned char *tile, int bytes, int there, int lane)
+template <int BYTES>
+__device__ __forceinline__ bool attn_check(unsigned char *tile, int there, int lane)
 {
-    bool found = false;
-    for (int i = lane * 16; i < bytes; i += 1024) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + i);
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top |= ((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-        if (top) {
-            if (i < there) found = true;
-            else *reinterpret_cast<u32x4 *>(tile + i) = u32x4{0, 0, 0, 0};
+    uint32_t top = 0;
+    if (there >= BYTES) {
+#pragma unroll 4
+        for (int i = 0; i < BYTES; i += 1024) top |= attn_not_finite(*reinterpret_cast<const u32x4 *>(tile + i + lane * 16));
+    } else
+        for (int i = lane * 16; i < BYTES; i += 1024) {
+            const uint32_t t = attn_not_finite(*reinterpret_cast<const u32x4 *>(tile + i));
+            if (i < there) top |= t;
+            else if (t) *reinterpret_cast<u32x4 *>(tile + i) = u32x4{0, 0, 0, 0};
         }
-    }
-    return __ballot(found) != 0;
+    return __ballot(top != 0) != 0;
 }
 __device__ __forceinline__ bf16x8 attn_marks(bf16x8 x)
 {

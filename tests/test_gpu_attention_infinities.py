@@ -41,3 +41,27 @@ def test_gradients_with_a_key_of_weight_zero(coda, monkeypatch, rows, past, caus
         want[0][sees, h * D + col] = math.nan
     for x, w, b, name in zip(got, want, bound, ("dQ", "dK", "dV")):
         R.check(x, w, b, name)
+
+
+@pytest.mark.parametrize("D", [64, 128, 40, 96])
+@pytest.mark.parametrize("streams", [1, 4])
+@pytest.mark.parametrize("fill", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("rows,past,causal,row", [(300, None, True, 71), (300, None, True, 299), (77, 200, True, 5), (150, -30, True, 40), (130, None, False, 129), (130, None, False, 9)])
+def test_gradients_with_an_infinite_element_of_the_outputs_gradient(coda, rows, past, causal, row, fill, streams, D):
+    """It reaches its own column of dV for the keys that its row sees, all of their dK, and all of its row of dQ; nothing else notices"""
+    col = D - 5
+    p = Pass(coda, [rows] + [0] * behind_empty(D, 2, streams), past, 2, 1, D, causal, seed=row + D)
+    p.dout[row, D + col] = fill                                                          # of the second head
+    got = p.run()
+    seen = R.visible(rows, p.k_at[1], causal)[row]
+    assert seen.any()
+    p.dout[row, D + col] = 0.0
+    want, bound = p.expected()
+    seen = torch.cat((seen, torch.zeros(p.K.shape[0] - p.k_at[1], dtype=torch.bool)))
+    want[2][seen, col] = fill                                                            # weights are positive
+    for x, w, b, name, left_out in zip(got, want, bound, ("dQ", "dK", "dV"), ((row, slice(D, None)), (seen, slice(None)), None)):
+        x = x.double().cpu()
+        if left_out is not None:
+            assert not torch.isfinite(x[left_out]).any(), name
+            x[left_out] = w[left_out]
+        R.check(x, w, b, name)
