@@ -52,6 +52,16 @@ __device__ __forceinline__ CachedSeq cached_seq(const CachedParams &p, int s, in
 }
 __device__ __forceinline__ int64_t cached_item(const CachedParams &p, const CachedSeq &q, int s, int rows) { return (int64_t)q.q0 * p.group / rows + s; }
 
+// Whether row `token` of a sequence of nq rows from q0 on sees no key at all: asked for rows whose sum of weights is zero, which may also see keys, all with a score of -inf
+__device__ __forceinline__ bool cached_sees_nothing(const CachedParams &p, int q0, int nq, int len, int token)
+{
+    const int drafts = len - nq;
+    if (!p.tree) return drafts + token + 1 <= 0;
+    if (drafts > 0) return false;
+    const uint64_t bits = p.tree[q0 + token] & (nq >= 64 ? ~0ull : (1ull << nq) - 1);
+    return drafts <= -64 || (bits >> -drafts) == 0;
+}
+
 __device__ __forceinline__ int64_t cached_uniform(int64_t x)
 {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
@@ -184,7 +194,7 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
         const int64_t item = cached_item(p, seq, s, C::ROWS) + tile;
         if (j0 == 0 && kv == 0 && threadIdx.x == 0) {      // the last step's range is the last that begins at or before it, at floor(range * total / ranges)
             const int last = j1 == seq.steps ? range : (int)(((base + (int64_t)(tile + 1) * length) * ranges - 1) / total);
-            p.spans[item] = {range, last - range + 1, seq.q0, tile * C::ROWS, seq.nq * p.group};
+            p.spans[item] = {range, last - range + 1, seq.q0, tile * C::ROWS, seq.nq * p.group, seq.len};
         }
         __syncthreads();                                   // the LDS of the range's last piece is free
         if (threadIdx.x == 0) dirty = 0;
@@ -357,7 +367,8 @@ __global__ __launch_bounds__((CachedTile<DP, MANY>::WAVES * 64), MANY ? 2 : 1) v
             w[i] = __builtin_amdgcn_exp2f(stats[0][i][member * 32 + (lane & 31)] - ms);
             l += w[i] * stats[1][i][member * 32 + (lane & 31)];
         }
-        const bool partial = j0 > 0 || j1 < seq.steps, there = row < nrows, none = m == -__builtin_inff() && l == 0.0f;
+        const bool partial = j0 > 0 || j1 < seq.steps, there = row < nrows;
+        const bool none = m == -__builtin_inff() && l == 0.0f && cached_sees_nothing(p, seq.q0, seq.nq, seq.len, token);
         const float inv = partial ? 1.0f : none ? 0.0f : 1.0f / l;
         float *to = nullptr;
         if (partial) to = p.part + ((range + item) * p.kv_heads + kv) * (C::ROWS * (DP + 2));
@@ -461,7 +472,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(CachedParams p)
                 w[i] = __builtin_amdgcn_exp2f(stats[0][i][r] - ms);
                 l += w[i] * stats[1][i][r];
             }
-            const bool none = m == -__builtin_inff() && l == 0.0f;
+            const bool none = m == -__builtin_inff() && l == 0.0f && row < nrows && cached_sees_nothing(p, q0, span.rows / p.group, span.len, token - q0);
             inv = none ? 0.0f : 1.0f / l;
             if (blockIdx.z == 0 && part == 0 && row < nrows && p.lse)
                 p.lse[(int64_t)head * p.Tq + token] = none ? -__builtin_inff() : LN2 * (m + __builtin_amdgcn_logf(l));

@@ -38,9 +38,9 @@ int64_t bwd_workgroups(const BwdParams &p);
 size_t bwd_bytes(int64_t Tq, int heads);
 hipError_t launch_attention_bwd(const BwdParams &p, hipStream_t s);
 
-// Who has a part of a tile of rows: the first range and how many ranges; the sequence's first row of Q, the tile's first row and the sequence's number of rows (times the group)
+// Who has a part of a tile of rows: the first range and how many ranges; the sequence's first row of Q, the tile's first row and the sequence's number of rows (times the group), its keys
 struct CachedSpan {
-    int32_t first, parts, q0, row, rows;
+    int32_t first, parts, q0, row, rows, len;
 };
 // Rows of Q over a paged cache
 struct CachedParams {

@@ -6,8 +6,9 @@ import pytest
 import torch
 
 from tests import attn_ref as R
-from tests.test_gpu_attention import behind_empty, coda  # noqa: F401
+from tests.test_gpu_attention import behind_empty, coda, device, offsets  # noqa: F401
 from tests.test_gpu_attention_bwd import Pass
+from tests.test_gpu_attention_cached import Cache
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,28 @@ def test_gradients_with_an_infinite_element_of_the_outputs_gradient(coda, rows, 
             assert not torch.isfinite(x[left_out]).any(), name
             x[left_out] = w[left_out]
         R.check(x, w, b, name)
+
+
+@pytest.mark.parametrize("D", [64, 128, 96])
+@pytest.mark.parametrize("lens,rows,tree", [([40, 3, 2], [1, 1, 2], None), ([6000, 5], [1, 3], None), ([300], [40], None), ([6000, 70], [33, 70], None), ([20, 3, 9], [4, 5, 1], "rows"),
+                                            ([300, 40], [40, 40], "rows"), ([50], [60], "nobody"), ([6000, 4], [20, 70], "nobody")])
+def test_rows_that_see_keys_of_no_weight_alone(coda, lens, rows, tree, D):
+    """Every score is -inf: NaN, with a log-sum-exp of -inf, as coda_attention has it; rows that see no key are zeros"""
+    c = Cache(coda, lens, rows, 4, 2, D, 16, seed=D + len(lens), tree={None: None, "rows": lambda n: [1 << i for i in range(n)], "nobody": lambda n: [0] * n}[tree])
+    for h in range(4):
+        c.Q[:, h * D] = c.Q[:, h * D].abs() + 0.25
+    for g in range(2):
+        c.K[:, g * D] = -math.inf
+    coda.coda_cache_store(c.K, c.V, c.slots, c.k, c.v)
+    out, lse = c.run()
+    assert (lse == -math.inf).all()
+    k_at = offsets(lens)
+    for s, (a, b) in enumerate(zip(c.q_at, c.q_at[1:])):
+        n = lens[s]
+        see = R.visible(b - a, n, True) if tree is None else R.tree_visible(b - a, n, c.bits[a:b])
+        some = see.any(1)
+        assert torch.isnan(out[a:b][some]).all() and (out[a:b][~some] == 0).all(), s
+        if tree is None:
+            plain, m = torch.empty_like(out[a:b]), torch.empty((4, b - a), device="cuda")
+            coda.coda_attention(c.Q[a:b], c.K[k_at[s]: k_at[s + 1]], c.V[k_at[s]: k_at[s + 1]], device([0, b - a]), plain, 4, 2, c.scale, lse=m, seq_k=device([0, n]))
+            assert torch.equal(plain.isnan(), out[a:b].isnan()) and torch.equal(plain.nan_to_num(), out[a:b].nan_to_num()) and torch.equal(m, lse[:, a:b])
