@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256, DP == 128 && SPLIT == 4 ? 1 : 2) void attentio
     const int64_t t = tiles - 1 - blockIdx.x / p.heads;
     int head = blockIdx.x % p.heads;
     if (p.heads % 8 == 0) head = head % 8 * (p.heads / 8) + head / 8;
-    const int s = attn_find(p.seq_q, p.n_seqs, 1, ROWS, t, lane);
+    const int s = attn_find(p.seq_q, p.n_seqs, ROWS, t, lane);
     const AttnSpan q = attn_span_of_wave(p.seq_q, s, p.Tq), k = attn_span_of_wave(p.seq_k, s, p.Tk);
     const int64_t first = (t - (max(p.seq_q[s], 0) / ROWS + s)) * ROWS;
     if (first < 0 || first >= q.count) return;

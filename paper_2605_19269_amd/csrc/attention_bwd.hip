@@ -88,7 +88,7 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
     const int kb = wave % KB, stream = wave / KB;
     const int64_t t = blockIdx.x / p.f.kv_heads;
     const int kv = blockIdx.x % p.f.kv_heads;
-    const int s = attn_find(p.f.seq_k, p.f.n_seqs, 1, KEYS, t, lane);
+    const int s = attn_find(p.f.seq_k, p.f.n_seqs, KEYS, t, lane);
     const AttnSpan q = attn_span_of_wave(p.f.seq_q, s, p.f.Tq), k = attn_span_of_wave(p.f.seq_k, s, p.f.Tk);
     const int64_t first = (t - (max(p.f.seq_k[s], 0) / KEYS + s)) * KEYS;
     if (first < 0 || first >= k.count) return;
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(KB * NS * 64, KB * NS / 4) void attention_dkv_kerne
         for (int u = 0; u < 2; ++u) x[u] = attn_operand(dp, u);
         attn_values<DP, 1, 4>(cols, x, dk);
     }
-    attn_wait();                                           // the last round's loads for the next, of rows that there are none of: where the parts come they may still leave zeros
+    attn_wait();                                           // the last round's loads for the next, which go where the parts come
     if (KB > 1 && !behind) attn_barrier();
     // The streams' parts are added up in their order: all of dK, then all of dV through LDS, and a stream finishes every NS-th 32 columns
     const int64_t row = (int64_t)k.begin + key;
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(256, DP == 64 && SPLIT < 4 ? 3 : 2) void attention_
     const int64_t t = tiles - 1 - blockIdx.x / p.f.heads;
     int head = blockIdx.x % p.f.heads;
     if (p.f.heads % 8 == 0) head = head % 8 * (p.f.heads / 8) + head / 8;
-    const int s = attn_find(p.f.seq_q, p.f.n_seqs, 1, ROWS, t, lane);
+    const int s = attn_find(p.f.seq_q, p.f.n_seqs, ROWS, t, lane);
     const AttnSpan q = attn_span_of_wave(p.f.seq_q, s, p.f.Tq), k = attn_span_of_wave(p.f.seq_k, s, p.f.Tk);
     const int64_t first = (t - (max(p.f.seq_q[s], 0) / ROWS + s)) * ROWS;
     if (first < 0 || first >= q.count) return;

@@ -41,23 +41,17 @@ __device__ __forceinline__ void attn_load16(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
-// The same from a uniform address and a lane's offset, by the lanes of `mask` alone, which need be none; what the others' 16 bytes of LDS hold stays.  No branch: the
-// callers issue these among their products, and a branch would part those.
 __device__ __forceinline__ uint64_t attn_uniform(uint64_t a)
 {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a);
-}
-__device__ __forceinline__ void attn_load16(const void *base, uint32_t off, uint32_t lds, uint64_t mask)
-{
-    uint64_t all;
-    asm volatile("s_mov_b64 %0, exec\n\ts_mov_b64 exec, %4\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, %0"
-                 : "=&s"(all) : "v"(off), "s"(attn_uniform(reinterpret_cast<uint64_t>(base))), "s"(lds), "s"(attn_uniform(mask)) : "memory", "m0");
 }
 // Four bytes a lane
 __device__ __forceinline__ void attn_load4(const void *p, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(p), "s"(lds) : "memory", "m0");
 }
+// The same from a uniform address and a lane's offset, by the lanes of `mask` alone, which need be none; what the others' four bytes of LDS hold stays.  No branch: the
+// callers issue these among their products, and a branch would part those.
 __device__ __forceinline__ void attn_load4(const void *base, uint32_t off, uint32_t lds, uint64_t mask)
 {
     uint64_t all;
@@ -87,7 +81,8 @@ __device__ __forceinline__ void attn_barrier()
 }
 
 // Tiles of ROWS rows of one head, loaded by NW waves together, 1 KB a load.  Loads go through a buffer descriptor that ends with the last row of the tile that there is, so rows behind it need no
-// mask: the card drops lanes past the end, and with them, in PAD kernels, those whose chunk is not below D (attn_zero() has cleared those).  A load is two instructions;
+// mask: lanes past the end read nothing from memory, and in PAD kernels those whose chunk is not below D are sent there too.  Their 16 bytes of LDS keep what they held or become zeros, and nothing
+// relies on either: what lies behind the last row is masked by selection and cleared where it is not finite, and chunks not below D were cleared by attn_zero().  A load is two instructions;
 // masks and 64-bit addresses took 18, a quarter of all that the forward kernel's loop issued.
 template <int DP, bool PAD, int ROWS, int NW>
 struct AttnLoad {
@@ -235,7 +230,7 @@ __device__ __forceinline__ u32x4 attn_store_unit(const float (&lo)[4], const flo
 // A weight of zero times an infinity or a NaN is NaN, so a row of V that is not finite would reach rows that do not see it.  Tiles that no mask
 // touches need nothing.  In the others (one or two for a tile of rows) what is not finite is replaced by zero in LDS before the products, and
 // only where there was any, its effect on the rows that do see it is added at the end: a product of the mask (0 or 1) with marks (+inf 1, -inf 2^10,
-// NaN 2^20; sums over a tile are exact in fp32) tells for each output whether it met +inf, -inf, both or a NaN.  Whatever order a sum takes
+// NaN 2^20) tells for each output whether it met +inf, -inf, both or a NaN: sums below 2^20 are exact in fp32, above it only that they are counts.  Whatever order a sum takes
 // these in, the result is the same, so the end is early enough.
 
 // Not zero if one of eight elements is not finite
@@ -464,12 +459,12 @@ __device__ __forceinline__ AttnSpan attn_span_of_wave(const int32_t *at, int s, 
 // Tiles of `rows` rows are numbered from begin / rows + s in sequence s, so that the number of a tile gives its sequence without anyone having
 // counted the tiles: the next sequence's first number is never below this one's last plus one.  Numbers that no sequence uses do nothing.
 // Returns the last sequence whose first number is not above t; 64 candidates are looked at at once.
-__device__ __forceinline__ int attn_find(const int32_t *at, int n_seqs, int64_t unit, int rows, int64_t t, int lane)
+__device__ __forceinline__ int attn_find(const int32_t *at, int n_seqs, int rows, int64_t t, int lane)
 {
     int lo = 0, width = n_seqs;
     while (width > 1) {
         const int step = (width + 63) / 64, i = lane * step;
-        const bool below = i < width && (int64_t)max(at[lo + i], 0) * unit / rows + lo + i <= t;
+        const bool below = i < width && (int64_t)(max(at[lo + i], 0) / rows) + lo + i <= t;
         const int k = __popcll(__ballot(below));
         if (k > 1) lo += (k - 1) * step;
         width = min(step, n_seqs - lo);
