@@ -388,7 +388,8 @@ CODA_API size_t coda_grad_scaled_workspace_bytes(int64_t M, int64_t N, int64_t K
  *     S_ij = scale * q_i . k_j       lse_i = log sum_j exp S_ij       out_i = sum_j exp(S_ij - lse_i) v_j
  *
  * over the keys j of row i's sequence, with causal != 0 those up to j = i + keys - rows (both counted from the sequence's start: the last row
- * sees all keys).  A row that sees no key is zeros with lse = -inf.  What a row does not see has no effect on it, infinities and NaN included.
+ * sees all keys).  A row that sees no key is zeros with lse = -inf (one that sees keys, all with a score of -inf, is NaN with lse = -inf).  What a row does
+ * not see has no effect on it, infinities and NaN included.  An infinity of V whose weight fp32 holds as zero is that infinity or NaN in the row's output.
  * lse (natural logarithm): f32 [heads x Tq], may be NULL.  scale is positive and below 2^127, and neither
  * Tk nor Tq times heads / kv_heads is above 2^31 - 512 (CODA_ERR_SHAPE).
  *
@@ -413,7 +414,8 @@ typedef struct coda_rope {
  * the QKV projection's outputs before its ROPE epilogue (pairs of columns of all D; D a multiple of 8 as there).
  * dQ, dK, dV: bf16 of the shapes of Q, K, V, overwritten; they may be column blocks of one matrix.  Rows of no sequence are left as they are; a key
  * that no row sees has gradients of zero.  P and dS are rounded to bf16 for their products (dS in two parts for that of dQ), sums are fp32; the order of additions depends on the
- * sizes only (no atomics).  A row of dO that is not finite makes NaN or infinities of what it reaches, and of nothing else.
+ * sizes only (no atomics).  What is not finite reaches what the formulas have it in, whatever the sizes, and nothing else: an element of dO its column of dV (as in V above), the dK of the keys that
+ * its row sees and its row of dQ; an infinity of K with a score of -inf, whose weight is zero, its column of dQ (as NaN, zero times an infinity) for the rows that see the key.
  * workspace: device memory, 16-byte aligned, coda_attention_bwd_workspace_bytes(...) bytes (CODA_ERR_WORKSPACE below that); it holds nothing
  * between calls, and two calls that share one must not overlap in time.
  */
