@@ -3,7 +3,7 @@
 //   S_ij = scale q_i . k_j,  lse_i = log sum_j exp S_ij,  o_i = sum_j exp(S_ij - lse_i) v_j   over the keys j that row i sees
 //
 // in one pass over the keys with the running maximum and sum of each row (attn_tile.hpp).  Bound by exponentials and products, which share a wave's issue: a workgroup of four waves has 128 rows and tiles of 64
-// keys, K and V doubly buffered in 64 KB of LDS at 128 columns, two workgroups a CU.  32 heads over 8 of 128 columns: 16384 rows 2040 to 2150 us (1020 to 1080 TFLOP/s), 8192 in six
+// keys, K and V doubly buffered in 64 KB of LDS at 128 columns, two workgroups a CU.  32 heads over 8 of 128 columns: 16384 rows 1980 us (1110 TFLOP/s) once the clock has settled, up to 2150 before; 8192 in six
 // sequences 195 to 204 (880 to 920).
 #include "attn_launch.hpp"
 #include "attn_tile.hpp"

@@ -5,9 +5,10 @@
 //
 // Two kernels, no atomics: dQ, a workgroup for 128 rows, over the keys, which also leaves the row statistics; dK and dV, a workgroup for 64 keys of a key / value
 // head, over all rows of all heads of the group.  S and dO V^T are formed in both (eight products, with dS in two parts, where five would do): the
-// alternative, dQ added up in fp32 across workgroups, is either of no fixed order or a partial of every row for every tile of keys.  Bound by the issue of vector instructions and products
-// on one port, dK and dV at 128 columns also by LDS: 4 x 2048 rows, 32 heads over 8 of 64 columns, 154 + 193 us (790 TFLOP/s over the eight products), 8192 rows in six
-// sequences of 128 columns 352 + 422 (930).
+// alternative, dQ added up in fp32 across workgroups, is either of no fixed order or a partial of every row for every tile of keys.  dQ is bound by vector instructions and
+// products, which take the time of a SIMD in turn (53 and 44 % of it at 64 columns, 38 and 53 % at 128); dK and dV at 64 columns by neither (34 and 33 %) but by waiting for each other, two barriers of eight waves for 32 rows, at 128
+// columns by products, LDS and vector instructions in turn (41, 33 and 29 %): 4 x 2048 rows, 32 heads over 8 of 64 columns, 146 + 169 us (870 TFLOP/s over the eight products), 8192 rows in six
+// sequences of 128 columns 327 + 395 (990), once the clock has settled; 152 + 192 and 345 + 414 from idle, as all further figures here are.
 #include "attn_launch.hpp"
 #include "attn_tile.hpp"
 

@@ -509,7 +509,10 @@ __global__ __launch_bounds__(256) void cache_store_kernel(const uint16_t *K, int
     *reinterpret_cast<u32x4 *>(v + to) = *reinterpret_cast<const u32x4 *>(V + t * ldv + col);
 }
 
-// Tiles of 128 rows once a sequence has more than 32 on average
+// Tiles of 128 rows once a sequence has more than 32 on average, which tiles of 32 would go over all keys twice for.  us with 32 / 128, 32 heads over 8, each sequence of 16, 32, 36, 64 and 128 rows (tokens times group): 64
+// columns, one sequence of 4096 keys 12.4 / 15.0, 12.6 / 15.2, 13.8 / 15.5, 14.1 / 15.6, 15.0 / 16.5; eight 23.5 / 26.7, 24.0 / 27.0, 26.0 / 27.6, 26.7 / 28.2, 33.2 / 30.6; 32 of 2048 32.5 / 34.8, 32.6 / 35.0, 53.5 / 35.2, 54.0 / 36.1, 92.5 / 40.1.
+// 128 columns, one 15.3 / 18.2, 16.0 / 18.5, 15.4 / 19.0, 16.2 / 19.6, 18.0 / 21.6; eight 34.6 / 39.6, 35.8 / 40.3, 37.0 / 41.1, 38.7 / 42.6, 52.6 / 47.5; 32 54.1 / 56.8, 54.8 / 57.4, 93.4 / 57.8, 94.4 / 58.7, 168.8 / 63.7.  A lone sequence loses
+// up to a quarter by it, eight a tenth just above 32 rows, and as many as fill the card's time with their keys gain a third or more.
 static bool cached_many(int64_t Tq, int n_seqs, int group) { return Tq * group > 32 * (int64_t)n_seqs; }
 // One workgroup for each CU
 static int cached_ranges(int kv_heads) { return (256 + kv_heads - 1) / kv_heads; }
